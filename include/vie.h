@@ -360,6 +360,120 @@ vie_status vie_scatter(const int32_t *ids_dev, const float *logits_dev, int32_t 
                        float *out_dev, void *hip_stream);
 
 /* ------------------------------------------------------------------------
+ * Around the head's logits: the int8 head, the token drawn, distillation
+ * ------------------------------------------------------------------------
+ * Full-vocabulary rows may be strided: row b starts at element b * ld, ld >=
+ * V; what lies between rows is neither read nor written.  Workspaces are
+ * 256-byte aligned device buffers of the caller's, need no initialisation,
+ * and carry data between the kernels of one call only: calls that share one
+ * must not overlap in time. */
+
+/* Bytes of device workspace vie_int8_logits needs for these sizes. */
+vie_status vie_int8_logits_workspace(int64_t V, int32_t d, int32_t B, size_t *bytes);
+
+/* The head on int8 rows (quantized data types are the paper's future work,
+ * Section 5): the full-vocabulary logits of B tokens from q_dev int8[V][d]
+ * and scale_dev fp32[V], as vie_quantize_rows writes them (values in [-127,
+ * 127]; any alignment).  Each token h_dev [B][d] of h_dtype is quantized by
+ * the same rule (scale xs, values x; a token with a NaN or an infinity gets
+ * the scale NaN), and
+ *   out[b][v] = fp32(fp32(fp32(sum_j q[v][j] x[b][j]) scale[v]) xs[b])
+ * with an exact integer sum, rounded to nearest even if out_dtype is
+ * VIE_BF16.  out_dev [B][out_ld] must not overlap the inputs.
+ * Errors: VIE_EINVAL, VIE_EHIP. */
+vie_status vie_int8_logits(const int8_t *q_dev, const float *scale_dev, int64_t V, int32_t d, const void *h_dev,
+                           vie_dtype h_dtype, int32_t B, void *out_dev, vie_dtype out_dtype, int64_t out_ld,
+                           void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/* How a token is drawn.  A setting applies to every row whose array (device
+ * memory, one value per row) is NULL. */
+typedef struct {
+    float temperature;            /* <= 0 or NaN: the best candidate */
+    int32_t top_k;                /* <= 0: no limit */
+    float top_p;                  /* >= 1 or NaN: no limit */
+    float min_p;                  /* <= 0 or NaN: no limit */
+    const float *temperature_dev; /* fp32[B] or NULL */
+    const int32_t *top_k_dev;     /* int32[B] or NULL */
+    const float *top_p_dev;       /* fp32[B] or NULL */
+    const float *min_p_dev;       /* fp32[B] or NULL */
+} vie_sample_params;
+
+/* Draws one token per list ids_dev int32[B][k], logits_dev fp32[B][k] (the
+ * lists of vie_dense_topk, vie_query and vie_query_forced; 1 <= k <= 2048)
+ * from the uniform numbers u_dev fp32[B] in [0, 1).
+ *   Candidates are the entries with id >= 0 and a logit above -inf (a NaN is
+ * none), ordered by logit descending, then id ascending, whatever their
+ * order in the list.  With l_1 the best logit and t the temperature,
+ * candidate j weighs w_j = exp((l_j - l_1) / t) (1 where l_j = l_1, else 0
+ * where l_1 is +inf) and C_j = w_1 + .. + w_j.  Kept is the shortest of three prefixes, and at least one
+ * candidate: the first K = min(top_k, candidates); the first n with C_n >=
+ * top_p C_K; those with w_j >= min_p.  The token is the first j with C_j > u
+ * C_kept.  Sums are 64-bit integers of weights rounded to 2^-44 of the best
+ * one or finer (for up to 2^18 candidates), so results do not depend on the
+ * order of additions.
+ *   token_dev int32[B] receives the id, prob_dev fp32[B] (or NULL) its
+ * probability w_j / C_kept, kept_dev int32[B] (or NULL) the number of kept
+ * candidates; a greedy draw (temperature <= 0) gives probability 1 and 1
+ * kept.  A list without candidates gives -1, 0 and 0.
+ * Errors: VIE_EINVAL, VIE_EHIP. */
+vie_status vie_sample(const int32_t *ids_dev, const float *logits_dev, int32_t B, int32_t k,
+                      const vie_sample_params *params, const float *u_dev, int32_t *token_dev, float *prob_dev,
+                      int32_t *kept_dev, void *hip_stream);
+
+/* Bytes of device workspace vie_sample_rows needs for these sizes. */
+vie_status vie_sample_rows_workspace(int64_t V, int32_t B, size_t *bytes);
+
+/* vie_sample over full-vocabulary rows logits_dev [B][ld] of dtype (of
+ * vie_int8_logits or vie_scatter): the candidates of a row are its ids 0 ..
+ * V - 1 whose logit is above -inf (a NaN is none), so a mask is a logit of
+ * -inf.  The same rule and results as for a list of those candidates (the
+ * integer sums are coarser for more than 2048 of them).
+ * Errors: VIE_EINVAL, VIE_EHIP. */
+vie_status vie_sample_rows(const void *logits_dev, vie_dtype dtype, int64_t V, int64_t ld, int32_t B,
+                           const vie_sample_params *params, const float *u_dev, int32_t *token_dev, float *prob_dev,
+                           int32_t *kept_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/* Bytes of device workspace vie_distill and vie_distill_step need. */
+vie_status vie_distill_workspace(int64_t V, int32_t N, size_t *bytes);
+
+/* Distillation from a teacher's top logits, forward: the loss of N tokens
+ * with the student's logits s = logits_dev [N][ld] of dtype over V ids and
+ * the teacher's lists ids_dev int32[N][k], teacher_dev fp32[N][k] (as the
+ * heads return them; 1 <= k <= 2048), at the temperature tau (1e-4 to 1e4):
+ *   p = softmax of teacher / tau over the listed entries (id in [0, V) and
+ *   logit not -inf), q = softmax of s / tau over the V ids,
+ *   loss = tau^2 sum_j p_j (log p_j - log q[id_j])
+ * (entries whose p_j rounds to zero add nothing).  An id listed more than
+ * once counts with each of its entries.  A row that lists nothing has loss 0.  A NaN or +inf
+ * among the logits of either side gives NaN, as does a row of the student's
+ * that is -inf throughout.  loss_dev fp32[N]; stats_dev fp32[N][2] receives what
+ * vie_distill_grad needs: the row's largest logit and the sum of
+ * exp((s - largest) / tau).
+ * Errors: VIE_EINVAL, VIE_EHIP. */
+vie_status vie_distill(const void *logits_dev, vie_dtype dtype, int32_t N, int64_t V, int64_t ld,
+                       const int32_t *ids_dev, const float *teacher_dev, int32_t k, float tau, float *loss_dev,
+                       float *stats_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/* Distillation, backward: grad[n][v] = g_n tau (q[n][v] - p[n][v]), rounded
+ * to dtype, with g_n = weight gloss_dev[n] (gloss_dev NULL: weight) and p[n][v]
+ * the sum of the p_j with id_j = v; 0 in a row that lists nothing.  stats_dev
+ * as vie_distill wrote it for the same logits and tau.  grad_dev [N][grad_ld]
+ * is logits_dev itself (with its stride) or does not overlap it.
+ * Errors: VIE_EINVAL, VIE_EHIP. */
+vie_status vie_distill_grad(const void *logits_dev, vie_dtype dtype, int32_t N, int64_t V, int64_t ld,
+                            const int32_t *ids_dev, const float *teacher_dev, int32_t k, float tau,
+                            const float *stats_dev, const float *gloss_dev, float weight, void *grad_dev,
+                            int64_t grad_ld, void *hip_stream);
+
+/* vie_distill and vie_distill_grad in one call, for a training step that
+ * knows g_n beforehand (1 / N for a mean): the same losses and gradients.
+ * Errors: VIE_EINVAL, VIE_EHIP. */
+vie_status vie_distill_step(const void *logits_dev, vie_dtype dtype, int32_t N, int64_t V, int64_t ld,
+                            const int32_t *ids_dev, const float *teacher_dev, int32_t k, float tau,
+                            const float *gloss_dev, float weight, float *loss_dev, void *grad_dev, int64_t grad_ld,
+                            void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/* ------------------------------------------------------------------------
  * Diagnostics
  * ------------------------------------------------------------------------ */
 

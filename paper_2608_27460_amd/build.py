@@ -18,7 +18,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 OUT_DIR = os.path.join(PKG, "lib")
 LIB = os.path.join(OUT_DIR, "libvie.so")
-SOURCES = ["kernels.hip", "knn_build.hip", "api.cpp", "builder.cpp", "index_io.cpp"]
+SOURCES = ["kernels.hip", "knn_build.hip", "int8_head.hip", "sample.hip", "distill.hip", "api.cpp", "operators.cpp",
+           "builder.cpp", "index_io.cpp"]
 ARCH = "gfx950"
 
 

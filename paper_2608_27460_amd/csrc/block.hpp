@@ -1,0 +1,122 @@
+// Wave and workgroup helpers shared by the operators' kernels.  A workgroup
+// is a whole number of 64-lane waves and every lane takes part.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace vie {
+
+constexpr int kLanes = 64;
+
+typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float from_bf16(uint32_t bits) { return __uint_as_float(bits << 16); }
+
+__device__ __forceinline__ uint16_t to_bf16(float v)  // nearest, ties to even
+{
+    return __builtin_bit_cast(uint16_t, (__bf16)v);
+}
+
+// Element types of rows: fp32, and bf16 as raw bits.
+template <bool BF16> struct Elem {
+    typedef float T;
+    static constexpr int kVec = 4;  // elements of 16 bytes
+    static __device__ __forceinline__ float get(T v) { return v; }
+    static __device__ __forceinline__ T put(float v) { return v; }
+    static __device__ __forceinline__ void unpack(word4 w, float *f)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(w[i]);
+    }
+    static __device__ __forceinline__ word4 pack(const float *f)
+    {
+        word4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(f[i]);
+        return w;
+    }
+};
+template <> struct Elem<true> {
+    typedef uint16_t T;
+    static constexpr int kVec = 8;
+    static __device__ __forceinline__ float get(T v) { return from_bf16(v); }
+    static __device__ __forceinline__ T put(float v) { return to_bf16(v); }
+    static __device__ __forceinline__ void unpack(word4 w, float *f)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(w[i] << 16);
+            f[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+    }
+    static __device__ __forceinline__ word4 pack(const float *f)
+    {
+        word4 w;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[i] = (uint32_t)to_bf16(f[2 * i]) | (uint32_t)to_bf16(f[2 * i + 1]) << 16;
+        return w;
+    }
+};
+
+// n elements from p on: `head` of them up to the first 16-byte boundary, then
+// `vecs` groups of 16 bytes, then the rest.
+template <typename T> struct Span {
+    int64_t head, vecs, tail0;
+    __device__ __forceinline__ Span(const T *p, int64_t n)
+    {
+        const int64_t h = (int64_t)((16 - ((uintptr_t)p & 15)) & 15) / (int64_t)sizeof(T);
+        head = h < n ? h : n;
+        vecs = (n - head) / (16 / (int64_t)sizeof(T));
+        tail0 = head + vecs * (16 / (int64_t)sizeof(T));
+    }
+};
+
+template <typename T> __device__ __forceinline__ T wave_sum(T v)
+{
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, kLanes);
+    return v;
+}
+template <typename T> __device__ __forceinline__ T wave_max(T v)
+{
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) {
+        const T x = __shfl_xor(v, o, kLanes);
+        v = x > v ? x : v;
+    }
+    return v;
+}
+// Inclusive sums over the lanes of a wave.
+template <typename T> __device__ __forceinline__ T wave_scan(T v)
+{
+    const int lane = threadIdx.x & (kLanes - 1);
+#pragma unroll
+    for (int o = 1; o < kLanes; o <<= 1) {
+        const T x = __shfl_up(v, o, kLanes);
+        if (lane >= o) v += x;
+    }
+    return v;
+}
+
+// The value `combine` makes of every thread's v, in every thread; the order
+// of combination is fixed.  `tmp`: NT / 64 values of LDS, free again after the
+// next barrier.
+template <int NT, typename T, typename F> __device__ __forceinline__ T block_reduce(T v, T *tmp, F combine)
+{
+    constexpr int W = NT / kLanes;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v = combine(v, __shfl_xor(v, o, kLanes));
+    if constexpr (W > 1) {
+        __syncthreads();
+        if ((threadIdx.x & (kLanes - 1)) == 0) tmp[threadIdx.x / kLanes] = v;
+        __syncthreads();
+        v = tmp[0];
+#pragma unroll
+        for (int w = 1; w < W; ++w) v = combine(v, tmp[w]);
+    }
+    return v;
+}
+
+}  // namespace vie

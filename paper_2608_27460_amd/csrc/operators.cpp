@@ -1,0 +1,194 @@
+// C ABI of the operators around the head's logits (include/vie.h): the int8
+// head, sampling and distillation.  Arguments are checked here, before
+// anything is enqueued.
+#include <hip/hip_runtime.h>
+
+#include "operators.hpp"
+
+using namespace vie;
+
+namespace {
+
+vie_status check_type(int32_t dtype, const char *what)
+{
+    if (dtype != VIE_F32 && dtype != VIE_BF16) return fail(VIE_EINVAL, "unknown dtype %d of %s", dtype, what);
+    return VIE_OK;
+}
+
+vie_status check_rows(int32_t B, int64_t V)
+{
+    if (B < 1 || B > 65535) return fail(VIE_EINVAL, "%d rows out of range [1, 65535]", B);
+    if (V < 1 || V >= (int64_t(1) << 31)) return fail(VIE_EINVAL, "V = %lld out of range", (long long)V);
+    return VIE_OK;
+}
+
+// Rows of V values, ld values apart, aligned to their type.
+vie_status check_matrix(const void *p, int32_t dtype, int64_t V, int64_t ld, const char *what)
+{
+    if (vie_status s = check_type(dtype, what)) return s;
+    if (ld < V || ld >= (int64_t(1) << 40))
+        return fail(VIE_EINVAL, "row stride %lld of %s outside [V, 2^40)", (long long)ld, what);
+    if ((uintptr_t)p % elem_bytes(dtype)) return fail(VIE_EINVAL, "%s is not aligned to its type", what);
+    return VIE_OK;
+}
+
+vie_status check_list(int32_t k)
+{
+    if (k < 1 || k > kMaxList) return fail(VIE_EINVAL, "k = %d out of range [1, %d]", k, kMaxList);
+    return VIE_OK;
+}
+
+vie_status check_workspace(const void *ws, size_t have, size_t need)
+{
+    if (need == 0) return VIE_OK;
+    if (!ws) return fail(VIE_EINVAL, "NULL workspace (%zu bytes needed)", need);
+    if ((uintptr_t)ws % 256) return fail(VIE_EINVAL, "workspace is not 256-byte aligned");
+    if (have < need) return fail(VIE_EINVAL, "workspace holds %zu bytes, needs %zu", have, need);
+    return VIE_OK;
+}
+
+vie_status check_distill(const void *logits, int32_t dtype, int32_t N, int64_t V, int64_t ld, const int32_t *ids,
+                         const float *teacher, int32_t k, float tau)
+{
+    if (!logits || !ids || !teacher) return fail(VIE_EINVAL, "NULL argument");
+    if (vie_status s = check_rows(N, V)) return s;
+    if (vie_status s = check_matrix(logits, dtype, V, ld, "logits")) return s;
+    if (vie_status s = check_list(k)) return s;
+    if (!(tau >= 1e-4f && tau <= 1e4f)) return fail(VIE_EINVAL, "tau = %g outside [1e-4, 1e4]", (double)tau);
+    return VIE_OK;
+}
+
+// The gradient's rows are the logits' own or apart from them.
+vie_status check_apart(const DistillLaunch &a)
+{
+    if (a.grad == a.logits) {
+        if (a.grad_ld != a.ld && a.N > 1)
+            return fail(VIE_EINVAL, "a gradient in place of the logits needs their row stride");
+        return VIE_OK;
+    }
+    const size_t e = (size_t)elem_bytes(a.dtype);
+    const uintptr_t p = (uintptr_t)a.logits, pe = p + ((size_t)(a.N - 1) * a.ld + a.V) * e;
+    const uintptr_t g = (uintptr_t)a.grad, ge = g + ((size_t)(a.N - 1) * a.grad_ld + a.V) * e;
+    if (p < ge && g < pe) return fail(VIE_EINVAL, "the gradient overlaps the logits without being in their place");
+    return VIE_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+vie_status vie_int8_logits_workspace(int64_t V, int32_t d, int32_t B, size_t *bytes)
+{
+    set_error("%s", "");
+    if (!bytes) return fail(VIE_EINVAL, "NULL argument");
+    if (vie_status s = check_rows(B, V)) return s;
+    if (d < 1 || d > kMaxD) return fail(VIE_EINVAL, "d = %d out of range [1, %d]", d, kMaxD);
+    *bytes = int8_workspace_bytes(V, d, B);
+    return VIE_OK;
+}
+
+vie_status vie_int8_logits(const int8_t *q_dev, const float *scale_dev, int64_t V, int32_t d, const void *h_dev,
+                           vie_dtype h_dtype, int32_t B, void *out_dev, vie_dtype out_dtype, int64_t out_ld,
+                           void *workspace_dev, size_t workspace_bytes, void *hip_stream)
+{
+    set_error("%s", "");
+    if (!q_dev || !scale_dev || !h_dev || !out_dev) return fail(VIE_EINVAL, "NULL argument");
+    if (vie_status s = check_rows(B, V)) return s;
+    if (d < 1 || d > kMaxD) return fail(VIE_EINVAL, "d = %d out of range [1, %d]", d, kMaxD);
+    if (vie_status s = check_matrix(h_dev, h_dtype, d, d, "h")) return s;
+    if (vie_status s = check_matrix(out_dev, out_dtype, V, out_ld, "the logits")) return s;
+    if ((uintptr_t)scale_dev % 4) return fail(VIE_EINVAL, "scale is not aligned to its type");
+    if (vie_status s = check_workspace(workspace_dev, workspace_bytes, int8_workspace_bytes(V, d, B))) return s;
+    const Int8Launch a{q_dev, scale_dev, V, d, h_dev, h_dtype, B, out_dev, out_dtype, out_ld, workspace_dev};
+    return launch_int8_logits(a, static_cast<hipStream_t>(hip_stream));
+}
+
+vie_status vie_sample(const int32_t *ids_dev, const float *logits_dev, int32_t B, int32_t k,
+                      const vie_sample_params *params, const float *u_dev, int32_t *token_dev, float *prob_dev,
+                      int32_t *kept_dev, void *hip_stream)
+{
+    set_error("%s", "");
+    if (!ids_dev || !logits_dev || !params || !u_dev || !token_dev) return fail(VIE_EINVAL, "NULL argument");
+    if (vie_status s = check_rows(B, 1)) return s;
+    if (vie_status s = check_list(k)) return s;
+    const SampleLaunch a{ids_dev, logits_dev, VIE_F32, k, k, B, *params, u_dev, token_dev, prob_dev, kept_dev, nullptr};
+    return launch_sample_lists(a, static_cast<hipStream_t>(hip_stream));
+}
+
+vie_status vie_sample_rows_workspace(int64_t V, int32_t B, size_t *bytes)
+{
+    set_error("%s", "");
+    if (!bytes) return fail(VIE_EINVAL, "NULL argument");
+    if (vie_status s = check_rows(B, V)) return s;
+    *bytes = sample_rows_workspace_bytes(V, B);
+    return VIE_OK;
+}
+
+vie_status vie_sample_rows(const void *logits_dev, vie_dtype dtype, int64_t V, int64_t ld, int32_t B,
+                           const vie_sample_params *params, const float *u_dev, int32_t *token_dev, float *prob_dev,
+                           int32_t *kept_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream)
+{
+    set_error("%s", "");
+    if (!logits_dev || !params || !u_dev || !token_dev) return fail(VIE_EINVAL, "NULL argument");
+    if (vie_status s = check_rows(B, V)) return s;
+    if (vie_status s = check_matrix(logits_dev, dtype, V, ld, "logits")) return s;
+    if (vie_status s = check_workspace(workspace_dev, workspace_bytes, sample_rows_workspace_bytes(V, B))) return s;
+    const SampleLaunch a{nullptr, logits_dev, dtype, V, ld, B, *params, u_dev, token_dev, prob_dev, kept_dev,
+                         workspace_dev};
+    return launch_sample_rows(a, static_cast<hipStream_t>(hip_stream));
+}
+
+vie_status vie_distill_workspace(int64_t V, int32_t N, size_t *bytes)
+{
+    set_error("%s", "");
+    if (!bytes) return fail(VIE_EINVAL, "NULL argument");
+    if (vie_status s = check_rows(N, V)) return s;
+    *bytes = distill_workspace_bytes(V, N);
+    return VIE_OK;
+}
+
+vie_status vie_distill(const void *logits_dev, vie_dtype dtype, int32_t N, int64_t V, int64_t ld,
+                       const int32_t *ids_dev, const float *teacher_dev, int32_t k, float tau, float *loss_dev,
+                       float *stats_dev, void *workspace_dev, size_t workspace_bytes, void *hip_stream)
+{
+    set_error("%s", "");
+    if (vie_status s = check_distill(logits_dev, dtype, N, V, ld, ids_dev, teacher_dev, k, tau)) return s;
+    if (!loss_dev || !stats_dev) return fail(VIE_EINVAL, "NULL argument");
+    if (vie_status s = check_workspace(workspace_dev, workspace_bytes, distill_workspace_bytes(V, N))) return s;
+    const DistillLaunch a{logits_dev, dtype, N, V, ld, ids_dev, teacher_dev, k, tau, loss_dev, stats_dev,
+                          nullptr, 1.0f, nullptr, 0, workspace_dev};
+    return launch_distill(a, static_cast<hipStream_t>(hip_stream));
+}
+
+vie_status vie_distill_grad(const void *logits_dev, vie_dtype dtype, int32_t N, int64_t V, int64_t ld,
+                            const int32_t *ids_dev, const float *teacher_dev, int32_t k, float tau,
+                            const float *stats_dev, const float *gloss_dev, float weight, void *grad_dev,
+                            int64_t grad_ld, void *hip_stream)
+{
+    set_error("%s", "");
+    if (vie_status s = check_distill(logits_dev, dtype, N, V, ld, ids_dev, teacher_dev, k, tau)) return s;
+    if (!stats_dev || !grad_dev) return fail(VIE_EINVAL, "NULL argument");
+    if (vie_status s = check_matrix(grad_dev, dtype, V, grad_ld, "the gradient")) return s;
+    const DistillLaunch a{logits_dev, dtype, N, V, ld, ids_dev, teacher_dev, k, tau, nullptr,
+                          const_cast<float *>(stats_dev), gloss_dev, weight, grad_dev, grad_ld, nullptr};
+    if (vie_status s = check_apart(a)) return s;
+    return launch_distill_grad(a, static_cast<hipStream_t>(hip_stream));
+}
+
+vie_status vie_distill_step(const void *logits_dev, vie_dtype dtype, int32_t N, int64_t V, int64_t ld,
+                            const int32_t *ids_dev, const float *teacher_dev, int32_t k, float tau,
+                            const float *gloss_dev, float weight, float *loss_dev, void *grad_dev, int64_t grad_ld,
+                            void *workspace_dev, size_t workspace_bytes, void *hip_stream)
+{
+    set_error("%s", "");
+    if (vie_status s = check_distill(logits_dev, dtype, N, V, ld, ids_dev, teacher_dev, k, tau)) return s;
+    if (!loss_dev || !grad_dev) return fail(VIE_EINVAL, "NULL argument");
+    if (vie_status s = check_matrix(grad_dev, dtype, V, grad_ld, "the gradient")) return s;
+    if (vie_status s = check_workspace(workspace_dev, workspace_bytes, distill_workspace_bytes(V, N))) return s;
+    const DistillLaunch a{logits_dev, dtype, N, V, ld, ids_dev, teacher_dev, k, tau, loss_dev, nullptr,
+                          gloss_dev, weight, grad_dev, grad_ld, workspace_dev};
+    if (vie_status s = check_apart(a)) return s;
+    return launch_distill_step(a, static_cast<hipStream_t>(hip_stream));
+}
+
+}  // extern "C"

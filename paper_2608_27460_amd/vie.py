@@ -40,6 +40,12 @@ class GpuBuildParams(C.Structure):
     _fields_ = [("K", C.c_int32), ("M0", C.c_int32), ("chunk_rows", C.c_int64)]
 
 
+class SamplingParams(C.Structure):
+    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float),
+                ("temperature_dev", C.c_void_p), ("top_k_dev", C.c_void_p), ("top_p_dev", C.c_void_p),
+                ("min_p_dev", C.c_void_p)]
+
+
 class IndexDesc(C.Structure):
     _fields_ = [("V", C.c_int64), ("d", C.c_int32), ("dtype", C.c_int32), ("M", C.c_int32), ("M0", C.c_int32),
                 ("ef_construction", C.c_int32), ("maxlevel", C.c_int32), ("entry", C.c_int32),
@@ -51,7 +57,7 @@ def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError("libvie.so is not built (%s); run `python -m paper_2608_27460_amd.build`" % LIB_PATH)
     L = C.CDLL(LIB_PATH)
-    vp, i32, i64, sz = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t
+    vp, i32, i64, sz, f32 = C.c_void_p, C.c_int32, C.c_int64, C.c_size_t, C.c_float
     st = C.c_int
     sig = {
         "vie_index_build": (st, [vp, i32, i64, i32, C.POINTER(BuildParams), C.POINTER(vp)]),
@@ -72,6 +78,15 @@ def _load() -> C.CDLL:
         "vie_dense_topk": (st, [vp, i32, i64, i32, vp, i32, i32, vp, vp, vp, sz, vp]),
         "vie_dense_topk_noalloc": (st, [vp, i32, i64, i32, vp, i32, i32, vp, vp, vp]),
         "vie_scatter": (st, [vp, vp, i32, i32, i64, vp, vp]),
+        "vie_int8_logits_workspace": (st, [i64, i32, i32, C.POINTER(sz)]),
+        "vie_int8_logits": (st, [vp, vp, i64, i32, vp, i32, i32, vp, i32, i64, vp, sz, vp]),
+        "vie_sample": (st, [vp, vp, i32, i32, vp, vp, vp, vp, vp, vp]),
+        "vie_sample_rows_workspace": (st, [i64, i32, C.POINTER(sz)]),
+        "vie_sample_rows": (st, [vp, i32, i64, i64, i32, vp, vp, vp, vp, vp, vp, sz, vp]),
+        "vie_distill_workspace": (st, [i64, i32, C.POINTER(sz)]),
+        "vie_distill": (st, [vp, i32, i32, i64, i64, vp, vp, i32, f32, vp, vp, vp, sz, vp]),
+        "vie_distill_grad": (st, [vp, i32, i32, i64, i64, vp, vp, i32, f32, vp, vp, f32, vp, i64, vp]),
+        "vie_distill_step": (st, [vp, i32, i32, i64, i64, vp, vp, i32, f32, vp, f32, vp, vp, i64, vp, sz, vp]),
         "vie_status_string": (C.c_char_p, [st]),
         "vie_last_error": (C.c_char_p, []),
         "vie_version": (i32, []),
@@ -356,3 +371,198 @@ def scatter(ids, logits, V: int):
     out = torch.empty((ids.shape[0], V), dtype=torch.float32, device=ids.device)
     scatter_into(ids, logits, V, out)
     return out
+
+
+# ---------------------------------------------------------------------------
+# around the head's logits: the int8 head, the token drawn, distillation
+# ---------------------------------------------------------------------------
+
+def _matrix(t, name: str):
+    """Pointer, dtype code, rows, row length and row stride of a device matrix of logits."""
+    if not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
+        raise ValueError("%s must be [rows, V] with contiguous rows" % name)
+    rows, V = t.shape
+    return C.c_void_p(t.data_ptr()), _dtype_of_tensor(t), rows, V, t.stride(0) if rows > 1 else V
+
+
+def _values(t, name: str, dtype, shape, device):
+    """Pointer of a contiguous device tensor of this type and shape."""
+    torch = _torch()
+    if t.dtype != getattr(torch, dtype):
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
+    if t.device != device:
+        raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
+    return _dev_ptr(t, name)
+
+
+def _workspace(nbytes: int, device):
+    """A workspace of this call (torch reuses its memory in stream order), and its pointer."""
+    if nbytes == 0:
+        return None, None
+    t = _torch().empty(nbytes, dtype=_torch().uint8, device=device)
+    return t, C.c_void_p(t.data_ptr())
+
+
+class Int8Head:
+    """Full-vocabulary logits from the int8 rows and scales of quantize_rows."""
+
+    def __init__(self, q, scale):
+        torch = _torch()
+        if q.dtype != torch.int8 or q.dim() != 2:
+            raise TypeError("q must be a 2-D int8 tensor")
+        _dev_ptr(q, "q")
+        _values(scale, "scale", "float32", (q.shape[0],), q.device)
+        self.q, self.scale = q, scale
+
+    def __call__(self, h, dtype=None, out=None):
+        """Logits [B, V] (vie_int8_logits) of h [B, d], fp32 unless dtype or out says bf16."""
+        torch = _torch()
+        if h.dim() == 1:
+            h = h.unsqueeze(0)
+        V, d = self.q.shape
+        if h.dim() != 2 or h.shape[1] != d:
+            raise ValueError("h must be [B, %d], got %s" % (d, list(h.shape)))
+        if h.device != self.q.device:
+            raise ValueError("h is on %s, not on %s" % (h.device, self.q.device))
+        B, hd = h.shape[0], _dtype_of_tensor(h)
+        if out is None:
+            out = torch.empty((B, V), dtype=dtype or torch.float32, device=h.device)
+        elif dtype is not None and out.dtype != dtype:
+            raise TypeError("out is %s, not %s" % (out.dtype, dtype))
+        op, od, rows, cols, ld = _matrix(out, "out")
+        if (rows, cols) != (B, V) or out.device != h.device:
+            raise ValueError("out must be [%d, %d] on %s" % (B, V, h.device))
+        hp = _dev_ptr(h, "h")
+        n = C.c_size_t()
+        _check(lib.vie_int8_logits_workspace(V, d, B, C.byref(n)))
+        with torch.cuda.device(h.device):
+            ws, wp = _workspace(n.value, h.device)
+            _check(lib.vie_int8_logits(C.c_void_p(self.q.data_ptr()), C.c_void_p(self.scale.data_ptr()), V, d, hp, hd,
+                                       B, op, od, ld, wp, n.value, _stream(h)))
+        return out
+
+
+def _sampling(B: int, device, temperature, top_k, top_p, min_p) -> SamplingParams:
+    """Each setting is a number, or a device tensor [B] (fp32; top_k int32)."""
+    p = SamplingParams(1.0, 0, 1.0, 0.0)
+    for name, v, dtype in (("temperature", temperature, "float32"), ("top_k", top_k, "int32"),
+                           ("top_p", top_p, "float32"), ("min_p", min_p, "float32")):
+        if hasattr(v, "data_ptr"):
+            setattr(p, name + "_dev", _values(v, name, dtype, (B,), device))
+        else:
+            setattr(p, name, v)
+    return p
+
+
+def _drawn(B: int, device):
+    torch = _torch()
+    return (torch.empty(B, dtype=torch.int32, device=device), torch.empty(B, dtype=torch.float32, device=device),
+            torch.empty(B, dtype=torch.int32, device=device))
+
+
+def sample(ids, logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """(token int32, probability fp32, kept candidates int32), each [B], drawn
+    from the lists ids int32 [B, k], logits fp32 [B, k] of a head with the
+    uniform numbers u fp32 [B] (vie_sample)."""
+    torch = _torch()
+    if ids.dim() == 1:
+        ids, logits = ids.unsqueeze(0), logits.unsqueeze(0)
+    if ids.dim() != 2:
+        raise ValueError("ids must be [B, k]")
+    (B, k), dev = ids.shape, ids.device
+    ip = _values(ids, "ids", "int32", (B, k), dev)
+    lp = _values(logits, "logits", "float32", (B, k), dev)
+    up = _values(u, "u", "float32", (B,), dev)
+    prm = _sampling(B, dev, temperature, top_k, top_p, min_p)
+    with torch.cuda.device(dev):
+        out = _drawn(B, dev)
+        _check(lib.vie_sample(ip, lp, B, k, C.byref(prm), up, *(C.c_void_p(t.data_ptr()) for t in out), _stream(ids)))
+    return out
+
+
+def sample_rows(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """sample() over full-vocabulary rows logits [B, V], fp32 or bf16, -inf where masked (vie_sample_rows)."""
+    torch = _torch()
+    if logits.dim() == 1:
+        logits = logits.unsqueeze(0)
+    lp, dt, B, V, ld = _matrix(logits, "logits")
+    dev = logits.device
+    up = _values(u, "u", "float32", (B,), dev)
+    prm = _sampling(B, dev, temperature, top_k, top_p, min_p)
+    n = C.c_size_t()
+    _check(lib.vie_sample_rows_workspace(V, B, C.byref(n)))
+    with torch.cuda.device(dev):
+        out = _drawn(B, dev)
+        ws, wp = _workspace(n.value, dev)
+        _check(lib.vie_sample_rows(lp, dt, V, ld, B, C.byref(prm), up, *(C.c_void_p(t.data_ptr()) for t in out), wp,
+                                   n.value, _stream(logits)))
+    return out
+
+
+def _distill_inputs(logits, ids, teacher):
+    m = _matrix(logits, "logits")
+    N = m[2]
+    if ids.dim() != 2:
+        raise ValueError("ids must be [N, k]")
+    k = ids.shape[1]
+    return m, _values(ids, "ids", "int32", (N, k), logits.device), _values(teacher, "teacher", "float32", (N, k), logits.device), k
+
+
+def _grad_of(logits, gloss, out):
+    """The gradient's tensor, pointer and row stride, and the pointer of the losses' gradients."""
+    torch = _torch()
+    N, V = logits.shape
+    if out is None:
+        out = torch.empty((N, V), dtype=logits.dtype, device=logits.device)
+    gp, gd, rows, cols, ld = _matrix(out, "out")
+    if (rows, cols) != (N, V) or out.dtype != logits.dtype or out.device != logits.device:
+        raise ValueError("out must be like logits")
+    return out, gp, ld, None if gloss is None else _values(gloss, "gloss", "float32", (N,), logits.device)
+
+
+def distill(logits, ids, teacher, tau: float = 1.0):
+    """(loss fp32 [N], stats fp32 [N, 2]) of the student's logits [N, V] (fp32
+    or bf16) against a teacher's lists ids int32 [N, k], teacher fp32 [N, k] of
+    logits at the temperature tau (vie_distill); stats goes to distill_grad."""
+    torch = _torch()
+    (lp, dt, N, V, ld), ip, tp, k = _distill_inputs(logits, ids, teacher)
+    n = C.c_size_t()
+    _check(lib.vie_distill_workspace(V, N, C.byref(n)))
+    with torch.cuda.device(logits.device):
+        loss = torch.empty(N, dtype=torch.float32, device=logits.device)
+        stats = torch.empty((N, 2), dtype=torch.float32, device=logits.device)
+        ws, wp = _workspace(n.value, logits.device)
+        _check(lib.vie_distill(lp, dt, N, V, ld, ip, tp, k, tau, C.c_void_p(loss.data_ptr()),
+                               C.c_void_p(stats.data_ptr()), wp, n.value, _stream(logits)))
+    return loss, stats
+
+
+def distill_grad(logits, ids, teacher, stats, tau: float = 1.0, gloss=None, weight: float = 1.0, out=None):
+    """Gradient of sum_n weight gloss[n] loss[n] (gloss fp32 [N], ones if None)
+    in the logits, in their type; out may be logits itself (vie_distill_grad)."""
+    torch = _torch()
+    (lp, dt, N, V, ld), ip, tp, k = _distill_inputs(logits, ids, teacher)
+    sp = _values(stats, "stats", "float32", (N, 2), logits.device)
+    with torch.cuda.device(logits.device):
+        out, gp, gld, glp = _grad_of(logits, gloss, out)
+        _check(lib.vie_distill_grad(lp, dt, N, V, ld, ip, tp, k, tau, sp, glp, weight, gp, gld, _stream(logits)))
+    return out
+
+
+def distill_step(logits, ids, teacher, tau: float = 1.0, gloss=None, weight: float = 1.0, out=None):
+    """(loss, gradient): distill and distill_grad at once (vie_distill_step)."""
+    torch = _torch()
+    (lp, dt, N, V, ld), ip, tp, k = _distill_inputs(logits, ids, teacher)
+    n = C.c_size_t()
+    _check(lib.vie_distill_workspace(V, N, C.byref(n)))
+    with torch.cuda.device(logits.device):
+        loss = torch.empty(N, dtype=torch.float32, device=logits.device)
+        out, gp, gld, glp = _grad_of(logits, gloss, out)
+        ws, wp = _workspace(n.value, logits.device)
+        _check(lib.vie_distill_step(lp, dt, N, V, ld, ip, tp, k, tau, glp, weight, C.c_void_p(loss.data_ptr()), gp, gld,
+                                    wp, n.value, _stream(logits)))
+    return loss, out

@@ -1,0 +1,563 @@
+"""The operators around the head's logits on the GPU, against plain 64-bit
+numpy: the int8 head (bitwise), sampling (tokens and counts equal), the
+distillation loss and its gradient (the formula's, and differences')."""
+import numpy as np
+import pytest
+
+from paper_2608_27460_amd import synth
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+INF = float("inf")
+F32, BF16 = torch.float32, torch.bfloat16
+LOWEST = {F32: torch.finfo(F32).min, BF16: torch.finfo(BF16).min}
+
+
+@pytest.fixture(scope="module")
+def vie():
+    assert torch.cuda.is_available(), "the gpu tests need an MI355X"
+    from paper_2608_27460_amd import vie as v
+    return v
+
+
+def say(*a):
+    print(*a, flush=True)
+
+
+def strided(t, ld, offset=0, fill=77.0):
+    """The matrix t on the device with row stride ld, `offset` elements into its buffer; and that buffer."""
+    R, V = t.shape
+    buf = torch.full((offset + R * ld + 8,), fill, dtype=t.dtype, device="cuda")
+    view = buf[offset:offset + R * ld].view(R, ld)[:, :V]
+    view.copy_(t)
+    return view, buf
+
+
+def between(buf, R, V, ld, offset):
+    """What lies in the buffer outside the matrix."""
+    b = buf.clone()
+    b[offset:offset + R * ld].view(R, ld)[:, :V] = 77.0
+    return b
+
+
+# ------------------------------------------------------------------ int8 head
+
+def int8_reference(q, scale, h, out):
+    """The definition, with numpy's fp32 products (rounded to nearest even)."""
+    h = h.float().numpy()
+    with np.errstate(invalid="ignore", divide="ignore"):
+        xs = (np.abs(h).max(1) / np.float32(127)).astype(np.float32)
+        bad = ~np.isfinite(h).all(1)
+        x = np.where(xs[:, None] > 0, np.rint((h / np.where(xs > 0, xs, 1)[:, None]).astype(np.float32)), 0)
+        x = np.clip(np.where(bad[:, None], 0, x), -127, 127)
+    xs = np.where(bad, np.float32(np.nan), xs)
+    z = (x.astype(np.float64) @ q.numpy().astype(np.float64).T).astype(np.float32)
+    z = (z * scale.numpy()[None]).astype(np.float32)
+    return torch.from_numpy((z * xs[:, None]).astype(np.float32)).to(out)
+
+
+def int8_inputs(V, d, B, dtype, seed):
+    g = torch.Generator().manual_seed(seed)
+    q = torch.randint(-127, 128, (V, d), generator=g, dtype=torch.int32).to(torch.int8)
+    scale = torch.rand(V, generator=g) * 1e-2
+    h = torch.randn(B, d, generator=g)
+    h[0, 0] = 9.0
+    if B > 2:
+        h[1] = 0.0
+    return q, scale, h.to(dtype)
+
+
+def same_bits(a, b):
+    a, b = a.cpu(), b.cpu()
+    assert a.dtype == b.dtype and a.shape == b.shape
+    i = torch.int32 if a.dtype == F32 else torch.int16
+    nan = torch.isnan(a) & torch.isnan(b)
+    x, y = a.contiguous().view(i), b.contiguous().view(i)
+    same = (x == y) | nan | ((a == 0) & (b == 0))
+    assert bool(same.all()), "%d of %d values differ" % (int((~same).sum()), same.numel())
+
+
+INT8_CASES = [
+    (1, 1, 1, F32, F32), (15, 7, 2, BF16, F32), (33, 16, 3, F32, BF16), (1000, 64, 1, BF16, F32),
+    (4099, 65, 5, BF16, BF16), (2049, 100, 16, F32, F32), (50257, 1000, 5, BF16, F32), (3001, 1024, 17, BF16, F32),
+    (4096, 2048, 1, F32, F32), (2000, 8192, 4, BF16, BF16), (777, 8191, 3, F32, F32), (5000, 256, 64, BF16, BF16),
+    (3333, 272, 65, BF16, F32), (1031, 512, 130, F32, BF16), (2111, 640, 300, BF16, BF16), (513, 96, 1000, BF16, F32),
+    (300, 33, 2100, F32, BF16), (140000, 48, 9, BF16, F32), (6007, 1536, 33, BF16, F32), (257, 2048, 257, BF16, BF16),
+    (129, 4096, 48, BF16, F32), (8200, 128, 8, F32, F32),
+]
+
+
+@pytest.mark.parametrize("V,d,B,ht,ot", INT8_CASES)
+def test_int8_logits_bitwise(vie, V, d, B, ht, ot):
+    say("int8", V, d, B, ht, ot)
+    q, scale, h = int8_inputs(V, d, B, ht, V + d + B)
+    head = vie.Int8Head(q.cuda(), scale.cuda())
+    ref = int8_reference(q, scale, h, ot)
+    out = head(h.cuda(), dtype=ot)
+    same_bits(out, ref)
+    # strided rows that are not 16-byte aligned; nothing between them is written
+    view, buf = strided(torch.zeros(B, V, dtype=ot), V + 3, 1)
+    head(h.cuda(), out=view)
+    same_bits(view, ref)
+    assert bool((between(buf, B, V, V + 3, 1) == 77.0).all())
+
+
+def test_int8_logits_extremes_and_unaligned_rows(vie):
+    say("int8 extremes")
+    V, d, B = 700, 8192, 3
+    q = torch.full((V, d), 127, dtype=torch.int8)
+    q[1::2] = -127
+    h = torch.ones(B, d)
+    scale = torch.ones(V)
+    same_bits(vie.Int8Head(q.cuda(), scale.cuda())(h.cuda()), int8_reference(q, scale, h, F32))  # the largest sums
+    # tokens with a NaN or an infinity, tiny and huge values, next to an ordinary one
+    q, scale, h = int8_inputs(300, 75, 6, F32, 3)
+    h[1, 5], h[2, 3], h[3], h[4] = float("nan"), -INF, h[3] * 1e-43, h[4] * 1e37
+    dq = torch.zeros(300 * 75 + 5, dtype=torch.int8).cuda()
+    view = dq[5:].view(300, 75)  # rows at odd addresses
+    view.copy_(q)
+    out = vie.Int8Head(view, scale.cuda())(h.cuda())
+    same_bits(out, int8_reference(q, scale, h, F32))
+    assert bool(torch.isnan(out[1:3]).all()) and not bool(torch.isnan(out[[0, 3, 4, 5]]).any())
+
+
+def test_int8_head_of_quantized_rows(vie):
+    """quantize_rows, Int8Head and the dense head: the int8 logits are the rows' own to the quantization's error."""
+    say("int8 of quantize_rows")
+    V, d, B = 3000, 256, 9
+    W = synth.make_w(V, d, synth.BF16, 5)
+    H, _ = synth.make_queries(W, synth.BF16, B, 6)
+    Wd, Hd = vie.host_to_torch(W, synth.BF16).cuda(), vie.host_to_torch(H, synth.BF16).cuda()
+    q, scale = vie.quantize_rows(Wd, synth.BF16)
+    z = vie.Int8Head(q, scale)(Hd)
+    same_bits(z, int8_reference(q.cpu(), scale.cpu(), Hd.cpu(), F32))
+    exact = Hd.double() @ Wd.double().t()
+    # each value is off by half a step on either side: |dz| <= sum |w| xs / 2 + |h| scale / 2 + xs scale / 4
+    xs = Hd.double().abs().amax(1) / 127
+    bound = (Wd.double().abs().sum(1)[None] * xs[:, None] + Hd.double().abs().sum(1)[:, None] * scale.double()[None]) / 2 \
+        + d * xs[:, None] * scale.double()[None] / 4
+    assert bool(((z.double() - exact).abs() <= bound * (1 + 1e-5)).all())
+
+
+# ------------------------------------------------------------------- sampling
+
+def draw_reference(l, ids, u, t, k, p, m):
+    """(token, probability, kept) of a row from the definition."""
+    at = np.flatnonzero((l > -np.inf) & (ids >= 0))
+    if not at.size:
+        return -1, 0.0, 0
+    at = at[np.lexsort((ids[at], -l[at]))]
+    x = l[at].astype(np.float64)
+    if not t > 0:
+        return int(ids[at[0]]), 1.0, 1
+    K = min(k, at.size) if k > 0 else at.size
+    with np.errstate(over="ignore", invalid="ignore"):
+        w = np.where(x == x[0], 1.0, np.nan_to_num(np.exp((x - x[0]) / np.float64(t))))[:K]
+    c = np.cumsum(w)
+    n = K
+    if p < 1:
+        n = min(n, int(np.searchsorted(c, np.float64(p) * c[-1], side="left")) + 1)
+    if m > 0:
+        n = min(n, int((w >= np.float64(m)).sum()))
+    n = max(n, 1)
+    j = min(int(np.searchsorted(c[:n], np.float64(u) * c[n - 1], side="right")), n - 1)
+    return int(ids[at[j]]), w[j] / c[n - 1], n
+
+
+def check_draws(got, l, ids, u, t, k, p, m, what):
+    tok, prob, kept = (x.cpu().numpy() for x in got)
+    B = l.shape[0]
+    full = lambda v, dt: np.broadcast_to(np.asarray(v.cpu() if hasattr(v, "cpu") else v, dt), (B,))  # noqa: E731
+    t, k, p, m = full(t, np.float32), full(k, np.int64), full(p, np.float32), full(m, np.float32)
+    for b in range(B):
+        rt, rp, rk = draw_reference(l[b], ids if ids.ndim == 1 else ids[b], u[b], t[b], k[b], p[b], m[b])
+        assert (tok[b], kept[b]) == (rt, rk), "%s row %d: token %d kept %d, expected %d and %d" % (what, b, tok[b], kept[b], rt, rk)
+        # fp32 rounding (2^-24) and the integer weights' (2^-45 of the best each, seen against the total)
+        assert abs(prob[b] - rp) <= 2.0 ** -23 * rp + 2.0 ** -44, (what, b, prob[b], rp)
+
+
+SETTINGS = [  # temperature, top_k, top_p, min_p
+    (1.0, 0, 1.0, 0.0), (0.0, 0, 1.0, 0.0), (0.7, 50, 1.0, 0.0), (1.0, 0, 0.9, 0.0), (1.0, 0, 1.0, 0.1), (0.8, 40, 0.95, 0.02),
+    (1.5, 3, 0.5, 0.0), (0.05, 20, 0.99, 0.0), (30.0, 0, 0.9, 0.0), (1.0, 1, 1.0, 0.0), (1.0, 0, 0.0, 0.0), (1.0, 0, 1.0, 1.0),
+    (1.0, 0, 0.9999, 0.0), (INF, 0, 0.5, 0.0), (1.0, 0, 1.0, 2.0), (float("nan"), 0, 1.0, 0.0), (1e-6, 0, 0.9, 0.0),
+]
+
+
+def lists(B, k, seed, pad=0, shuffled=False):
+    rng = np.random.default_rng(seed)
+    lg = -np.sort(-(rng.standard_normal((B, k)) * 2 + 8).astype(np.float32), axis=1)
+    ids = np.stack([rng.choice(20 * k + 10, k, replace=False) for _ in range(B)]).astype(np.int32)
+    if pad:
+        lg[:, k - pad:], ids[:, k - pad:] = -np.inf, -1
+    if shuffled:
+        for b in range(B):
+            o = rng.permutation(k)
+            lg[b], ids[b] = lg[b, o], ids[b, o]
+    return lg, ids, rng.random(B).astype(np.float32)
+
+
+def dev(*a):
+    return tuple(torch.from_numpy(np.ascontiguousarray(x)).cuda() for x in a)
+
+
+@pytest.mark.parametrize("B,k,pad,shuffled", [(1, 1, 0, False), (7, 50, 0, False), (5, 64, 13, True), (9, 65, 0, True),
+                                              (300, 114, 30, False), (4, 1000, 7, True), (3, 2048, 0, True), (2, 129, 129, False)])
+def test_sample_lists(vie, B, k, pad, shuffled):
+    lg, ids, u = lists(B, k, B + k, pad, shuffled)
+    for t, tk, tp, mp in SETTINGS:
+        say("lists", B, k, pad, shuffled, t, tk, tp, mp)
+        got = vie.sample(*dev(ids, lg, u), temperature=t, top_k=tk, top_p=tp, min_p=mp)
+        check_draws(got, lg, ids, u, t, tk, tp, mp, "lists")
+
+
+def test_sample_lists_odd_entries(vie):
+    """Ties, infinities, NaN, -inf before the end, negative ids, an id twice, u at its ends."""
+    say("lists, odd entries")
+    n, i = np.float32(np.nan), np.float32(np.inf)
+    lg = np.array([[3, 3, 3, 1, 1, -i], [i, i, 5, n, 2, -i], [n, n, n, n, n, n], [-i, 2, -i, 2, 0, n],
+                   [7, 6, 6, 5, 5, 4], [0, -0.0, 0, -0.0, -1, -1]], np.float32)
+    ids = np.array([[9, 2, 5, 1, 0, 3], [4, 1, 3, 2, 0, 9], [1, 2, 3, 4, 5, 6], [8, 5, 7, 5, -1, 2],
+                    [-1, 3, 3, -7, 2, 1], [6, 5, 4, 3, 2, 1]], np.int32)
+    for u0 in (0.0, 0.25, 0.5, 0.74, np.float32(1 - 2 ** -24)):
+        u = np.full(6, u0, np.float32)
+        for t, tk, tp, mp in SETTINGS:
+            got = vie.sample(*dev(ids, lg, u), temperature=t, top_k=tk, top_p=tp, min_p=mp)
+            check_draws(got, lg, ids, u, t, tk, tp, mp, "odd entries")
+    # outside [0, 1): still one of the kept
+    for u0 in (1.0, 2.0, np.inf, -1.0, np.nan):
+        tok = vie.sample(*dev(ids, lg, np.full(6, u0, np.float32)), top_k=2)[0].cpu().numpy()
+        assert tok[0] in (2, 5) and tok[1] in (1, 4) and tok[2] == -1 and tok[3] == 5
+
+
+def row_logits(B, V, dtype, seed, masked):
+    g = torch.Generator().manual_seed(seed)
+    z = 1.7 * torch.randn(B, V, generator=g)
+    for b in range(B):
+        at = torch.randint(0, V, (20,), generator=g)
+        z[b, at] += 5
+    if masked:
+        z[::2][torch.rand(z[::2].shape, generator=g) < 0.9] = -INF
+        if B > 1:
+            z[-1] = -INF
+    u = torch.rand(B, generator=g)
+    return z.to(dtype), u
+
+
+ROW_CASES = [(1, 1, F32, False), (2, 2, BF16, True), (3, 7, BF16, False), (4, 1000, F32, True), (9, 4099, BF16, True),
+             (1, 50257, F32, False), (5, 50257, BF16, True), (1, 262144, F32, False), (2, 262147, BF16, False),
+             (70, 3001, F32, True), (300, 513, BF16, True), (3, 151936, BF16, True)]
+
+
+@pytest.mark.parametrize("B,V,dtype,masked", ROW_CASES)
+def test_sample_rows(vie, B, V, dtype, masked):
+    z, u = row_logits(B, V, dtype, B + V, masked)
+    l, ids, un = z.float().numpy(), np.arange(V), u.numpy()
+    view, buf = strided(z, V + 5, 3)
+    for t, tk, tp, mp in SETTINGS if V < 100000 else SETTINGS[:9]:
+        say("rows", B, V, dtype, masked, t, tk, tp, mp)
+        got = vie.sample_rows(z.cuda(), u.cuda(), temperature=t, top_k=tk, top_p=tp, min_p=mp)
+        check_draws(got, l, ids, un, t, tk, tp, mp, "rows")
+        again = vie.sample_rows(view, u.cuda(), temperature=t, top_k=tk, top_p=tp, min_p=mp)
+        assert all(torch.equal(x, y) for x, y in zip(got, again))
+    assert bool((between(buf, B, V, V + 5, 3) == 77.0).all())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_sample_rows_settings_per_row(vie, dtype):
+    B, V = 64, 9001
+    z, u = row_logits(B, V, dtype, 4, True)
+    rng = np.random.default_rng(9)
+    s = [np.array([SETTINGS[i][c] for i in rng.integers(0, len(SETTINGS), B)], np.float32 if c != 1 else np.int32)
+         for c in range(4)]
+    t, tk, tp, mp = dev(*s)
+    say("rows, settings per row", dtype)
+    got = vie.sample_rows(z.cuda(), u.cuda(), temperature=t, top_k=tk, top_p=tp, min_p=mp)
+    check_draws(got, z.float().numpy(), np.arange(V), u.numpy(), *s, "per row")
+    lg, ids, un = lists(B, 120, 11)
+    got = vie.sample(*dev(ids, lg, un), temperature=t, top_k=tk, top_p=tp, min_p=mp)
+    check_draws(got, lg, ids, un, *s, "lists per row")
+
+
+@pytest.mark.parametrize("V", [300, 5000, 70001])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_sample_rows_ties_and_special_values(vie, V, dtype):
+    """Rows of one value, of two, of the lowest, with NaN and infinities, narrow and wide ranges."""
+    say("rows, ties", V, dtype)
+    g = torch.Generator().manual_seed(V)
+    z = torch.zeros(12, V)
+    z[1, ::3] = 1.0
+    z[2] = LOWEST[dtype]
+    z[2, 5] = 0.0
+    z[3] = LOWEST[dtype]
+    z[4] = torch.randn(V, generator=g)
+    z[4, ::2] = float("nan")
+    z[5, 7:20] = INF
+    z[6] = 20 + 1e-3 * torch.randn(V, generator=g)
+    z[7] = 1e30 * torch.randn(V, generator=g)
+    z[8] = -torch.arange(V).float()
+    z[9] = 10 + torch.randint(0, 3, (V,), generator=g) / 16
+    z[10] = 1e-30 * torch.randn(V, generator=g)
+    z[11] = torch.where(torch.rand(V, generator=g) < 0.5, 0.0, -0.0)
+    z = z.to(dtype)
+    u = torch.rand(12, generator=g)
+    for t, tk, tp, mp in SETTINGS:
+        say("  ", t, tk, tp, mp)
+        got = vie.sample_rows(z.cuda(), u.cuda(), temperature=t, top_k=tk, top_p=tp, min_p=mp)
+        check_draws(got, z.float().numpy(), np.arange(V), u.numpy(), t, tk, tp, mp, "ties")
+
+
+def test_sample_frequencies(vie):
+    """Tokens drawn with evenly spread uniform numbers: each as often as its weight says, to one draw."""
+    say("frequencies")
+    V, B = 50, 20000
+    z = torch.randn(V, generator=torch.Generator().manual_seed(1))
+    u = (torch.arange(B) + 0.5) / B
+    tok = vie.sample_rows(z.repeat(B, 1).cuda(), u.cuda())[0].cpu()
+    freq = torch.bincount(tok.long(), minlength=V).double() / B
+    assert bool(((freq - torch.softmax(z.double(), 0)).abs() <= 1.01 / B).all())
+
+
+# --------------------------------------------------------------- distillation
+
+def distill_reference(s, ids, t, tau, g):
+    """Loss [N], gradient [N, V], q and p [N, V] in 64 bits."""
+    N, V = s.shape
+    tau = np.float64(np.float32(tau))
+    x = s.astype(np.float64) / tau
+    loss, grad, Q, P = np.zeros(N), np.zeros((N, V)), np.zeros((N, V)), np.zeros((N, V))
+    with np.errstate(all="ignore"):
+        for n in range(N):
+            top = x[n].max()
+            e = np.exp(x[n] - top)
+            q = e / e.sum()
+            logq = x[n] - top - np.log(e.sum())
+            ok = (ids[n] >= 0) & (ids[n] < V) & ~(t[n] == -np.inf)
+            if not ok.any():
+                continue
+            y = t[n][ok].astype(np.float64) / tau
+            p = np.exp(y - y.max())
+            p /= p.sum()
+            logp = y - y.max() - np.log(np.exp(y - y.max()).sum())
+            at = ids[n][ok]
+            terms = np.where(p == 0, 0, p * (logp - logq[at]))
+            loss[n] = tau * tau * terms.sum()
+            pv = np.zeros(V)
+            np.add.at(pv, at, p)
+            grad[n] = g[n] * tau * (q - pv)
+            Q[n], P[n] = q, pv
+    return loss, grad, Q, P
+
+
+def check_loss(got, ref, tau, V, what):
+    # log Z: up to V / 512 + 32 fp32 additions in a row, exponents off by 2^-23 relative (times at most log V + 1
+    # on average), all times tau^2; then one rounding
+    tol = tau * tau * ((V / 512 + 32) * 2.0 ** -24 + (np.log(V) + 3) * 2.0 ** -22) + 2.0 ** -23 * np.abs(ref)
+    with np.errstate(invalid="ignore", over="ignore"):  # (a loss above fp32's range, tau^2 times 1e38, is +inf)
+        bad = ~(np.abs(got - ref) <= tol) & ~(np.isnan(got) & np.isnan(ref)) & (got != ref.astype(np.float32))
+    assert not bad.any(), (what, got[bad][:4], ref[bad][:4])
+
+
+def check_grad(got, ref, Q, P, s, tau, g, dtype, what):
+    V = s.shape[1]
+    with np.errstate(all="ignore"):
+        x = np.abs(s.astype(np.float64) - s.max(1, keepdims=True)) / tau
+        # q: its exponent is off by 2^-22 relative, its sum as above, a product or two; p: fp32; the type's rounding
+        q_tol = Q * ((np.minimum(x, 200) + 4) * 2.0 ** -22 + (V / 512 + 32) * 2.0 ** -24 + (np.log(V) + 3) * 2.0 ** -22)
+        tol = np.abs(g)[:, None] * tau * (q_tol + P * 2.0 ** -22) + torch.finfo(dtype).eps / 2 * np.abs(ref) + 1e-37
+        bad = ~(np.abs(got - ref) <= tol) & ~(np.isnan(got) & np.isnan(ref)) & (got != ref)  # (tol is NaN beside a NaN)
+    assert not bad.any(), (what, int(bad.sum()), got[bad][:4], ref[bad][:4], np.argwhere(bad)[:4])
+
+
+def distill_inputs(N, V, k, dtype, seed, kind="plain"):
+    rng = np.random.default_rng(seed)
+    s = torch.from_numpy((rng.standard_normal((N, V)) * 2).astype(np.float32)).to(dtype)
+    t = (rng.standard_normal((N, k)) * 2 + 4).astype(np.float32)
+    kk = min(k, V)
+    ids = np.full((N, k), -1, np.int32)
+    for n in range(N):
+        ids[n, :kk] = rng.choice(V, kk, replace=False)
+    t[:, kk:] = -np.inf
+    if kind == "odd":
+        ids[0] = -1                                   # nothing listed
+        if N > 1:
+            t[1] = -np.inf                            # nothing listed either
+        if N > 2 and kk > 2:
+            ids[2, 1], ids[2, 2] = V + 5, ids[2, 0]   # out of range, an id twice
+        if N > 3:
+            s[3, 1:] = LOWEST[dtype]                  # masks of the lowest value
+            t[3, 0] = -np.inf
+        if N > 4:
+            s[4, rng.random(V) < 0.5] = -INF          # masks of -inf, listed ids among them
+        if N > 5:
+            s[5, V // 2] = float("nan")
+        if N > 6:
+            s[6] = -INF
+        if N > 7:
+            t[7, 0] = np.nan
+        if N > 8:
+            ids[8] = ids[8, 0]                        # one id, k times
+        if N > 9:
+            s[9, 0] = INF
+        if N > 10:
+            ids[10] = -1
+            s[10] = float("nan")                      # nothing listed over NaN: 0
+    return s, ids, t
+
+
+DISTILL_CASES = [(1, 1, 1, F32, 1.0, "plain"), (2, 2, 3, BF16, 2.0, "plain"), (3, 7, 7, F32, 0.5, "plain"),
+                 (13, 1000, 50, BF16, 1.0, "odd"), (13, 1000, 50, F32, 3.0, "odd"), (12, 4099, 2048, F32, 1.0, "odd"),
+                 (5, 50257, 64, BF16, 2.0, "plain"), (1, 262144, 50, F32, 1.0, "plain"), (2, 151936, 1000, BF16, 4.0, "odd"),
+                 (700, 300, 20, BF16, 1.0, "odd"), (1200, 129, 5, F32, 1.0, "odd"), (40, 9001, 600, F32, 0.05, "odd"),
+                 (300, 20000, 64, BF16, 2.0, "odd")]
+
+
+@pytest.mark.parametrize("N,V,k,dtype,tau,kind", DISTILL_CASES)
+def test_distill(vie, N, V, k, dtype, tau, kind):
+    say("distill", N, V, k, dtype, tau, kind)
+    s, ids, t = distill_inputs(N, V, k, dtype, N + V + k, kind)
+    rng = np.random.default_rng(1)
+    gl = rng.standard_normal(N).astype(np.float32)
+    w = 0.25
+    g = gl.astype(np.float64) * w
+    sn = s.float().numpy()
+    ref, grad, Q, P = distill_reference(sn, ids, t, tau, g)
+    sd, (idd, td, gd) = s.cuda(), dev(ids, t, gl)
+    loss, stats = vie.distill(sd, idd, td, tau)
+    check_loss(loss.cpu().numpy(), ref, tau, V, "loss")
+    got = vie.distill_grad(sd, idd, td, stats, tau, gloss=gd, weight=w)
+    assert got.dtype == dtype
+    check_grad(got.float().cpu().numpy(), grad, Q, P, sn, tau, g, dtype, "grad")
+    # both at once, strided, at an odd address: the same bits
+    view, buf = strided(s, V + 3, 1)
+    out, obuf = strided(torch.zeros(N, V, dtype=dtype), V + 7, 3)
+    loss2, got2 = vie.distill_step(view, idd, td, tau, gloss=gd, weight=w, out=out)
+    check_loss(loss2.cpu().numpy(), ref, tau, V, "step loss")
+    check_grad(got2.float().cpu().numpy(), grad, Q, P, sn, tau, g, dtype, "step grad")
+    assert bool((between(buf, N, V, V + 3, 1) == 77.0).all()) and bool((between(obuf, N, V, V + 7, 3) == 77.0).all())
+    # in place
+    loss3, got3 = vie.distill_step(view, idd, td, tau, gloss=gd, weight=w, out=view)
+    assert got3.data_ptr() == view.data_ptr()
+    check_loss(loss3.cpu().numpy(), ref, tau, V, "in place loss")
+    check_grad(view.float().cpu().numpy(), grad, Q, P, sn, tau, g, dtype, "in place grad")
+    same = vie.distill_grad(sd, idd, td, stats, tau, gloss=gd, weight=w, out=sd)
+    same_bits(same, got)
+
+
+def test_distill_gradient_by_differences(vie):
+    """Central differences of the 64-bit loss, error h^2 / 6 times a third derivative of at most 1."""
+    say("distill differences")
+    N, V, k, tau = 3, 40, 6, 2.0
+    s, ids, t = distill_inputs(N, V, k, F32, 7)
+    one = np.ones(N)
+    sn = s.numpy().astype(np.float64)
+    h = 1e-3
+    diff = np.zeros((N, V))
+    for v in range(V):
+        up, dn = sn.copy(), sn.copy()
+        up[:, v] += h
+        dn[:, v] -= h
+        diff[:, v] = (distill_reference(up, ids, t, tau, one)[0] - distill_reference(dn, ids, t, tau, one)[0]) / (2 * h)
+    loss, grad = vie.distill_step(s.cuda(), *dev(ids, t), tau)
+    assert np.abs(grad.cpu().numpy() - diff).max() <= tau * tau * h * h + 1e-5
+    check_loss(loss.cpu().numpy(), distill_reference(sn, ids, t, tau, one)[0], tau, V, "loss")
+
+
+# ------------------------------------------------------------------- together
+
+def test_heads_sampling_and_distillation_together(vie):
+    """A decoding step and a training step: lists of the dense head and rows
+    of the int8 head give tokens, and the dense head's lists teach the int8
+    logits, whose gradient replaces them."""
+    say("together")
+    V, d, B, k = 5003, 128, 12, 40
+    W = synth.make_w(V, d, synth.BF16, 15)
+    H, _ = synth.make_queries(W, synth.BF16, B, 16)
+    Wd, Hd = vie.host_to_torch(W, synth.BF16).cuda(), vie.host_to_torch(H, synth.BF16).cuda()
+    u = torch.rand(B, generator=torch.Generator().manual_seed(2)).cuda()
+    ids, lg = vie.DenseHead(Wd, max_batch=B, max_k=k)(Hd, k)
+    how = dict(temperature=0.3, top_k=30, top_p=0.9, min_p=0.01)
+    got = vie.sample(ids, lg, u, **how)
+    # the scattered rows hold the same candidates
+    rows = vie.sample_rows(vie.scatter(ids, lg, V), u, **how)
+    assert torch.equal(got[0], rows[0]) and torch.equal(got[2], rows[2])
+    assert float((got[1] - rows[1]).abs().max()) <= 2.0 ** -23
+    check_draws(got, lg.cpu().numpy(), ids.cpu().numpy(), u.cpu().numpy(), 0.3, 30, 0.9, 0.01, "together")
+    q, scale = vie.quantize_rows(Wd, synth.BF16)
+    z = vie.Int8Head(q, scale)(Hd)
+    tok = vie.sample_rows(z, u, **how)
+    check_draws(tok, z.cpu().numpy(), np.arange(V), u.cpu().numpy(), 0.3, 30, 0.9, 0.01, "int8 rows")
+    zn = z.cpu().numpy()
+    ref, grad, Q, P = distill_reference(zn, ids.cpu().numpy(), lg.cpu().numpy(), 1.5, np.full(B, 1 / B))
+    loss, g = vie.distill_step(z, ids, lg, 1.5, weight=1 / B, out=z)
+    check_loss(loss.cpu().numpy(), ref, 1.5, V, "together")
+    check_grad(z.cpu().numpy(), grad, Q, P, zn, 1.5, np.full(B, 1 / B), F32, "together")
+
+
+@pytest.mark.parametrize("B,V", [(2, 30011), (40, 3001)])
+def test_graph_replays_and_side_streams(vie, B, V):
+    """Two captured graphs of the chain, replayed in turn with new inputs and
+    eager calls between, and a stream of its own."""
+    d, k = 96, 20
+    say("graphs", B, V)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q = torch.randint(-127, 128, (V, d), generator=g, device="cuda", dtype=torch.int32).to(torch.int8)
+    head = vie.Int8Head(q, torch.rand(V, device="cuda", generator=g) * 1e-3)
+    ids = torch.argsort(torch.rand(B, V, device="cuda", generator=g), dim=1)[:, :k].to(torch.int32).contiguous()
+
+    def new():
+        return (torch.randn(B, d, device="cuda", generator=g), torch.rand(B, device="cuda", generator=g),
+                torch.randn(B, k, device="cuda", generator=g))
+
+    def chain(h, u, t):
+        z = head(h)
+        tok = vie.sample_rows(z, u, temperature=0.9, top_k=0, top_p=0.9)
+        lst = vie.sample(ids, t, u, top_p=0.8)
+        loss, stats = vie.distill(z, ids, t, 2.0)
+        back = vie.distill_grad(z, ids, t, stats, 2.0)
+        loss2, grad = vie.distill_step(z, ids, t, 2.0, out=z)
+        return (*tok, *lst, loss, back, loss2, grad)
+
+    graphs = []
+    for _ in range(2):
+        held = new()
+        chain(*held)
+        torch.cuda.synchronize()
+        gr = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(gr):
+            out = chain(*held)
+        graphs.append((gr, held, out))
+    for rep in range(3):
+        for gr, held, out in graphs:
+            for x, y in zip(held, new()):
+                x.copy_(y)
+            want = [x.clone() for x in chain(*held)]
+            gr.replay()
+            torch.cuda.synchronize()
+            for x, y in zip(out, want):
+                assert torch.equal(x, y), rep
+    args = new()
+    want = chain(*args)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        got = chain(*args)
+    side.synchronize()
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+
+
+def test_results_do_not_change_between_runs(vie):
+    say("run to run")
+    z, u = row_logits(6, 40009, BF16, 8, True)
+    zd, ud = z.cuda(), u.cuda()
+    s, ids, t = distill_inputs(20, 30000, 70, BF16, 5)
+    sd, (idd, td) = s.cuda(), dev(ids, t)
+    first = None
+    for _ in range(4):
+        got = [*vie.sample_rows(zd, ud, top_p=0.97), *vie.distill_step(sd, idd, td, 2.0)]
+        torch.cuda.synchronize()
+        if first is None:
+            first = got
+        assert all(torch.equal(x, y) for x, y in zip(got, first))

@@ -1,0 +1,114 @@
+"""Refusals of the operators around the head's logits (int8 head, sampling,
+distillation): reported before anything is enqueued, so they need no GPU."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2608_27460_amd import vie
+
+L = vie.lib
+P = C.c_void_p(4096)      # never dereferenced: every call below fails its checks first
+ODD = C.c_void_p(4097)
+PRM = vie.SamplingParams(1.0, 0, 1.0, 0.0)
+BIG = 1 << 40
+
+
+def _int8(q=P, scale=P, V=100, d=64, h=P, ht=vie.BF16, B=2, out=P, ot=vie.F32, ld=100, ws=P, n=BIG):
+    return L.vie_int8_logits(q, scale, V, d, h, ht, B, out, ot, ld, ws, n, None)
+
+
+@pytest.mark.parametrize("change", [
+    {"q": None}, {"scale": None}, {"h": None}, {"out": None}, {"V": 0}, {"V": 1 << 31, "ld": 1 << 31}, {"d": 0}, {"d": 8193},
+    {"B": 0}, {"B": 65536}, {"ht": 2}, {"ot": -1}, {"ld": 99}, {"ws": None}, {"ws": C.c_void_p(4096 + 128)}, {"n": 10},
+    {"h": ODD}, {"out": ODD}, {"scale": ODD},
+])
+def test_int8_logits_refuses(change):
+    assert _int8(**change) == vie.EINVAL
+    assert vie.lib.vie_last_error()
+
+
+def _sample(ids=P, lg=P, B=2, k=5, prm=C.byref(PRM), u=P, tok=P):
+    return L.vie_sample(ids, lg, B, k, prm, u, tok, None, None, None)
+
+
+@pytest.mark.parametrize("change", [{"ids": None}, {"lg": None}, {"B": 0}, {"B": 65536}, {"k": 0}, {"k": 2049},
+                                    {"prm": None}, {"u": None}, {"tok": None}])
+def test_sample_refuses(change):
+    assert _sample(**change) == vie.EINVAL
+
+
+def _rows(lg=P, dt=vie.BF16, V=100, ld=100, B=2, prm=C.byref(PRM), u=P, tok=P, ws=P, n=BIG):
+    return L.vie_sample_rows(lg, dt, V, ld, B, prm, u, tok, None, None, ws, n, None)
+
+
+@pytest.mark.parametrize("change", [{"lg": None}, {"lg": ODD}, {"dt": 7}, {"V": 0}, {"ld": 99}, {"B": 0}, {"prm": None},
+                                    {"u": None}, {"tok": None}])
+def test_sample_rows_refuses(change):
+    assert _rows(**change) == vie.EINVAL
+
+
+def _loss(lg=P, dt=vie.BF16, N=2, V=100, ld=100, ids=P, t=P, k=5, tau=1.0, loss=P, stats=P, ws=P, n=BIG):
+    return L.vie_distill(lg, dt, N, V, ld, ids, t, k, tau, loss, stats, ws, n, None)
+
+
+def _grad(lg=P, dt=vie.BF16, N=2, V=100, ld=100, ids=P, t=P, k=5, tau=1.0, stats=P, grad=C.c_void_p(1 << 20), gld=100):
+    return L.vie_distill_grad(lg, dt, N, V, ld, ids, t, k, tau, stats, None, 1.0, grad, gld, None)
+
+
+def _step(lg=P, dt=vie.BF16, N=2, V=100, ld=100, ids=P, t=P, k=5, tau=1.0, loss=P, grad=C.c_void_p(1 << 20), gld=100,
+          ws=P, n=BIG):
+    return L.vie_distill_step(lg, dt, N, V, ld, ids, t, k, tau, None, 1.0, loss, grad, gld, ws, n, None)
+
+
+@pytest.mark.parametrize("call", [_loss, _grad, _step])
+@pytest.mark.parametrize("change", [{"lg": None}, {"lg": ODD}, {"dt": 3}, {"N": 0}, {"N": 65536}, {"V": 0}, {"ld": 99},
+                                    {"ids": None}, {"t": None}, {"k": 0}, {"k": 2049}, {"tau": 0.0}, {"tau": -1.0},
+                                    {"tau": float("nan")}, {"tau": 2e4}])
+def test_distill_refuses(call, change):
+    assert call(**change) == vie.EINVAL
+
+
+def test_distill_refuses_results_and_overlaps():
+    assert _loss(loss=None) == vie.EINVAL
+    assert _loss(stats=None) == vie.EINVAL
+    assert _step(loss=None) == vie.EINVAL
+    for call in (_grad, _step):
+        assert call(grad=None) == vie.EINVAL
+        assert call(gld=99) == vie.EINVAL
+        assert call(grad=C.c_void_p(4096 + 200)) == vie.EINVAL  # one row further: overlaps
+        assert call(grad=C.c_void_p(4096 - 2)) == vie.EINVAL
+        assert call(grad=P, gld=101) == vie.EINVAL  # in place, another stride
+        assert b"in place" in L.vie_last_error()
+    assert _grad(stats=None) == vie.EINVAL
+
+
+def test_workspace_queries():
+    n = C.c_size_t()
+    assert L.vie_int8_logits_workspace(1000, 64, 3, C.byref(n)) == vie.OK and n.value >= 3 * 64
+    assert L.vie_sample_rows_workspace(1000, 3, C.byref(n)) == vie.OK
+    assert L.vie_distill_workspace(1000, 3, C.byref(n)) == vie.OK
+    for f, args in ((L.vie_int8_logits_workspace, (0, 64, 3)), (L.vie_int8_logits_workspace, (10, 0, 3)),
+                    (L.vie_int8_logits_workspace, (10, 4, 0)), (L.vie_sample_rows_workspace, (0, 3)),
+                    (L.vie_sample_rows_workspace, (10, 0)), (L.vie_distill_workspace, (10, 65536))):
+        assert f(*args, C.byref(n)) == vie.EINVAL
+        assert f(*args, None) == vie.EINVAL
+
+
+def test_binding_refuses_host_tensors_types_and_shapes():
+    f, i = torch.zeros(2, 5), torch.zeros(2, 5, dtype=torch.int32)
+    u = torch.zeros(2)
+    with pytest.raises(ValueError, match="device tensor"):
+        vie.Int8Head(torch.zeros(4, 8, dtype=torch.int8), torch.zeros(4))
+    with pytest.raises(TypeError, match="int8"):
+        vie.Int8Head(f, u)
+    with pytest.raises(ValueError, match="device tensor"):
+        vie.sample(i, f, u)
+    with pytest.raises(TypeError, match="int32"):
+        vie.sample(i.long(), f, u)
+    with pytest.raises(ValueError, match="device tensor"):
+        vie.sample_rows(f, u)
+    for call in (lambda: vie.distill(f, i, f), lambda: vie.distill_step(f, i, f),
+                 lambda: vie.distill_grad(f, i, f, torch.zeros(2, 2))):
+        with pytest.raises(ValueError, match="device tensor"):
+            call()
