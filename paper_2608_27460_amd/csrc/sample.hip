@@ -18,6 +18,8 @@
 // the result is the same from run to run however the additions fall.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "block.hpp"
 #include "keys.hpp"
 #include "operators.hpp"
@@ -181,11 +183,59 @@ template <int NT> __global__ __launch_bounds__(NT) void sample_list_kernel(Sampl
 // ---------------------------------------------------------------------------
 // full rows
 // ---------------------------------------------------------------------------
+//
+// A row of V logits would have to be sorted for its limits and its token to
+// be read off; but all of them are borders in one order, and only the
+// candidates around a border matter one by one.  So the candidates are
+// counted and weighed in bins that keep the order, by their distance from the
+// best logit, and only those of a bin that a border may fall into are put in
+// order themselves:
+//
+//   rows_best_kernel   the best key of each part of a row,
+//   rows_bins_kernel   how many candidates and how much weight each bin holds
+//                      (in LDS, then added up in memory), and how many
+//                      candidates pass min-p,
+//   rows_draw_kernel   sums over the bins; the bins that each border can fall
+//                      into, given those before it (top-k, then top-p, then
+//                      the token); their candidates, collected.  The last
+//                      workgroup of a row to finish orders them, and their
+//                      sums, from those of the bins before, give the exact
+//                      borders.
+//
+// A bin is the leading bits of the fp32 distance: 256 to the octave from
+// 2^-8 to 2^8, so the bins are finest where the candidates are few and weigh
+// most, whatever the spread of the logits and the temperature.  A border in
+// the bulk of 262144 normal logits meets some 1600 candidates of its bin.
+// Rows whose border bins hold more than kCollect (constant rows, or spreads
+// far from a model's) take the borders one after the other from histograms
+// of the keys' digits: exact too, in up to 24 passes of one workgroup.
 
 constexpr int kRowThreads = 1024;
 constexpr int kRowWaves = kRowThreads / kLanes;
 constexpr int kDigit = 11;                 // key bits settled by a pass
-constexpr int kBins = 1 << kDigit;
+constexpr int kDigits = 1 << kDigit;
+constexpr int kBins = 4096;
+constexpr int kBinsPer = kBins / kRowThreads;
+constexpr int kCollect = 2048;             // candidates put in order one by one
+constexpr int kMaxParts = 32;
+constexpr int kMaxRows = 1024;             // rows of one round of launches (66 KB of workspace each)
+
+// The bin of a logit: monotone, bin 0 the best.
+__device__ __forceinline__ int bin_of(float best, float l)
+{
+    constexpr int kFirst = 119 << 8;  // 2^-8: exponent 119, eight mantissa bits
+    const int x = (int)(__float_as_uint(l == best ? 0.0f : best - l) >> 15) - kFirst + 1;
+    return x < 0 ? 0 : x > kBins - 1 ? kBins - 1 : x;
+}
+
+// A row's part of the workspace.
+struct RowSpace {
+    uint64_t best[kMaxParts];
+    uint64_t sum[kBins];
+    uint64_t key[kCollect];
+    uint32_t count[kBins];
+    uint32_t pass, collected, done, unused;
+};
 
 // A candidate's place in the order: how many and how much weight come up to
 // it (itself included), and its key.
@@ -194,12 +244,12 @@ struct Place {
     int64_t rank;
 };
 
-struct RowLds {
-    uint64_t sum[kBins];
-    uint32_t count[kBins];
+struct DigitLds {
+    uint64_t sum[kDigits];
+    uint32_t count[kDigits];
     uint64_t wave_sum[kRowWaves];
     uint32_t wave_count[kRowWaves];
-    uint64_t key[kRowWaves];
+    int wave_bin[kRowWaves];
     Place at;
     int bin;
 };
@@ -211,32 +261,45 @@ template <bool BF16> struct Row {
     float best;
     double inv_t, one;
 
-    // f(logit, id) for every candidate, by the whole workgroup
-    template <typename F> __device__ __forceinline__ void each(F f) const
+    // f(logit, id) for every candidate from i0 on, n of them, by the whole workgroup
+    template <typename F> __device__ __forceinline__ void each(int64_t i0, int64_t n, F f) const
     {
-        const Span<typename E::T> sp(l, n);
-        const word4 *v = reinterpret_cast<const word4 *>(l + sp.head);
+        const typename E::T *p = l + i0;
+        const Span<typename E::T> sp(p, n);
+        const word4 *v = reinterpret_cast<const word4 *>(p + sp.head);
         for (int64_t i = threadIdx.x; i < sp.vecs; i += kRowThreads) {
             float x[E::kVec];
             E::unpack(v[i], x);
 #pragma unroll
             for (int e = 0; e < E::kVec; ++e)
-                if (candidate(x[e])) f(x[e], (int32_t)(sp.head + i * E::kVec + e));
+                if (candidate(x[e])) f(x[e], (int32_t)(i0 + sp.head + i * E::kVec + e));
         }
         for (int64_t i = threadIdx.x; i < sp.head + n - sp.tail0; i += kRowThreads) {
             const int64_t at = i < sp.head ? i : sp.tail0 + i - sp.head;
-            const float x = E::get(l[at]);
-            if (candidate(x)) f(x, (int32_t)at);
+            const float x = E::get(p[at]);
+            if (candidate(x)) f(x, (int32_t)(i0 + at));
         }
     }
+    __device__ __forceinline__ uint64_t units(float l) const { return fixed(weight(l, best, inv_t), one); }
 };
+
+// Inclusive sums over the workgroup's threads of a count and a sum.
+__device__ __forceinline__ void block_scan(uint32_t &c, uint64_t &s, uint32_t *wave_count, uint64_t *wave_sum)
+{
+    const int wave = threadIdx.x / kLanes;
+    c = wave_scan(c);
+    s = wave_scan(s);
+    if ((threadIdx.x & (kLanes - 1)) == kLanes - 1) wave_count[wave] = c, wave_sum[wave] = s;
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) c += wave_count[w], s += wave_sum[w];
+}
 
 // The first candidate in the order whose rank is at least `rank` (BY_RANK),
 // or else whose sum is at least `sum`: digits of the keys from the top, each
 // by a histogram of the candidates that share the digits before.  If there is
 // none (`sum` above the total), the last candidate.
 template <bool BF16, bool BY_RANK>
-__device__ Place find(const Row<BF16> &row, int64_t rank, uint64_t sum, RowLds &s)
+__device__ Place find(const Row<BF16> &row, int64_t rank, uint64_t sum, DigitLds &s)
 {
     const int tid = threadIdx.x;
     uint64_t prefix = 0, before_sum = 0;
@@ -245,28 +308,26 @@ __device__ Place find(const Row<BF16> &row, int64_t rank, uint64_t sum, RowLds &
         const int bits = shift < kDigit ? shift : kDigit;
         shift -= bits;
         __syncthreads();
-        for (int i = tid; i < kBins; i += kRowThreads) s.sum[i] = 0, s.count[i] = 0;
+        for (int i = tid; i < kDigits; i += kRowThreads) s.sum[i] = 0, s.count[i] = 0;
         __syncthreads();
-        row.each([&](float l, int32_t id) {
+        row.each(0, row.n, [&](float l, int32_t id) {
             const uint64_t key = make_key(l, id);
             if (shift + bits < 64 && (key >> (shift + bits)) != prefix) return;
             const int bin = (int)((key >> shift) & ((1u << bits) - 1));
             atomicAdd(&s.count[bin], 1u);
-            atomicAdd((unsigned long long *)&s.sum[bin], (unsigned long long)fixed(weight(l, row.best, row.inv_t), row.one));
+            atomicAdd((unsigned long long *)&s.sum[bin], (unsigned long long)row.units(l));
         });
         __syncthreads();
         // bins from the top, two a thread
-        const int top = kBins - 1 - 2 * tid;
+        const int top = kDigits - 1 - 2 * tid;
         const uint64_t s0 = s.sum[top], s1 = s.sum[top - 1];
         const uint32_t c0 = s.count[top], c1 = s.count[top - 1];
-        uint64_t cs = wave_scan(s0 + s1);
-        uint32_t cc = wave_scan(c0 + c1);
-        if ((tid & (kLanes - 1)) == kLanes - 1) s.wave_sum[tid / kLanes] = cs, s.wave_count[tid / kLanes] = cc;
+        uint64_t cs = s0 + s1;
+        uint32_t cc = c0 + c1;
         if (tid == 0) s.bin = -1;
-        __syncthreads();
+        block_scan(cc, cs, s.wave_count, s.wave_sum);
         cs += before_sum;
-        int64_t rc = before + cc;
-        for (int w = 0; w < tid / kLanes; ++w) cs += s.wave_sum[w], rc += s.wave_count[w];
+        const int64_t rc = before + cc;
         // (the places after bins `top` and `top - 1`)
         const uint64_t e1 = cs, e0 = cs - s1, b0 = e0 - s0;
         const int64_t r1 = rc, r0 = rc - c1, q0 = r0 - c0;
@@ -276,11 +337,8 @@ __device__ Place find(const Row<BF16> &row, int64_t rank, uint64_t sum, RowLds &
         if (c1 && hit(r1, e1) && !(r0 > before && hit(r0, e0))) take(top - 1, e0, r0);
         __syncthreads();
         if (s.bin < 0) {  // beyond the last candidate: its bin
-            int last = -1;
-            if (c0) last = top;
-            if (c1) last = top - 1;
-            int low = last < 0 ? kBins : last;
-            low = block_reduce<kRowThreads>(low, reinterpret_cast<int *>(s.key), [](int x, int y) { return x < y ? x : y; });
+            int low = c1 ? top - 1 : c0 ? top : kDigits;
+            low = block_reduce<kRowThreads>(low, s.wave_bin, [](int x, int y) { return x < y ? x : y; });
             if (low == top) take(top, b0, q0);
             if (low == top - 1) take(top - 1, e0, r0);
             __syncthreads();
@@ -289,53 +347,353 @@ __device__ Place find(const Row<BF16> &row, int64_t rank, uint64_t sum, RowLds &
         before_sum = s.at.sum;
         before = s.at.rank;
     }
-    const uint64_t w = fixed(weight(key_logit(prefix), row.best, row.inv_t), row.one);
-    return {prefix, before_sum + w, before + 1};
+    return {prefix, before_sum + row.units(key_logit(prefix)), before + 1};
 }
 
-// One workgroup per row.
-template <bool BF16> __global__ __launch_bounds__(kRowThreads) void sample_row_kernel(SampleLaunch a)
+// The drawn candidate as a result; `end` units of weight are kept.
+template <bool BF16> __device__ __forceinline__ Result drawn(const Row<BF16> &row, uint64_t key, uint64_t end, int64_t kept)
 {
-    typedef typename Elem<BF16>::T T;
-    __shared__ RowLds s;
-    const int b = blockIdx.x, tid = threadIdx.x;
-    const Settings st = settings(a.prm, b);
-    Row<BF16> row{static_cast<const T *>(a.logits) + (int64_t)b * a.ld, a.n, 0.0f, 0.0, 0.0};
-    uint64_t top = 0;
-    row.each([&](float l, int32_t id) { top = max(top, make_key(l, id)); });
-    top = block_reduce<kRowThreads>(top, s.key, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
-    if (top == 0 || !(st.t > 0.0f)) {
-        if (tid == 0) put(a, b, top == 0 ? Result{-1, 0.0f, 0} : Result{key_id(top), 1.0f, 1});
-        return;
-    }
-    row.best = key_logit(top);
-    row.inv_t = 1.0 / (double)st.t;
-    row.one = ldexp(1.0, fixed_shift(a.n));
-    // how many candidates there are, how many pass min-p, and the total
-    uint64_t total = 0;
-    uint32_t live = 0, pass = 0;
-    row.each([&](float l, int32_t) {
-        const double w = weight(l, row.best, row.inv_t);
-        total += fixed(w, row.one);
-        ++live;
-        pass += w >= (double)st.m;
-    });
-    auto plus = [](auto x, auto y) { return x + y; };
-    total = block_reduce<kRowThreads>(total, s.wave_sum, plus);
-    live = block_reduce<kRowThreads>(live, s.wave_count, plus);
-    __syncthreads();
-    pass = block_reduce<kRowThreads>(pass, s.wave_count, plus);
+    return {key_id(key), (float)(weight(key_logit(key), row.best, row.inv_t) * row.one / (double)end), (int32_t)kept};
+}
+
+// The borders one after the other, over the whole row: `live` candidates,
+// `total` units of weight, `pass` candidates within min-p.
+template <bool BF16>
+__device__ Result draw_by_digits(const Row<BF16> &row, Settings st, float u, uint32_t live, uint64_t total, uint32_t pass,
+                                 DigitLds &s)
+{
     Place end{0, total, (int64_t)live};  // the last candidate kept
     if (st.k > 0 && st.k < live) end = find<BF16, true>(row, st.k, 0, s);
     if (st.p < 1.0f) end = find<BF16, false>(row, 0, reach(st.p, end.sum), s);
     if (st.m > 0.0f && (int64_t)pass < end.rank) end = find<BF16, true>(row, max(pass, 1u), 0, s);
     // (never beyond the kept ones, also for u of 1 and above)
-    const uint64_t past = below(a.u[b], end.sum) + 1;
+    const uint64_t past = below(u, end.sum) + 1;
     const Place at = find<BF16, false>(row, 0, past < end.sum ? past : end.sum, s);
-    if (tid == 0) {
-        const double w = weight(key_logit(at.key), row.best, row.inv_t);
-        put(a, b, {key_id(at.key), (float)(w * row.one / (double)end.sum), (int32_t)end.rank});
+    return drawn(row, at.key, end.sum, end.rank);
+}
+
+// Workgroup (c, i) takes part c of row b0 + i in each of the three kernels.
+struct Parts {
+    int64_t len;  // candidates of a part
+    int b0;
+    RowSpace *ws;
+};
+template <bool BF16> __device__ __forceinline__ Row<BF16> row_of(const SampleLaunch &a, int b)
+{
+    return {static_cast<const typename Elem<BF16>::T *>(a.logits) + (int64_t)b * a.ld, a.n, 0.0f, 0.0, 0.0};
+}
+
+template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_best_kernel(SampleLaunch a, Parts parts)
+{
+    __shared__ uint64_t tmp[kRowWaves];
+    const int b = parts.b0 + blockIdx.y, c = blockIdx.x, S = gridDim.x;
+    RowSpace &ws = parts.ws[blockIdx.y];
+    for (int i = c * kRowThreads + threadIdx.x; i < kBins; i += S * kRowThreads) ws.sum[i] = 0, ws.count[i] = 0;
+    if (c == 0 && threadIdx.x == 0) ws.pass = ws.collected = ws.done = 0;
+    const Row<BF16> row = row_of<BF16>(a, b);
+    uint64_t best = 0;
+    const int64_t i0 = c * parts.len;
+    row.each(i0, min(parts.len, a.n - i0), [&](float l, int32_t id) {
+        const uint64_t key = make_key(l, id);
+        best = key > best ? key : best;
+    });
+    best = block_reduce<kRowThreads>(best, tmp, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
+    if (threadIdx.x == 0) ws.best[c] = best;
+}
+
+__device__ __forceinline__ uint64_t best_key(const RowSpace &ws, int S)
+{
+    uint64_t k = 0;
+    for (int i = 0; i < S; ++i) k = ws.best[i] > k ? ws.best[i] : k;
+    return k;
+}
+
+// The row's best logit and scale; false if nothing is left to draw (no
+// candidate, or the best one).
+template <bool BF16> __device__ __forceinline__ bool begin(Row<BF16> &row, uint64_t best, Settings st, int64_t n)
+{
+    if (best == 0 || !(st.t > 0.0f)) return false;
+    row.best = key_logit(best);
+    row.inv_t = 1.0 / (double)st.t;
+    row.one = ldexp(1.0, fixed_shift(n));
+    return true;
+}
+
+template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_bins_kernel(SampleLaunch a, Parts parts)
+{
+    __shared__ uint64_t s_sum[kBins];
+    __shared__ uint32_t s_count[kBins];
+    __shared__ uint32_t s_pass;
+    const int b = parts.b0 + blockIdx.y, tid = threadIdx.x;
+    RowSpace &ws = parts.ws[blockIdx.y];
+    const Settings st = settings(a.prm, b);
+    Row<BF16> row = row_of<BF16>(a, b);
+    if (!begin(row, best_key(ws, gridDim.x), st, a.n)) return;
+    for (int i = tid; i < kBins; i += kRowThreads) s_sum[i] = 0, s_count[i] = 0;
+    if (tid == 0) s_pass = 0;
+    __syncthreads();
+    uint32_t pass = 0;
+    const int64_t i0 = blockIdx.x * parts.len;
+    row.each(i0, min(parts.len, a.n - i0), [&](float l, int32_t) {
+        const int bin = bin_of(row.best, l);
+        const double w = weight(l, row.best, row.inv_t);
+        pass += w >= (double)st.m;
+        atomicAdd(&s_count[bin], 1u);
+        atomicAdd((unsigned long long *)&s_sum[bin], (unsigned long long)fixed(w, row.one));
+    });
+    pass = wave_sum(pass);
+    if ((tid & (kLanes - 1)) == 0) atomicAdd(&s_pass, pass);
+    __syncthreads();
+    for (int i = tid; i < kBins; i += kRowThreads)
+        if (s_count[i]) {
+            atomicAdd(&ws.count[i], s_count[i]);
+            atomicAdd((unsigned long long *)&ws.sum[i], (unsigned long long)s_sum[i]);
+        }
+    if (tid == 0) atomicAdd(&ws.pass, s_pass);
+}
+
+// The bin that a border falls into, with what lies before it and up to its end.
+struct Bin {
+    int bin;
+    uint32_t count0, count1;
+    uint64_t sum0, sum1;
+};
+
+struct DrawLds {
+    union {
+        struct {
+            uint64_t key[kCollect], sum[kCollect];  // the collected candidates in order, their sums
+            uint64_t base[kBins];                   // weight before a bin
+            uint32_t first[kBins];                  // collected candidates before a bin
+            uint32_t rank[kBins];                   // candidates before a bin
+            uint32_t flag[kBins / 32];              // the bins collected
+        } d;
+        DigitLds digits;
+    };
+    uint64_t wave_sum[kRowWaves];
+    uint32_t wave_count[kRowWaves];
+    Bin at[2];
+    uint64_t found_sum, found_key;
+    int64_t found_rank;
+    uint32_t base, last;
+};
+
+template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_kernel(SampleLaunch a, Parts parts)
+{
+    extern __shared__ __align__(16) char smem[];
+    DrawLds &s = *reinterpret_cast<DrawLds *>(smem);
+    const int b = parts.b0 + blockIdx.y, tid = threadIdx.x, S = gridDim.x;
+    RowSpace &ws = parts.ws[blockIdx.y];
+    const Settings st = settings(a.prm, b);
+    Row<BF16> row = row_of<BF16>(a, b);
+    const uint64_t best = best_key(ws, S);
+    if (!begin(row, best, st, a.n)) {
+        if (blockIdx.x == 0 && tid == 0) put(a, b, best == 0 ? Result{-1, 0.0f, 0} : Result{key_id(best), 1.0f, 1});
+        return;
     }
+    const float u = a.u[b];
+
+    // sums over the bins, kBinsPer a thread
+    uint32_t cnt[kBinsPer], c = 0;
+    uint64_t sum[kBinsPer], x = 0;
+#pragma unroll
+    for (int i = 0; i < kBinsPer; ++i) {
+        cnt[i] = ws.count[tid * kBinsPer + i];
+        sum[i] = ws.sum[tid * kBinsPer + i];
+        c += cnt[i];
+        x += sum[i];
+    }
+    block_scan(c, x, s.wave_count, s.wave_sum);
+    uint32_t live = 0;
+    uint64_t total = 0;
+    for (int w = 0; w < kRowWaves; ++w) live += s.wave_count[w], total += s.wave_sum[w];
+    const uint32_t pass = ws.pass;
+    // before each of this thread's bins
+    uint32_t c0[kBinsPer];
+    uint64_t x0[kBinsPer];
+#pragma unroll
+    for (int i = kBinsPer - 1; i >= 0; --i) {
+        c -= cnt[i];
+        x -= sum[i];
+        c0[i] = c;
+        x0[i] = x;
+        s.d.base[tid * kBinsPer + i] = x;
+        s.d.rank[tid * kBinsPer + i] = c;
+    }
+    if (tid < kBins / 32) s.d.flag[tid] = 0;
+    // the bins of two borders, lo <= hi: each the first bin, not empty, up to
+    // whose end the rank (or the sum) is reached
+    auto bins = [&](bool by_rank, uint64_t lo, uint64_t hi) {
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < kBinsPer; ++i) {
+            const uint64_t v0 = by_rank ? c0[i] : x0[i], v1 = by_rank ? c0[i] + cnt[i] : x0[i] + sum[i];
+            const Bin at{tid * kBinsPer + i, c0[i], c0[i] + cnt[i], x0[i], x0[i] + sum[i]};
+            if (cnt[i] && v1 >= lo && (c0[i] == 0 || v0 < lo)) s.at[0] = at;
+            if (cnt[i] && v1 >= hi && (c0[i] == 0 || v0 < hi)) s.at[1] = at;
+        }
+        __syncthreads();
+    };
+    // this thread's bins from `first` to `last` are collected (a thread's
+    // bits lie in one word that it shares with seven others)
+    auto collect = [&](int first, int last) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < kBinsPer; ++i) {
+            const int bin = tid * kBinsPer + i;
+            if (bin >= first && bin <= last) m |= 1u << (bin % 32);
+        }
+        if (m) atomicOr(&s.d.flag[tid * kBinsPer / 32], m);
+    };
+    // Each quantity as the range that the bins leave it: C_K, ...
+    const uint32_t K = st.k > 0 && st.k < live ? st.k : live;
+    uint64_t lo = total, hi = total;
+    if (K < live) {
+        bins(true, K, K);
+        const Bin at = s.at[0];
+        hi = at.sum1;
+        lo = at.count1 == K ? hi : at.sum0;
+        if (lo != hi) collect(at.bin, at.bin);
+    }
+    const bool exact_k = lo == hi;
+    const uint64_t sum_k = hi;
+    // ... the number kept ...
+    const uint32_t most = st.m > 0.0f ? max(min(K, pass), 1u) : K;
+    uint32_t kmin = most, kmax = most;
+    if (st.p < 1.0f) {
+        bins(false, reach(st.p, lo), reach(st.p, hi));
+        kmin = min(most, s.at[0].count0 + 1);
+        kmax = min(most, s.at[1].count1);
+        collect(s.at[0].bin, s.at[1].bin);
+    }
+    // ... their weight ...
+    lo = hi = total;
+    bool exact_end = true;
+    if (kmin < live) {
+        bins(true, kmin, kmax);
+        hi = s.at[1].sum1;
+        exact_end = kmin == kmax && s.at[0].count1 == kmin;
+        lo = exact_end ? hi : s.at[0].sum0;
+        if (!exact_end) collect(s.at[0].bin, s.at[1].bin);
+    }
+    const uint64_t sum_end = hi;
+    // ... and the token.
+    auto past = [&](uint64_t end) { return min(below(u, end) + 1, end); };
+    bins(false, past(lo), past(hi));
+    collect(s.at[0].bin, s.at[1].bin);
+    __syncthreads();
+
+    // how many candidates that makes
+    uint32_t f = 0;
+#pragma unroll
+    for (int i = 0; i < kBinsPer; ++i)
+        if (s.d.flag[tid * kBinsPer / 32] >> ((tid * kBinsPer + i) % 32) & 1) f += cnt[i];
+    uint64_t unused = 0;
+    uint32_t fi = f;
+    block_scan(fi, unused, s.wave_count, s.wave_sum);
+    fi -= f;
+    uint32_t M = 0;
+    for (int w = 0; w < kRowWaves; ++w) M += s.wave_count[w];
+#pragma unroll
+    for (int i = 0; i < kBinsPer; ++i) {
+        s.d.first[tid * kBinsPer + i] = fi;
+        if (s.d.flag[tid * kBinsPer / 32] >> ((tid * kBinsPer + i) % 32) & 1) fi += cnt[i];
+    }
+    if (tid == 0) s.base = 0;
+    __syncthreads();
+    if (M > kCollect) {  // (the same in every workgroup of the row)
+        if (blockIdx.x != 0) return;
+        const Result r = draw_by_digits(row, st, u, live, total, pass, s.digits);
+        if (tid == 0) put(a, b, r);
+        return;
+    }
+
+    // collect: this part's in LDS, then all parts' in the workspace
+    const int64_t i0 = blockIdx.x * parts.len;
+    row.each(i0, min(parts.len, a.n - i0), [&](float l, int32_t id) {
+        const int bin = bin_of(row.best, l);
+        if (s.d.flag[bin / 32] >> (bin % 32) & 1) s.d.key[atomicAdd(&s.base, 1u)] = make_key(l, id);
+    });
+    __syncthreads();
+    if (S > 1) {
+        const uint32_t mine = s.base;
+        if (tid == 0) s.last = atomicAdd(&ws.collected, mine);
+        __syncthreads();
+        for (uint32_t i = tid; i < mine; i += kRowThreads) ws.key[s.last + i] = s.d.key[i];
+        __threadfence();
+        __syncthreads();
+        if (tid == 0) s.last = __hip_atomic_fetch_add(&ws.done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if (s.last != (uint32_t)S - 1) return;
+        __threadfence();
+        for (uint32_t i = tid; i < M; i += kRowThreads)
+            s.d.key[i] = __hip_atomic_load(&ws.key[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+    }
+
+    // their order, and their sums: a candidate's is that of the bins before
+    // its own and of those before it in its own
+    int P = 64;
+    while (P < (int)M) P <<= 1;
+    for (int i = (int)M + tid; i < P; i += kRowThreads) s.d.key[i] = 0;
+    __syncthreads();
+    sort_keys<kRowThreads>(s.d.key, P);
+    uint64_t own[kCollect / kRowThreads];
+    int64_t rank[kCollect / kRowThreads];
+    uint64_t base = 0;
+#pragma unroll
+    for (int h = 0; h < kCollect / kRowThreads; ++h) {
+        const int i = h * kRowThreads + tid;
+        uint32_t none = 0;
+        uint64_t w = i < (int)M ? row.units(key_logit(s.d.key[i])) : 0ull;
+        block_scan(none, w, s.wave_count, s.wave_sum);
+        s.d.sum[i] = base + w;
+        for (int v = 0; v < kRowWaves; ++v) base += s.wave_sum[v];
+        __syncthreads();
+    }
+#pragma unroll
+    for (int h = 0; h < kCollect / kRowThreads; ++h) {
+        const int i = h * kRowThreads + tid;
+        own[h] = ~0ull;
+        rank[h] = INT64_MAX;
+        if (i >= (int)M) continue;
+        const int bin = bin_of(row.best, key_logit(s.d.key[i]));
+        const uint32_t first = s.d.first[bin];
+        own[h] = s.d.base[bin] + s.d.sum[i] - (first ? s.d.sum[first - 1] : 0ull);
+        rank[h] = (int64_t)s.d.rank[bin] + i - first + 1;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < kCollect / kRowThreads; ++h) s.d.sum[h * kRowThreads + tid] = own[h];
+    // the first of the collected candidates with that rank, or sum
+    auto first = [&](bool by_rank, uint64_t v) {
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < kCollect / kRowThreads; ++h) {
+            const int i = h * kRowThreads + tid;
+            if (i >= (int)M) continue;
+            const bool hit = by_rank ? rank[h] == (int64_t)v : own[h] >= v && (i == 0 || s.d.sum[i - 1] < v);
+            if (hit) s.found_key = s.d.key[i], s.found_sum = own[h], s.found_rank = rank[h];
+        }
+        __syncthreads();
+    };
+    uint64_t ck = sum_k;
+    if (!exact_k) {
+        first(true, K);
+        ck = s.found_sum;
+    }
+    int64_t kept = most;
+    if (st.p < 1.0f) {
+        first(false, reach(st.p, ck));
+        kept = min(kept, s.found_rank);
+    }
+    uint64_t end = sum_end;
+    if (!exact_end) {
+        first(true, kept);
+        end = s.found_sum;
+    }
+    first(false, past(end));
+    if (tid == 0) put(a, b, drawn(row, s.found_key, end, kept));
 }
 
 vie_status launched(const char *what)
@@ -346,7 +704,7 @@ vie_status launched(const char *what)
 
 }  // namespace
 
-size_t sample_rows_workspace_bytes(int64_t, int) { return 0; }
+size_t sample_rows_workspace_bytes(int64_t, int B) { return (size_t)std::min(B, kMaxRows) * sizeof(RowSpace); }
 
 vie_status launch_sample_lists(const SampleLaunch &a, hipStream_t s)
 {
@@ -358,11 +716,31 @@ vie_status launch_sample_lists(const SampleLaunch &a, hipStream_t s)
     return launched("list sampling launch");
 }
 
+namespace {
+template <bool BF16> vie_status rows_launch(const SampleLaunch &a, hipStream_t s)
+{
+    // Parts of a row: enough for two workgroups a CU, of 8192 candidates at
+    // least (a part's work is a small part of its kernel below that).
+    const int64_t want = std::min<int64_t>((a.n + 8191) / 8192, 512 / a.B);
+    const int S = (int)std::max<int64_t>(1, std::min<int64_t>(want, kMaxParts));
+    const int64_t len = ((a.n + S - 1) / S + 63) / 64 * 64;
+    const hipError_t e = hipFuncSetAttribute((const void *)rows_draw_kernel<BF16>,
+                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(DrawLds));
+    if (e != hipSuccess) return fail(VIE_EHIP, "row sampling: %s", hipGetErrorString(e));
+    for (int b0 = 0; b0 < a.B; b0 += kMaxRows) {
+        const Parts parts{len, b0, static_cast<RowSpace *>(a.ws)};
+        const dim3 grid((unsigned)((a.n + len - 1) / len), (unsigned)std::min(kMaxRows, a.B - b0));
+        rows_best_kernel<BF16><<<grid, kRowThreads, 0, s>>>(a, parts);
+        rows_bins_kernel<BF16><<<grid, kRowThreads, 0, s>>>(a, parts);
+        rows_draw_kernel<BF16><<<grid, kRowThreads, sizeof(DrawLds), s>>>(a, parts);
+    }
+    return launched("row sampling launch");
+}
+}  // namespace
+
 vie_status launch_sample_rows(const SampleLaunch &a, hipStream_t s)
 {
-    if (a.dtype == VIE_BF16) sample_row_kernel<true><<<a.B, kRowThreads, 0, s>>>(a);
-    else sample_row_kernel<false><<<a.B, kRowThreads, 0, s>>>(a);
-    return launched("row sampling launch");
+    return a.dtype == VIE_BF16 ? rows_launch<true>(a, s) : rows_launch<false>(a, s);
 }
 
 }  // namespace vie
