@@ -388,10 +388,10 @@ vie_status vie_int8_logits(const int8_t *q_dev, const float *scale_dev, int64_t 
 /* How a token is drawn.  A setting applies to every row whose array (device
  * memory, one value per row) is NULL. */
 typedef struct {
-    float temperature;            /* <= 0 or NaN: the best candidate */
+    double temperature;           /* <= 0 or NaN: the best candidate */
+    double top_p;                 /* >= 1 or NaN: no limit */
+    double min_p;                 /* <= 0 or NaN: no limit */
     int32_t top_k;                /* <= 0: no limit */
-    float top_p;                  /* >= 1 or NaN: no limit */
-    float min_p;                  /* <= 0 or NaN: no limit */
     const float *temperature_dev; /* fp32[B] or NULL */
     const int32_t *top_k_dev;     /* int32[B] or NULL */
     const float *top_p_dev;       /* fp32[B] or NULL */

@@ -73,6 +73,37 @@ template <typename T> struct Span {
     }
 };
 
+// The value held by lane (lane ^ s), s = 1, 2, 4, 8, 16 or 32, without an LDS
+// round trip: quad permutes for 1 and 2, row shifts for 4, a row rotation for
+// 8, permlane swaps across rows.  Every lane of the wave is active, and s a
+// compile-time constant.
+__device__ __forceinline__ uint32_t lane_xor(uint32_t v, int s)
+{
+    const int lane = threadIdx.x & (kLanes - 1);
+    switch (s) {
+    case 1: return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xF, 0xF, true);
+    case 2: return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xF, 0xF, true);
+    case 4: {
+        const uint32_t up = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x104, 0xF, 0xF, true);
+        const uint32_t dn = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x114, 0xF, 0xF, true);
+        return (lane & 4) ? dn : up;
+    }
+    case 8: return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xF, 0xF, true);
+    case 16: {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return (lane & 16) ? r[0] : r[1];
+    }
+    default: {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return (lane & 32) ? r[0] : r[1];
+    }
+    }
+}
+__device__ __forceinline__ uint64_t lane_xor(uint64_t v, int s)
+{
+    return ((uint64_t)lane_xor((uint32_t)(v >> 32), s) << 32) | lane_xor((uint32_t)v, s);
+}
+
 template <typename T> __device__ __forceinline__ T wave_sum(T v)
 {
 #pragma unroll

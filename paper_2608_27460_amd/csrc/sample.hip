@@ -29,13 +29,14 @@ namespace vie {
 namespace {
 
 struct Settings {
-    float t, p, m;
+    double t, p, m;
     int k;
 };
 __device__ __forceinline__ Settings settings(const vie_sample_params &a, int b)
 {
-    return {a.temperature_dev ? a.temperature_dev[b] : a.temperature, a.top_p_dev ? a.top_p_dev[b] : a.top_p,
-            a.min_p_dev ? a.min_p_dev[b] : a.min_p, a.top_k_dev ? a.top_k_dev[b] : a.top_k};
+    return {a.temperature_dev ? (double)a.temperature_dev[b] : a.temperature,
+            a.top_p_dev ? (double)a.top_p_dev[b] : a.top_p, a.min_p_dev ? (double)a.min_p_dev[b] : a.min_p,
+            a.top_k_dev ? a.top_k_dev[b] : a.top_k};
 }
 
 __host__ __device__ inline int fixed_shift(int64_t n)
@@ -45,15 +46,48 @@ __host__ __device__ inline int fixed_shift(int64_t n)
     return 62 - lg;
 }
 
+// exp(x) for x <= 0 (or NaN, which gives 0), to 2^-49 relative: 2^(n / 64)
+// from the exponent and a 64-bit value per n % 64, times the Taylor sum of the rest, at
+// most ln 2 / 128 in size, to the fifth power (the sixth is below 2^-54).
+struct Exp2Table {
+    double v[64];
+};
+constexpr double exp2_64(int i)  // 2^(i / 64) by its series
+{
+    const double x = i * 0.69314718055994530942 / 64;
+    double t = 1.0, s = 1.0;
+    for (int n = 1; n < 26; ++n) t *= x / n, s += t;
+    return s;
+}
+constexpr Exp2Table make_table()
+{
+    Exp2Table t{};
+    for (int i = 0; i < 64; ++i) t.v[i] = exp2_64(i);
+    return t;
+}
+__device__ constexpr Exp2Table kExp2 = make_table();
+
+__device__ __forceinline__ double exp_down(double x)
+{
+    const double k = rint(fmax(x, -800.0) * (64 * 1.4426950408889634074));  // (fmax: the number, if one is NaN)
+    double r = fma(k, -0.69314718055994530942 / 64, x);
+    r = fma(k, -2.3190468138462996e-17 / 64, r);
+    double p = fma(r, 1.0 / 120, 1.0 / 24);
+    p = fma(p, r, 1.0 / 6);
+    p = fma(p, r, 0.5);
+    p = fma(p, r, 1.0);
+    p = fma(p, r, 1.0);
+    const int n = (int)k;
+    return x >= -745.0 ? ldexp(kExp2.v[n & 63] * p, n >> 6) : 0.0;
+}
 __device__ __forceinline__ double weight(float l, float best, double inv_t)
 {
-    const double x = ((double)l - (double)best) * inv_t;
-    return l == best ? 1.0 : x == x ? exp(x) : 0.0;  // (no number: the best is +inf and so is t)
+    return l == best ? 1.0 : exp_down(((double)l - (double)best) * inv_t);
 }
 __device__ __forceinline__ uint64_t fixed(double w, double one) { return (uint64_t)(w * one + 0.5); }
 
 // Borders as integers: C >= p T iff C >= reach(p, T), C > u T iff C > below(u, T).
-__device__ __forceinline__ uint64_t reach(float p, uint64_t total) { return p > 0.0f ? (uint64_t)ceil((double)p * (double)total) : 0ull; }
+__device__ __forceinline__ uint64_t reach(double p, uint64_t total) { return p > 0.0 ? (uint64_t)ceil(p * (double)total) : 0ull; }
 __device__ __forceinline__ uint64_t below(float u, uint64_t total)
 {
     return u > 0.0f ? (uint64_t)fmin((double)u * (double)total, 9.2e18) : 0ull;
@@ -141,12 +175,12 @@ template <int NT> __global__ __launch_bounds__(NT) void sample_list_kernel(Sampl
         if (tid == 0) put(a, b, {-1, 0.0f, 0});
         return;
     }
-    if (!(st.t > 0.0f)) {
+    if (!(st.t > 0.0)) {
         if (tid == 0) put(a, b, {key_id(s_key[0]), 1.0f, 1});
         return;
     }
     const float best = key_logit(s_key[0]);
-    const double inv_t = 1.0 / (double)st.t, one = ldexp(1.0, fixed_shift(kMaxList));
+    const double inv_t = 1.0 / st.t, one = ldexp(1.0, fixed_shift(kMaxList));
     const int K = st.k > 0 && st.k < live ? st.k : live;
     // sums in order, NT candidates at a time; the prefix that passes min-p
     uint64_t base = 0;
@@ -154,7 +188,7 @@ template <int NT> __global__ __launch_bounds__(NT) void sample_list_kernel(Sampl
         const int j = j0 + tid;
         double w = 0.0;
         if (j < K) w = weight(key_logit(s_key[j]), best, inv_t);
-        const bool ok = j < K && w >= (double)st.m;
+        const bool ok = j < K && w >= st.m;
         uint64_t x = wave_scan(j < K ? fixed(w, one) : 0ull);
         const unsigned long long pass = __ballot(ok);
         if (W > 1) {
@@ -172,8 +206,8 @@ template <int NT> __global__ __launch_bounds__(NT) void sample_list_kernel(Sampl
     __syncthreads();
     if (tid != 0) return;
     int kept = K;
-    if (st.p < 1.0f) kept = min(kept, first_at<false>(s_sum, K, reach(st.p, s_sum[K - 1])) + 1);
-    if (st.m > 0.0f) kept = min(kept, s_min);
+    if (st.p < 1.0) kept = min(kept, first_at<false>(s_sum, K, reach(st.p, s_sum[K - 1])) + 1);
+    if (st.m > 0.0) kept = min(kept, s_min);
     kept = max(kept, 1);
     const uint64_t total = s_sum[kept - 1];
     const int j = min(first_at<true>(s_sum, kept, below(u, total)), kept - 1);
@@ -202,29 +236,30 @@ template <int NT> __global__ __launch_bounds__(NT) void sample_list_kernel(Sampl
 //                      sums, from those of the bins before, give the exact
 //                      borders.
 //
-// A bin is the leading bits of the fp32 distance: 256 to the octave from
-// 2^-8 to 2^8, so the bins are finest where the candidates are few and weigh
-// most, whatever the spread of the logits and the temperature.  A border in
-// the bulk of 262144 normal logits meets some 1600 candidates of its bin.
-// Rows whose border bins hold more than kCollect (constant rows, or spreads
-// far from a model's) take the borders one after the other from histograms
-// of the keys' digits: exact too, in up to 24 passes of one workgroup.
+// A bin is the leading bits of the fp32 distance: 1024 to the octave from 1/8
+// to 32, so that the bins are finest where the candidates are few and weigh
+// most.  A border in the bulk of 262144 normal logits meets some 400
+// candidates of its bin.  Rows whose border bins hold more than kCollect
+// (constant rows, or spreads far from a model's) take the borders one after
+// the other from histograms of the keys' digits: exact too, in up to 24
+// passes of one workgroup.
 
 constexpr int kRowThreads = 1024;
 constexpr int kRowWaves = kRowThreads / kLanes;
 constexpr int kDigit = 11;                 // key bits settled by a pass
 constexpr int kDigits = 1 << kDigit;
-constexpr int kBins = 4096;
+constexpr int kBins = 8192;
 constexpr int kBinsPer = kBins / kRowThreads;
 constexpr int kCollect = 2048;             // candidates put in order one by one
-constexpr int kMaxParts = 32;
-constexpr int kMaxRows = 1024;             // rows of one round of launches (66 KB of workspace each)
+constexpr int kMaxParts = 128;
+constexpr int kMaxSlots = 256;             // bins that borders can fall into
+constexpr int kMaxRows = 1024;             // rows of one round of launches (114 KB of workspace each)
 
 // The bin of a logit: monotone, bin 0 the best.
 __device__ __forceinline__ int bin_of(float best, float l)
 {
-    constexpr int kFirst = 119 << 8;  // 2^-8: exponent 119, eight mantissa bits
-    const int x = (int)(__float_as_uint(l == best ? 0.0f : best - l) >> 15) - kFirst + 1;
+    constexpr int kFirst = 124 << 10;  // 2^-3: exponent 124, ten mantissa bits
+    const int x = (int)(__float_as_uint(l == best ? 0.0f : best - l) >> 13) - kFirst + 1;
     return x < 0 ? 0 : x > kBins - 1 ? kBins - 1 : x;
 }
 
@@ -294,12 +329,12 @@ __device__ __forceinline__ void block_scan(uint32_t &c, uint64_t &s, uint32_t *w
     for (int w = 0; w < wave; ++w) c += wave_count[w], s += wave_sum[w];
 }
 
-// The first candidate in the order whose rank is at least `rank` (BY_RANK),
+// The first candidate in the order whose rank is at least `rank` (by_rank),
 // or else whose sum is at least `sum`: digits of the keys from the top, each
 // by a histogram of the candidates that share the digits before.  If there is
 // none (`sum` above the total), the last candidate.
-template <bool BF16, bool BY_RANK>
-__device__ Place find(const Row<BF16> &row, int64_t rank, uint64_t sum, DigitLds &s)
+template <bool BF16>
+__device__ __noinline__ Place find(const Row<BF16> &row, bool by_rank, int64_t rank, uint64_t sum, DigitLds &s)
 {
     const int tid = threadIdx.x;
     uint64_t prefix = 0, before_sum = 0;
@@ -332,7 +367,7 @@ __device__ Place find(const Row<BF16> &row, int64_t rank, uint64_t sum, DigitLds
         const uint64_t e1 = cs, e0 = cs - s1, b0 = e0 - s0;
         const int64_t r1 = rc, r0 = rc - c1, q0 = r0 - c0;
         auto take = [&](int bin, uint64_t sum0, int64_t rank0) { s.bin = bin, s.at.sum = sum0, s.at.rank = rank0; };
-        auto hit = [&](int64_t r, uint64_t c) { return BY_RANK ? r >= rank : c >= sum; };
+        auto hit = [&](int64_t r, uint64_t c) { return by_rank ? r >= rank : c >= sum; };
         if (c0 && hit(r0, e0) && !(q0 > before && hit(q0, b0))) take(top, b0, q0);
         if (c1 && hit(r1, e1) && !(r0 > before && hit(r0, e0))) take(top - 1, e0, r0);
         __syncthreads();
@@ -359,16 +394,16 @@ template <bool BF16> __device__ __forceinline__ Result drawn(const Row<BF16> &ro
 // The borders one after the other, over the whole row: `live` candidates,
 // `total` units of weight, `pass` candidates within min-p.
 template <bool BF16>
-__device__ Result draw_by_digits(const Row<BF16> &row, Settings st, float u, uint32_t live, uint64_t total, uint32_t pass,
+__device__ __noinline__ Result draw_by_digits(const Row<BF16> &row, Settings st, float u, uint32_t live, uint64_t total, uint32_t pass,
                                  DigitLds &s)
 {
     Place end{0, total, (int64_t)live};  // the last candidate kept
-    if (st.k > 0 && st.k < live) end = find<BF16, true>(row, st.k, 0, s);
-    if (st.p < 1.0f) end = find<BF16, false>(row, 0, reach(st.p, end.sum), s);
-    if (st.m > 0.0f && (int64_t)pass < end.rank) end = find<BF16, true>(row, max(pass, 1u), 0, s);
+    if (st.k > 0 && st.k < live) end = find<BF16>(row, true, st.k, 0, s);
+    if (st.p < 1.0) end = find<BF16>(row, false, 0, reach(st.p, end.sum), s);
+    if (st.m > 0.0 && (int64_t)pass < end.rank) end = find<BF16>(row, true, max(pass, 1u), 0, s);
     // (never beyond the kept ones, also for u of 1 and above)
     const uint64_t past = below(u, end.sum) + 1;
-    const Place at = find<BF16, false>(row, 0, past < end.sum ? past : end.sum, s);
+    const Place at = find<BF16>(row, false, 0, past < end.sum ? past : end.sum, s);
     return drawn(row, at.key, end.sum, end.rank);
 }
 
@@ -404,25 +439,26 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_best_ke
 __device__ __forceinline__ uint64_t best_key(const RowSpace &ws, int S)
 {
     uint64_t k = 0;
-    for (int i = 0; i < S; ++i) k = ws.best[i] > k ? ws.best[i] : k;
-    return k;
+    for (int i = threadIdx.x & (kLanes - 1); i < S; i += kLanes) k = max(k, ws.best[i]);
+    return wave_max(k);
 }
 
 // The row's best logit and scale; false if nothing is left to draw (no
 // candidate, or the best one).
 template <bool BF16> __device__ __forceinline__ bool begin(Row<BF16> &row, uint64_t best, Settings st, int64_t n)
 {
-    if (best == 0 || !(st.t > 0.0f)) return false;
+    if (best == 0 || !(st.t > 0.0)) return false;
     row.best = key_logit(best);
-    row.inv_t = 1.0 / (double)st.t;
+    row.inv_t = 1.0 / st.t;
     row.one = ldexp(1.0, fixed_shift(n));
     return true;
 }
 
 template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_bins_kernel(SampleLaunch a, Parts parts)
 {
-    __shared__ uint64_t s_sum[kBins];
-    __shared__ uint32_t s_count[kBins];
+    extern __shared__ __align__(16) char smem[];
+    uint64_t *s_sum = reinterpret_cast<uint64_t *>(smem);
+    uint32_t *s_count = reinterpret_cast<uint32_t *>(s_sum + kBins);
     __shared__ uint32_t s_pass;
     const int b = parts.b0 + blockIdx.y, tid = threadIdx.x;
     RowSpace &ws = parts.ws[blockIdx.y];
@@ -437,7 +473,7 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_bins_ke
     row.each(i0, min(parts.len, a.n - i0), [&](float l, int32_t) {
         const int bin = bin_of(row.best, l);
         const double w = weight(l, row.best, row.inv_t);
-        pass += w >= (double)st.m;
+        pass += w >= st.m;
         atomicAdd(&s_count[bin], 1u);
         atomicAdd((unsigned long long *)&s_sum[bin], (unsigned long long)fixed(w, row.one));
     });
@@ -459,13 +495,18 @@ struct Bin {
     uint64_t sum0, sum1;
 };
 
+// A bin whose candidates are collected: what lies before it, and how many
+// collected candidates.
+struct Slot {
+    uint64_t base;
+    uint32_t rank, first;
+};
+
 struct DrawLds {
     union {
         struct {
             uint64_t key[kCollect], sum[kCollect];  // the collected candidates in order, their sums
-            uint64_t base[kBins];                   // weight before a bin
-            uint32_t first[kBins];                  // collected candidates before a bin
-            uint32_t rank[kBins];                   // candidates before a bin
+            Slot slot[kMaxSlots];
             uint32_t flag[kBins / 32];              // the bins collected
         } d;
         DigitLds digits;
@@ -477,6 +518,57 @@ struct DrawLds {
     int64_t found_rank;
     uint32_t base, last;
 };
+
+// P keys (a power of two, at most E kRowThreads) in descending order: thread
+// t holds keys t, t + kRowThreads, ..; pairs less than a wave apart meet by
+// lane exchanges, the others in LDS.
+template <int E> __device__ void sort_row(uint64_t *key, int P)
+{
+    const int tid = threadIdx.x;
+    uint64_t v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = e * kRowThreads + tid < P ? key[e * kRowThreads + tid] : 0ull;
+    auto keep = [&](int e, uint64_t o, int k, int j) {  // the larger one goes first in a descending run
+        const int i = e * kRowThreads + tid;
+        const bool larger = ((i & k) == 0) == ((i & j) == 0);
+        v[e] = (v[e] > o) == larger ? v[e] : o;
+    };
+    for (int k = 2; k <= P; k <<= 1) {
+        for (int j = k >> 1; j >= kLanes; j >>= 1) {
+            if (j >= kRowThreads) {
+                if constexpr (E == 2) {
+                    const uint64_t a = v[0], b = v[1];
+                    keep(0, b, k, j);
+                    keep(1, a, k, j);
+                }
+                continue;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (e * kRowThreads + tid < P) key[e * kRowThreads + tid] = v[e];
+            __syncthreads();
+#pragma unroll
+            for (int e = 0; e < E; ++e)
+                if (e * kRowThreads + tid < P) keep(e, key[(e * kRowThreads + tid) ^ j], k, j);
+        }
+#define VIE_LANE_STEP(J)                                                                  \
+    if (k > J)                                                                            \
+        for (int e = 0; e < E; ++e) keep(e, lane_xor(v[e], J), k, J);
+        VIE_LANE_STEP(32)
+        VIE_LANE_STEP(16)
+        VIE_LANE_STEP(8)
+        VIE_LANE_STEP(4)
+        VIE_LANE_STEP(2)
+        VIE_LANE_STEP(1)
+#undef VIE_LANE_STEP
+    }
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+        if (e * kRowThreads + tid < P) key[e * kRowThreads + tid] = v[e];
+    __syncthreads();
+}
 
 template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_kernel(SampleLaunch a, Parts parts)
 {
@@ -503,47 +595,47 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
         c += cnt[i];
         x += sum[i];
     }
+    const uint32_t call = c;
+    const uint64_t xall = x;
     block_scan(c, x, s.wave_count, s.wave_sum);
     uint32_t live = 0;
     uint64_t total = 0;
     for (int w = 0; w < kRowWaves; ++w) live += s.wave_count[w], total += s.wave_sum[w];
     const uint32_t pass = ws.pass;
-    // before each of this thread's bins
-    uint32_t c0[kBinsPer];
-    uint64_t x0[kBinsPer];
-#pragma unroll
-    for (int i = kBinsPer - 1; i >= 0; --i) {
-        c -= cnt[i];
-        x -= sum[i];
-        c0[i] = c;
-        x0[i] = x;
-        s.d.base[tid * kBinsPer + i] = x;
-        s.d.rank[tid * kBinsPer + i] = c;
-    }
-    if (tid < kBins / 32) s.d.flag[tid] = 0;
+    // before this thread's bins
+    c -= call;
+    x -= xall;
+    for (int i = tid; i < kBins / 32; i += kRowThreads) s.d.flag[i] = 0;
     // the bins of two borders, lo <= hi: each the first bin, not empty, up to
-    // whose end the rank (or the sum) is reached
+    // whose end the rank (or the sum) is reached; one thread holds it
+    const uint32_t cend = c + call;
+    const uint64_t xend = x + xall;
+    auto bin_at = [&](bool by_rank, uint64_t v, Bin &out) {
+        const uint64_t before = by_rank ? c : x, after = by_rank ? cend : xend;
+        if (call == 0 || after < v || (c != 0 && before >= v)) return;
+        uint32_t ci = c;
+        uint64_t xi = x;
+#pragma unroll
+        for (int i = 0; i < kBinsPer; ++i) {
+            const uint64_t v0 = by_rank ? ci : xi, v1 = by_rank ? ci + cnt[i] : xi + sum[i];
+            if (cnt[i] && v1 >= v && (ci == 0 || v0 < v)) out = {tid * kBinsPer + i, ci, ci + cnt[i], xi, xi + sum[i]};
+            ci += cnt[i];
+            xi += sum[i];
+        }
+    };
     auto bins = [&](bool by_rank, uint64_t lo, uint64_t hi) {
         __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kBinsPer; ++i) {
-            const uint64_t v0 = by_rank ? c0[i] : x0[i], v1 = by_rank ? c0[i] + cnt[i] : x0[i] + sum[i];
-            const Bin at{tid * kBinsPer + i, c0[i], c0[i] + cnt[i], x0[i], x0[i] + sum[i]};
-            if (cnt[i] && v1 >= lo && (c0[i] == 0 || v0 < lo)) s.at[0] = at;
-            if (cnt[i] && v1 >= hi && (c0[i] == 0 || v0 < hi)) s.at[1] = at;
-        }
+        bin_at(by_rank, lo, s.at[0]);
+        if (hi != lo) bin_at(by_rank, hi, s.at[1]);
         __syncthreads();
+        return hi != lo ? 1 : 0;  // where the second one is
     };
     // this thread's bins from `first` to `last` are collected (a thread's
-    // bits lie in one word that it shares with seven others)
+    // bits lie in one word that it shares with three others)
     auto collect = [&](int first, int last) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < kBinsPer; ++i) {
-            const int bin = tid * kBinsPer + i;
-            if (bin >= first && bin <= last) m |= 1u << (bin % 32);
-        }
-        if (m) atomicOr(&s.d.flag[tid * kBinsPer / 32], m);
+        if (first >= (tid + 1) * kBinsPer || last < tid * kBinsPer) return;
+        const int f = max(first - tid * kBinsPer, 0), l = min(last - tid * kBinsPer, kBinsPer - 1);
+        atomicOr(&s.d.flag[tid * kBinsPer / 32], ((2u << l) - (1u << f)) << (tid * kBinsPer % 32));
     };
     // Each quantity as the range that the bins leave it: C_K, ...
     const uint32_t K = st.k > 0 && st.k < live ? st.k : live;
@@ -558,50 +650,63 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     const bool exact_k = lo == hi;
     const uint64_t sum_k = hi;
     // ... the number kept ...
-    const uint32_t most = st.m > 0.0f ? max(min(K, pass), 1u) : K;
+    const uint32_t most = st.m > 0.0 ? max(min(K, pass), 1u) : K;
     uint32_t kmin = most, kmax = most;
-    if (st.p < 1.0f) {
-        bins(false, reach(st.p, lo), reach(st.p, hi));
+    if (st.p < 1.0) {
+        const int e = bins(false, reach(st.p, lo), reach(st.p, hi));
         kmin = min(most, s.at[0].count0 + 1);
-        kmax = min(most, s.at[1].count1);
-        collect(s.at[0].bin, s.at[1].bin);
+        kmax = min(most, s.at[e].count1);
+        collect(s.at[0].bin, s.at[e].bin);
     }
     // ... their weight ...
     lo = hi = total;
     bool exact_end = true;
     if (kmin < live) {
-        bins(true, kmin, kmax);
-        hi = s.at[1].sum1;
+        const int e = bins(true, kmin, kmax);
+        hi = s.at[e].sum1;
         exact_end = kmin == kmax && s.at[0].count1 == kmin;
         lo = exact_end ? hi : s.at[0].sum0;
-        if (!exact_end) collect(s.at[0].bin, s.at[1].bin);
+        if (!exact_end) collect(s.at[0].bin, s.at[e].bin);
     }
     const uint64_t sum_end = hi;
     // ... and the token.
     auto past = [&](uint64_t end) { return min(below(u, end) + 1, end); };
-    bins(false, past(lo), past(hi));
-    collect(s.at[0].bin, s.at[1].bin);
+    const int e = bins(false, past(lo), past(hi));
+    collect(s.at[0].bin, s.at[e].bin);
     __syncthreads();
 
-    // how many candidates that makes
-    uint32_t f = 0;
+    // how many bins and candidates that makes
+    const uint32_t flags = s.d.flag[tid * kBinsPer / 32] >> (tid * kBinsPer % 32);
+    uint32_t f = 0, n = 0;
+    if (flags & ((1u << kBinsPer) - 1)) {
 #pragma unroll
-    for (int i = 0; i < kBinsPer; ++i)
-        if (s.d.flag[tid * kBinsPer / 32] >> ((tid * kBinsPer + i) % 32) & 1) f += cnt[i];
-    uint64_t unused = 0;
+        for (int i = 0; i < kBinsPer; ++i)
+            if (flags >> i & 1 && cnt[i]) f += cnt[i], ++n;
+    }
+    uint64_t slots = n;
     uint32_t fi = f;
-    block_scan(fi, unused, s.wave_count, s.wave_sum);
+    block_scan(fi, slots, s.wave_count, s.wave_sum);
     fi -= f;
-    uint32_t M = 0;
-    for (int w = 0; w < kRowWaves; ++w) M += s.wave_count[w];
+    slots -= n;
+    uint32_t M = 0, nslot = 0;
+    for (int w = 0; w < kRowWaves; ++w) M += s.wave_count[w], nslot += (uint32_t)s.wave_sum[w];
+    if (n) {
+        uint32_t ci = c;
+        uint64_t xi = x;
 #pragma unroll
-    for (int i = 0; i < kBinsPer; ++i) {
-        s.d.first[tid * kBinsPer + i] = fi;
-        if (s.d.flag[tid * kBinsPer / 32] >> ((tid * kBinsPer + i) % 32) & 1) fi += cnt[i];
+        for (int i = 0; i < kBinsPer; ++i) {
+            if (flags >> i & 1 && cnt[i]) {
+                if (slots < kMaxSlots) s.d.slot[slots] = Slot{xi, ci, fi};
+                fi += cnt[i];
+                ++slots;
+            }
+            ci += cnt[i];
+            xi += sum[i];
+        }
     }
     if (tid == 0) s.base = 0;
     __syncthreads();
-    if (M > kCollect) {  // (the same in every workgroup of the row)
+    if (M > kCollect || nslot > kMaxSlots) {  // (the same in every workgroup of the row)
         if (blockIdx.x != 0) return;
         const Result r = draw_by_digits(row, st, u, live, total, pass, s.digits);
         if (tid == 0) put(a, b, r);
@@ -619,13 +724,17 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
         const uint32_t mine = s.base;
         if (tid == 0) s.last = atomicAdd(&ws.collected, mine);
         __syncthreads();
-        for (uint32_t i = tid; i < mine; i += kRowThreads) ws.key[s.last + i] = s.d.key[i];
-        __threadfence();
+        // Stores and loads at the device's point of coherence: no cache is
+        // written back for them (with fences, which do that, the kernel took
+        // 46 us for a row of 262144).  A store is there once it is counted
+        // down, so that the workgroup that counts last sees all of them.
+        for (uint32_t i = tid; i < mine; i += kRowThreads)
+            __hip_atomic_store(&ws.key[s.last + i], s.d.key[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        if (tid == 0) s.last = __hip_atomic_fetch_add(&ws.done, 1u, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+        if (tid == 0) s.last = __hip_atomic_fetch_add(&ws.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
         if (s.last != (uint32_t)S - 1) return;
-        __threadfence();
         for (uint32_t i = tid; i < M; i += kRowThreads)
             s.d.key[i] = __hip_atomic_load(&ws.key[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
@@ -637,7 +746,8 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     while (P < (int)M) P <<= 1;
     for (int i = (int)M + tid; i < P; i += kRowThreads) s.d.key[i] = 0;
     __syncthreads();
-    sort_keys<kRowThreads>(s.d.key, P);
+    if (P <= kRowThreads) sort_row<1>(s.d.key, P);
+    else sort_row<2>(s.d.key, P);
     uint64_t own[kCollect / kRowThreads];
     int64_t rank[kCollect / kRowThreads];
     uint64_t base = 0;
@@ -657,10 +767,15 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
         own[h] = ~0ull;
         rank[h] = INT64_MAX;
         if (i >= (int)M) continue;
-        const int bin = bin_of(row.best, key_logit(s.d.key[i]));
-        const uint32_t first = s.d.first[bin];
-        own[h] = s.d.base[bin] + s.d.sum[i] - (first ? s.d.sum[first - 1] : 0ull);
-        rank[h] = (int64_t)s.d.rank[bin] + i - first + 1;
+        int lo = 0, hi = (int)nslot - 1;  // its bin: the last slot that begins at or before it
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (s.d.slot[mid].first <= (uint32_t)i) lo = mid;
+            else hi = mid - 1;
+        }
+        const Slot at = s.d.slot[lo];
+        own[h] = at.base + s.d.sum[i] - (at.first ? s.d.sum[at.first - 1] : 0ull);
+        rank[h] = (int64_t)at.rank + i - at.first + 1;
     }
     __syncthreads();
 #pragma unroll
@@ -683,7 +798,7 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
         ck = s.found_sum;
     }
     int64_t kept = most;
-    if (st.p < 1.0f) {
+    if (st.p < 1.0) {
         first(false, reach(st.p, ck));
         kept = min(kept, s.found_rank);
     }
@@ -719,19 +834,21 @@ vie_status launch_sample_lists(const SampleLaunch &a, hipStream_t s)
 namespace {
 template <bool BF16> vie_status rows_launch(const SampleLaunch &a, hipStream_t s)
 {
-    // Parts of a row: enough for two workgroups a CU, of 8192 candidates at
-    // least (a part's work is a small part of its kernel below that).
-    const int64_t want = std::min<int64_t>((a.n + 8191) / 8192, 512 / a.B);
+    // Parts of a row: one workgroup a CU, of 4096 candidates at least.
+    const int64_t want = std::min<int64_t>((a.n + 4095) / 4096, 256 / a.B);
     const int S = (int)std::max<int64_t>(1, std::min<int64_t>(want, kMaxParts));
     const int64_t len = ((a.n + S - 1) / S + 63) / 64 * 64;
-    const hipError_t e = hipFuncSetAttribute((const void *)rows_draw_kernel<BF16>,
-                                             hipFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(DrawLds));
+    constexpr int kBinsLds = kBins * 12;
+    hipError_t e = hipFuncSetAttribute((const void *)rows_draw_kernel<BF16>, hipFuncAttributeMaxDynamicSharedMemorySize,
+                                       (int)sizeof(DrawLds));
+    if (e == hipSuccess)
+        e = hipFuncSetAttribute((const void *)rows_bins_kernel<BF16>, hipFuncAttributeMaxDynamicSharedMemorySize, kBinsLds);
     if (e != hipSuccess) return fail(VIE_EHIP, "row sampling: %s", hipGetErrorString(e));
     for (int b0 = 0; b0 < a.B; b0 += kMaxRows) {
         const Parts parts{len, b0, static_cast<RowSpace *>(a.ws)};
         const dim3 grid((unsigned)((a.n + len - 1) / len), (unsigned)std::min(kMaxRows, a.B - b0));
         rows_best_kernel<BF16><<<grid, kRowThreads, 0, s>>>(a, parts);
-        rows_bins_kernel<BF16><<<grid, kRowThreads, 0, s>>>(a, parts);
+        rows_bins_kernel<BF16><<<grid, kRowThreads, kBinsLds, s>>>(a, parts);
         rows_draw_kernel<BF16><<<grid, kRowThreads, sizeof(DrawLds), s>>>(a, parts);
     }
     return launched("row sampling launch");

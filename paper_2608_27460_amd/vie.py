@@ -41,7 +41,7 @@ class GpuBuildParams(C.Structure):
 
 
 class SamplingParams(C.Structure):
-    _fields_ = [("temperature", C.c_float), ("top_k", C.c_int32), ("top_p", C.c_float), ("min_p", C.c_float),
+    _fields_ = [("temperature", C.c_double), ("top_p", C.c_double), ("min_p", C.c_double), ("top_k", C.c_int32),
                 ("temperature_dev", C.c_void_p), ("top_k_dev", C.c_void_p), ("top_p_dev", C.c_void_p),
                 ("min_p_dev", C.c_void_p)]
 
@@ -448,7 +448,7 @@ class Int8Head:
 
 def _sampling(B: int, device, temperature, top_k, top_p, min_p) -> SamplingParams:
     """Each setting is a number, or a device tensor [B] (fp32; top_k int32)."""
-    p = SamplingParams(1.0, 0, 1.0, 0.0)
+    p = SamplingParams(1.0, 1.0, 0.0, 0)
     for name, v, dtype in (("temperature", temperature, "float32"), ("top_k", top_k, "int32"),
                            ("top_p", top_p, "float32"), ("min_p", min_p, "float32")):
         if hasattr(v, "data_ptr"):

@@ -169,8 +169,7 @@ def draw_reference(l, ids, u, t, k, p, m):
 def check_draws(got, l, ids, u, t, k, p, m, what):
     tok, prob, kept = (x.cpu().numpy() for x in got)
     B = l.shape[0]
-    full = lambda v, dt: np.broadcast_to(np.asarray(v.cpu() if hasattr(v, "cpu") else v, dt), (B,))  # noqa: E731
-    t, k, p, m = full(t, np.float32), full(k, np.int64), full(p, np.float32), full(m, np.float32)
+    t, k, p, m = (np.broadcast_to(np.asarray(v), (B,)) for v in (t, k, p, m))  # (numbers in 64 bits, arrays in fp32)
     for b in range(B):
         rt, rp, rk = draw_reference(l[b], ids if ids.ndim == 1 else ids[b], u[b], t[b], k[b], p[b], m[b])
         assert (tok[b], kept[b]) == (rt, rk), "%s row %d: token %d kept %d, expected %d and %d" % (what, b, tok[b], kept[b], rt, rk)

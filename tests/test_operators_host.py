@@ -10,7 +10,7 @@ from paper_2608_27460_amd import vie
 L = vie.lib
 P = C.c_void_p(4096)      # never dereferenced: every call below fails its checks first
 ODD = C.c_void_p(4097)
-PRM = vie.SamplingParams(1.0, 0, 1.0, 0.0)
+PRM = vie.SamplingParams(1.0, 1.0, 0.0, 0)
 BIG = 1 << 40
 
 
