@@ -11,6 +11,9 @@
 // (v_mfma_i32_16x16x64_i8: 16 rows, 16 tokens, 64 columns).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <type_traits>
+
 #include "block.hpp"
 #include "operators.hpp"
 
@@ -20,9 +23,10 @@ namespace {
 
 typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kStep = 64;  // columns of a matrix instruction
+constexpr int kStep = 64;   // columns of a matrix instruction
+constexpr int kPad = 128;   // tokens are padded to whole stages
 
-__host__ __device__ inline int padded(int d) { return (d + kStep - 1) / kStep * kStep; }
+__host__ __device__ inline int padded(int d) { return (d + kPad - 1) / kPad * kPad; }
 
 __device__ __forceinline__ int quantized(float x, float scale)
 {
@@ -97,6 +101,290 @@ __global__ __launch_bounds__(256) void int8_simple_kernel(const int8_t *__restri
     }
 }
 
+// ---------------------------------------------------------------------------
+// tiles through LDS
+// ---------------------------------------------------------------------------
+//
+// A workgroup of eight waves takes tiles of up to VT = 256 rows and BT tokens.
+// Columns go by stages of KC bytes: the rows' and the tokens' bytes of a stage
+// go from memory straight to LDS (16 bytes a lane), NBUF stages ahead and
+// across the ends of tiles, and a wave reads the operands of the next stage
+// from LDS into registers while it multiplies those of the present one, so
+// that the matrix cores wait for neither.  A wave multiplies 16 MT rows by 16
+// NT tokens.
+//
+// Piece p (16 bytes) of staged row x sits in slot p ^ swizzle(x) of that row,
+// so that the operand reads (16 rows, one piece each) hit every LDS bank
+// once.  Pieces past a row re-read its last one, against zeros of the token;
+// rows and tokens past the tile re-read its last one, and their results are
+// not stored.
+//
+// The logits leave through 4 KB of LDS of each wave's own, 16 tokens at a
+// time, so that a store covers runs of 256 bytes of a token's row; the
+// stages of the next tile go on arriving meanwhile.
+
+constexpr int kWaves = 8;
+constexpr int kThreads = kWaves * kLanes;
+constexpr int kWorkgroups = 256;  // one per CU
+constexpr int kTileRows = 256;
+
+template <int KC> __device__ __forceinline__ int swizzle(int x) { return KC == 64 ? x >> 2 & 3 : x >> 1 & 7; }
+
+__device__ __forceinline__ void load_lds16(const int8_t *src, char *dst)
+{
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)src,
+                                     (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
+}
+
+constexpr int tile_stage(int BT, int KC) { return (kTileRows + BT) * KC; }
+constexpr int tile_lds(int BT, int KC, int NBUF) { return tile_stage(BT, KC) * NBUF + kWaves * 4096; }
+
+// Tile t of a workgroup: XCD blockIdx.x % 8 takes a run of the tiles, its
+// workgroups take every 32nd of them, and the order goes over up to eight
+// token tiles first, so that an XCD's workgroups share rows and tokens in L2.
+struct Tiles {
+    int rows;          // rows of a tile (at most kTileRows)
+    int nv, nb;        // tiles of rows, of tokens
+    int per_xcd, step; // tiles of an XCD's run, its workgroups
+};
+
+template <int MT, int NT, int WB, int KC, int NBUF, bool AHEAD, bool OUT_BF16>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void int8_tile_kernel(
+    const int8_t *__restrict__ q, int pitch, const float *__restrict__ scale, int64_t V, const int8_t *__restrict__ x,
+    int dp, const float *__restrict__ xs, int B, typename Elem<OUT_BF16>::T *__restrict__ out, int64_t ld, Tiles tiles)
+{
+    typedef Elem<OUT_BF16> E;
+    extern __shared__ __align__(16) char smem[];
+    constexpr int BT = 16 * NT * WB;
+    static_assert(kWaves / WB * MT * 16 == kTileRows, "the waves cover a tile");
+    constexpr int kStage = tile_stage(BT, KC), P = KC / 16, LR = kLanes / P, KS = KC / kStep;
+    constexpr int WL = kTileRows / kWaves / LR;                      // loads of a wave's rows per stage
+    constexpr int XR = BT / kWaves, XL = (XR + LR - 1) / LR;         // tokens a wave stages, their loads
+    constexpr int L = WL + XL;
+    const int tid = threadIdx.x, lane = tid & (kLanes - 1), r = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / kLanes);
+    const int wv = wave / WB, wb = wave % WB;
+    const int nstage = dp / KC;
+
+    // this workgroup's tiles: first, first + step, .. below end
+    const int xcd = blockIdx.x % 8;
+    const int first = xcd * tiles.per_xcd + blockIdx.x / 8;
+    const int end = min((xcd + 1) * tiles.per_xcd, tiles.nv * tiles.nb);
+    if (first >= end) return;
+    auto place = [&](int t, int64_t &v0, int &b0) {
+        const int group = t / (8 * tiles.nv), in = min(8, tiles.nb - 8 * group), k = t - group * 8 * tiles.nv;
+        v0 = (int64_t)(k / in) * tiles.rows;
+        b0 = (8 * group + k % in) * BT;
+    };
+
+    const int lrow = lane / P, slot = lane % P;
+    const int8_t *wsrc[WL], *xsrc[XL];
+    int wcol[WL], xcol[XL];
+#pragma unroll
+    for (int t = 0; t < WL; ++t) wcol[t] = 16 * (slot ^ swizzle<KC>(LR * t + lrow));
+#pragma unroll
+    for (int t = 0; t < XL; ++t) xcol[t] = 16 * (slot ^ swizzle<KC>(wave * XR + LR * t + lrow));
+    auto set_tile = [&](int t) {
+        int64_t v0;
+        int b0;
+        place(t, v0, b0);
+        const int64_t vlast = min<int64_t>(V, v0 + tiles.rows) - 1;
+#pragma unroll
+        for (int i = 0; i < WL; ++i)
+            wsrc[i] = q + min<int64_t>(v0 + wave * (kTileRows / kWaves) + LR * i + lrow, vlast) * pitch;
+#pragma unroll
+        for (int i = 0; i < XL; ++i) xsrc[i] = x + (int64_t)min(b0 + wave * XR + LR * i + lrow, B - 1) * dp;
+    };
+    int lt = first, lst = 0;  // the stage to load next
+    auto load_next = [&](int buf) {
+        char *dst = smem + buf * kStage;
+        const int c = lst * KC;
+#pragma unroll
+        for (int i = 0; i < WL; ++i)
+            load_lds16(wsrc[i] + min(c + wcol[i], pitch - 16), dst + (wave * (kTileRows / kWaves) + LR * i) * KC);
+#pragma unroll
+        for (int i = 0; i < XL; ++i)
+            if (XR >= LR || lane < XR * P)
+                load_lds16(xsrc[i] + c + xcol[i], dst + (kTileRows + wave * XR + LR * i) * KC);
+        if (++lst == nstage) {  // past the last tile: its stages again, unused
+            lst = 0;
+            if (lt + tiles.step < end) lt += tiles.step;
+            set_tile(lt);
+        }
+    };
+    struct Operands {
+        word4 a[KS][MT], b[KS][NT];
+    };
+    auto read = [&](int buf, Operands &o) {
+        const char *A = smem + buf * kStage + (wv * MT * 16 + r) * KC;
+        const char *X = smem + buf * kStage + (kTileRows + wb * NT * 16 + r) * KC;
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            const int at = 16 * ((4 * k + g) ^ swizzle<KC>(r));
+#pragma unroll
+            for (int n = 0; n < NT; ++n) o.b[k][n] = *reinterpret_cast<const word4 *>(X + n * 16 * KC + at);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) o.a[k][m] = *reinterpret_cast<const word4 *>(A + m * 16 * KC + at);
+        }
+    };
+    i32x4 acc[MT][NT];
+#pragma unroll
+    for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[m][n] = i32x4{0, 0, 0, 0};
+    auto multiply = [&](const Operands &o) {
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+                    acc[m][n] = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, o.a[k][m]),
+                                                                      __builtin_bit_cast(i32x4, o.b[k][n]), acc[m][n], 0, 0, 0);
+    };
+
+    // What the logits of tile t need besides: the scales of the wave's rows
+    // (lane, lane + 64) and of its tokens.
+    constexpr int kScales = (16 * MT + kLanes - 1) / kLanes;
+    float sc[kScales], xf[NT];
+    auto load_scales = [&](int t) {
+        int64_t v0;
+        int b0;
+        place(t, v0, b0);
+#pragma unroll
+        for (int i = 0; i < kScales; ++i) sc[i] = scale[min<int64_t>(v0 + wv * MT * 16 + i * kLanes + lane, V - 1)];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) xf[n] = xs[min(b0 + (wb * NT + n) * 16 + r, B - 1)];
+    };
+    // lane (r, g) holds rows 4 g + i of row tile m for token 16 n + r
+    constexpr int kHalves = OUT_BF16 ? 1 : 2, kPer = MT / kHalves;  // a token's run: kPer row tiles
+    constexpr int kUnits = kPer * 16 / E::kVec;                      // 16-byte units of it
+    constexpr int kStores = kHalves * NT * 16 * kUnits / kLanes;
+    auto store = [&](int t) {  // whether every store of the wave was made
+        int64_t v0;
+        int b0;
+        place(t, v0, b0);
+        const int64_t vend = min<int64_t>(V, v0 + tiles.rows);
+        v0 += wv * MT * 16;
+        b0 += wb * NT * 16;
+        char *tmp = smem + NBUF * kStage + wave * 4096;
+        // (this lane's addresses are made here: kept over the stages they
+        // would take the registers that the operands need)
+        int lane = threadIdx.x & (kLanes - 1);
+        asm volatile("" : "+v"(lane));
+        const int r = lane & 15, g = lane >> 4;
+        // the scales to their lanes; the sums become logits in place
+#pragma unroll
+        for (int i = 0; i < kScales; ++i) reinterpret_cast<float *>(tmp)[i * kLanes + lane] = sc[i];
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (the wave's own writes, read by its other lanes)
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+            float f[4];
+            Elem<false>::unpack(*reinterpret_cast<const word4 *>(tmp + 64 * m + 16 * g), f);
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[m][n][i] = __float_as_int((float)acc[m][n][i] * f[i] * xf[n]);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int h = 0; h < kHalves; ++h) {
+#pragma unroll
+                for (int m = 0; m < kPer; ++m) {
+                    float f[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) f[i] = __int_as_float(acc[h * kPer + m][n][i]);
+                    if constexpr (OUT_BF16) {
+                        const uint32_t w[2] = {(uint32_t)to_bf16(f[0]) | (uint32_t)to_bf16(f[1]) << 16,
+                                               (uint32_t)to_bf16(f[2]) | (uint32_t)to_bf16(f[3]) << 16};
+                        char *p = tmp + r * (kUnits * 16) + 16 * ((2 * m + g / 2) ^ (r & (kUnits - 1))) + 8 * (g & 1);
+                        *reinterpret_cast<uint64_t *>(p) = (uint64_t)w[1] << 32 | w[0];
+                    } else {
+                        *reinterpret_cast<word4 *>(tmp + r * (kUnits * 16) + 16 * ((4 * m + g) ^ (r & (kUnits - 1)))) =
+                            Elem<false>::pack(f);
+                    }
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < 16 * kUnits / kLanes; ++i) {
+                    const int row = (i * kLanes + lane) / kUnits, unit = lane % kUnits;
+                    const word4 w = *reinterpret_cast<const word4 *>(tmp + row * (kUnits * 16) + 16 * (unit ^ (row & (kUnits - 1))));
+                    const int b = b0 + 16 * n + row;
+                    const int64_t v = v0 + h * kPer * 16 + unit * E::kVec;
+                    typename E::T *o = out + (int64_t)b * ld + v;
+                    if (b < B && v + E::kVec <= vend) {
+                        __builtin_memcpy(o, &w, 16);  // (at any alignment)
+                    } else if (b < B) {
+                        for (int e = 0; e < E::kVec && v + e < vend; ++e) {
+                            typename E::T val;
+                            __builtin_memcpy(&val, reinterpret_cast<const char *>(tmp + row * (kUnits * 16) + 16 * (unit ^ (row & (kUnits - 1)))) + e * sizeof val, sizeof val);
+                            o[e] = val;
+                        }
+                    }
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc[m][n] = i32x4{0, 0, 0, 0};
+        return v0 + MT * 16 <= vend && b0 + 16 * NT <= B;
+    };
+
+    set_tile(first);
+#pragma unroll
+    for (int i = 0; i < NBUF - !AHEAD; ++i) load_next(i);
+    int buf = 0, stored = 0, t = first, st = 0;
+    Operands now, next;
+    if constexpr (AHEAD) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NBUF - 1) * L) : "memory");
+        __builtin_amdgcn_s_barrier();
+        read(0, now);
+    }
+    auto step = [&](Operands &cur, Operands &nxt) {  // false past the last stage
+        // The stage to be read has landed, and the operands of the stage
+        // before it are read, in every wave past the barrier.  (The first
+        // stages after a tile's end were issued before its stores, which may
+        // be in flight too.)
+        __builtin_amdgcn_sched_barrier(0);
+        if (stored > 0) {
+            --stored;
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NBUF - 2) * L + kStores) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((NBUF - 2) * L) : "memory");
+        }
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        if (st == nstage - 1) load_scales(t);
+        if constexpr (AHEAD) {
+            load_next(buf);
+            buf = buf == NBUF - 1 ? 0 : buf + 1;
+            read(buf, nxt);
+        } else {
+            load_next(buf == 0 ? NBUF - 1 : buf - 1);
+            read(buf, cur);
+            buf = buf == NBUF - 1 ? 0 : buf + 1;
+        }
+        multiply(cur);
+        if (++st == nstage) {
+            stored = store(t) ? NBUF - 1 : 0;
+            st = 0;
+            t += tiles.step;
+            return t < end;
+        }
+        return true;
+    };
+    if constexpr (AHEAD)
+        while (step(now, next) && step(next, now)) {
+        }
+    else
+        while (step(now, now)) {
+        }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load into LDS outlives the workgroup
+}
+
 vie_status launched(const char *what)
 {
     const hipError_t e = hipGetLastError();
@@ -110,6 +398,42 @@ size_t tokens_bytes(int d, int B) { return ((size_t)B * padded(d) + 255) & ~(siz
 // The tokens' int8 values and scales.
 size_t int8_workspace_bytes(int64_t, int d, int B) { return tokens_bytes(d, B) + (size_t)B * 4; }
 
+namespace {
+template <int MT, int NT, int WB, int KC, int NBUF, bool AHEAD, bool OUT_BF16>
+hipError_t tile_launch(const Int8Launch &a, const int8_t *x, const float *xs, bool even, hipStream_t s)
+{
+    constexpr int BT = 16 * NT * WB, lds = tile_lds(BT, KC, NBUF);
+    static_assert(lds <= 160 * 1024, "a tile's stages fit LDS");
+    auto kern = int8_tile_kernel<MT, NT, WB, KC, NBUF, AHEAD, OUT_BF16>;
+    hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    if (e != hipSuccess) return e;
+    Tiles t;
+    t.nb = (a.B + BT - 1) / BT;
+    t.rows = kTileRows;
+    if (even) {  // every workgroup as many rows as the others, to eight
+        const int64_t rounds = (a.V + kTileRows * kWorkgroups - 1) / (kTileRows * kWorkgroups);
+        const int64_t rows = (a.V + rounds * kWorkgroups - 1) / (rounds * kWorkgroups);
+        t.rows = (int)((rows + 7) / 8 * 8);
+    }
+    t.nv = (int)((a.V + t.rows - 1) / t.rows);
+    const int64_t n = (int64_t)t.nv * t.nb;
+    t.per_xcd = (int)((n + 7) / 8);
+    t.step = std::min(kWorkgroups / 8, t.per_xcd);
+    kern<<<8 * t.step, kThreads, lds, s>>>(a.q, a.d, a.scale, a.V, x, padded(a.d), xs, a.B,
+                                           static_cast<typename Elem<OUT_BF16>::T *>(a.out), a.ld, t);
+    return hipGetLastError();
+}
+
+template <bool OUT_BF16> hipError_t tiles_launch(const Int8Launch &a, const int8_t *x, const float *xs, hipStream_t s)
+{
+    if (a.B <= 16) return tile_launch<2, 1, 1, 128, 3, true, OUT_BF16>(a, x, xs, true, s);
+    if (a.B <= 32) return tile_launch<2, 2, 1, 128, 3, true, OUT_BF16>(a, x, xs, true, s);
+    if (a.B <= 64) return tile_launch<2, 4, 1, 128, 3, true, OUT_BF16>(a, x, xs, true, s);
+    if (a.B <= 128) return tile_launch<4, 4, 2, 64, 4, true, OUT_BF16>(a, x, xs, false, s);
+    return tile_launch<8, 4, 4, 64, 4, false, OUT_BF16>(a, x, xs, false, s);
+}
+}  // namespace
+
 vie_status launch_int8_logits(const Int8Launch &a, hipStream_t s)
 {
     int8_t *x = static_cast<int8_t *>(a.ws);
@@ -118,6 +442,10 @@ vie_status launch_int8_logits(const Int8Launch &a, hipStream_t s)
     if (a.h_dtype == VIE_BF16) tokens_kernel<true><<<tg, 256, 0, s>>>(static_cast<const uint16_t *>(a.h), a.B, a.d, x, xs);
     else tokens_kernel<false><<<tg, 256, 0, s>>>(static_cast<const float *>(a.h), a.B, a.d, x, xs);
     if (vie_status e = launched("token quantization launch")) return e;
+    if (a.d % 16 == 0 && (uintptr_t)a.q % 16 == 0) {
+        const hipError_t e = a.out_dtype == VIE_BF16 ? tiles_launch<true>(a, x, xs, s) : tiles_launch<false>(a, x, xs, s);
+        return e == hipSuccess ? VIE_OK : fail(VIE_EHIP, "int8 head launch: %s", hipGetErrorString(e));
+    }
     const dim3 grid((unsigned)((a.V + 63) / 64), (unsigned)((a.B + 15) / 16));
     if (a.out_dtype == VIE_BF16)
         int8_simple_kernel<true><<<grid, 256, 0, s>>>(a.q, a.scale, a.V, a.d, x, xs, a.B, static_cast<uint16_t *>(a.out), a.ld);
