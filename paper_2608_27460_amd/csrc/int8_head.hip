@@ -33,29 +33,58 @@ __device__ __forceinline__ int quantized(float x, float scale)
     return scale == 0.0f ? 0 : (int)fminf(fmaxf(rintf(__fdiv_rn(x, scale)), -127.0f), 127.0f);
 }
 
-// The tokens' int8 values [B][padded(d)] (zero past d) and their scales: one
-// wave per token.
+// The tokens' int8 values [B][padded(d)] (zero past d) and their scales: a
+// workgroup per token, whose values it holds in registers, eight to a chunk.
+constexpr int kTokenThreads = 256;
+constexpr int kChunks = kMaxD / 8 / kTokenThreads;
+
 template <bool BF16>
-__global__ __launch_bounds__(256) void tokens_kernel(const typename Elem<BF16>::T *__restrict__ h, int B, int d,
-                                                     int8_t *__restrict__ x, float *__restrict__ xs)
+__global__ __launch_bounds__(kTokenThreads) void tokens_kernel(const typename Elem<BF16>::T *__restrict__ h, int d,
+                                                               int8_t *__restrict__ x, float *__restrict__ xs)
 {
     typedef Elem<BF16> E;
-    const int b = blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes, lane = threadIdx.x & (kLanes - 1);
-    if (b >= B) return;
+    __shared__ float s_top[kTokenThreads / kLanes];
+    const int b = blockIdx.x, tid = threadIdx.x;
     const typename E::T *row = h + (int64_t)b * d;
-    float top = 0.0f;
+    float v[kChunks][8], top = 0.0f;
     bool bad = false;
-    for (int j = lane; j < d; j += kLanes) {
-        const float v = fabsf(E::get(row[j]));
-        bad |= !(v < __builtin_inff());
-        top = fmaxf(top, v);
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const int j = (i * kTokenThreads + tid) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
+        if (j + 8 <= d) {
+            word4 w[8 / E::kVec];
+            __builtin_memcpy(w, row + j, sizeof w);  // (at any alignment)
+#pragma unroll
+            for (int k = 0; k < 8 / E::kVec; ++k) E::unpack(w[k], &v[i][k * E::kVec]);
+        } else if (j < d) {
+#pragma unroll
+            for (int e = 0; e < 7; ++e)
+                if (j + e < d) v[i][e] = E::get(row[j + e]);
+        }
     }
-    top = wave_max(top);
-    bad = __any(bad);
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            bad |= !(fabsf(v[i][e]) < __builtin_inff());
+            top = fmaxf(top, fabsf(v[i][e]));
+        }
+    top = bad ? __builtin_inff() : top;
+    top = block_reduce<kTokenThreads>(top, s_top, [](float a, float b) { return fmaxf(a, b); });
+    bad = top == __builtin_inff();
     const float scale = bad ? 0.0f : __fdiv_rn(top, 127.0f);
-    for (int j = lane; j < padded(d); j += kLanes)
-        x[(int64_t)b * padded(d) + j] = j < d ? (int8_t)quantized(E::get(row[j]), scale) : 0;
-    if (lane == 0) xs[b] = bad ? __builtin_nanf("") : scale;
+#pragma unroll
+    for (int i = 0; i < kChunks; ++i) {
+        const int j = (i * kTokenThreads + tid) * 8;
+        if (j >= padded(d)) break;
+        uint64_t w = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w |= (uint64_t)(uint8_t)quantized(v[i][e], scale) << 8 * e;
+        *reinterpret_cast<uint64_t *>(x + (int64_t)b * padded(d) + j) = w;
+    }
+    if (tid == 0) xs[b] = bad ? __builtin_nanf("") : scale;
 }
 
 // 16 int8 values from p on, as far as they lie before `end`; the bytes past
@@ -438,9 +467,8 @@ vie_status launch_int8_logits(const Int8Launch &a, hipStream_t s)
 {
     int8_t *x = static_cast<int8_t *>(a.ws);
     float *xs = reinterpret_cast<float *>(x + tokens_bytes(a.d, a.B));
-    const unsigned tg = (unsigned)((a.B + 3) / 4);
-    if (a.h_dtype == VIE_BF16) tokens_kernel<true><<<tg, 256, 0, s>>>(static_cast<const uint16_t *>(a.h), a.B, a.d, x, xs);
-    else tokens_kernel<false><<<tg, 256, 0, s>>>(static_cast<const float *>(a.h), a.B, a.d, x, xs);
+    if (a.h_dtype == VIE_BF16) tokens_kernel<true><<<a.B, kTokenThreads, 0, s>>>(static_cast<const uint16_t *>(a.h), a.d, x, xs);
+    else tokens_kernel<false><<<a.B, kTokenThreads, 0, s>>>(static_cast<const float *>(a.h), a.d, x, xs);
     if (vie_status e = launched("token quantization launch")) return e;
     if (a.d % 16 == 0 && (uintptr_t)a.q % 16 == 0) {
         const hipError_t e = a.out_dtype == VIE_BF16 ? tiles_launch<true>(a, x, xs, s) : tiles_launch<false>(a, x, xs, s);
