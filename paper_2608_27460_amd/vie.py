@@ -7,7 +7,9 @@ raises on import.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -115,6 +117,13 @@ def _torch():
 def _stream(t) -> C.c_void_p:
     torch = _torch()
     return C.c_void_p(torch.cuda.current_stream(t.device).cuda_stream)
+
+
+def _raw_stream(device) -> int:
+    """The current stream of a device, without the Stream object of _stream (1.8 us of a call)."""
+    torch = _torch()
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return raw(device.index) if raw else torch.cuda.current_stream(device).cuda_stream
 
 
 def _dtype_of_tensor(t) -> int:
@@ -377,6 +386,15 @@ def scatter(ids, logits, V: int):
 # around the head's logits: the int8 head, the token drawn, distillation
 # ---------------------------------------------------------------------------
 
+_SAME_DEVICE = contextlib.nullcontext()
+
+
+def _on(device):
+    """A context in which `device` is the current one (entering torch's costs 1.3 us, so only where it is not)."""
+    torch = _torch()
+    return _SAME_DEVICE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
 def _matrix(t, name: str):
     """Pointer, dtype code, rows, row length and row stride of a device matrix of logits."""
     if not t.is_cuda:
@@ -384,19 +402,27 @@ def _matrix(t, name: str):
     if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1):
         raise ValueError("%s must be [rows, V] with contiguous rows" % name)
     rows, V = t.shape
-    return C.c_void_p(t.data_ptr()), _dtype_of_tensor(t), rows, V, t.stride(0) if rows > 1 else V
+    return t.data_ptr(), _dtype_of_tensor(t), rows, V, t.stride(0) if rows > 1 else V
 
 
-def _values(t, name: str, dtype, shape, device):
+def _values(t, name: str, dtype, shape, device) -> int:
     """Pointer of a contiguous device tensor of this type and shape."""
-    torch = _torch()
-    if t.dtype != getattr(torch, dtype):
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.device == device and t.is_contiguous():
+        return t.data_ptr()
+    if t.dtype is not dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
-    if t.device != device:
+    if t.is_cuda and t.device != device:
         raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
-    return _dev_ptr(t, name)
+    return _dev_ptr(t, name).value
+
+
+@functools.lru_cache(maxsize=256)
+def _workspace_bytes(query: str, *sizes) -> int:
+    n = C.c_size_t()
+    _check(getattr(lib, query)(*sizes, C.byref(n)))
+    return n.value
 
 
 def _workspace(nbytes: int, device):
@@ -404,7 +430,7 @@ def _workspace(nbytes: int, device):
     if nbytes == 0:
         return None, None
     t = _torch().empty(nbytes, dtype=_torch().uint8, device=device)
-    return t, C.c_void_p(t.data_ptr())
+    return t, t.data_ptr()
 
 
 class Int8Head:
@@ -415,7 +441,7 @@ class Int8Head:
         if q.dtype != torch.int8 or q.dim() != 2:
             raise TypeError("q must be a 2-D int8 tensor")
         _dev_ptr(q, "q")
-        _values(scale, "scale", "float32", (q.shape[0],), q.device)
+        _values(scale, "scale", torch.float32, (q.shape[0],), q.device)
         self.q, self.scale = q, scale
 
     def __call__(self, h, dtype=None, out=None):
@@ -437,22 +463,21 @@ class Int8Head:
         if (rows, cols) != (B, V) or out.device != h.device:
             raise ValueError("out must be [%d, %d] on %s" % (B, V, h.device))
         hp = _dev_ptr(h, "h")
-        n = C.c_size_t()
-        _check(lib.vie_int8_logits_workspace(V, d, B, C.byref(n)))
-        with torch.cuda.device(h.device):
-            ws, wp = _workspace(n.value, h.device)
-            _check(lib.vie_int8_logits(C.c_void_p(self.q.data_ptr()), C.c_void_p(self.scale.data_ptr()), V, d, hp, hd,
-                                       B, op, od, ld, wp, n.value, _stream(h)))
+        n = _workspace_bytes("vie_int8_logits_workspace", V, d, B)
+        with _on(h.device):
+            ws, wp = _workspace(n, h.device)
+            _check(lib.vie_int8_logits(self.q.data_ptr(), self.scale.data_ptr(), V, d, hp, hd, B, op, od, ld, wp, n,
+                                       _raw_stream(h.device)))
         return out
 
 
 def _sampling(B: int, device, temperature, top_k, top_p, min_p) -> SamplingParams:
     """Each setting is a number, or a device tensor [B] (fp32; top_k int32)."""
     p = SamplingParams(1.0, 1.0, 0.0, 0)
-    for name, v, dtype in (("temperature", temperature, "float32"), ("top_k", top_k, "int32"),
-                           ("top_p", top_p, "float32"), ("min_p", min_p, "float32")):
-        if hasattr(v, "data_ptr"):
-            setattr(p, name + "_dev", _values(v, name, dtype, (B,), device))
+    torch = _torch()
+    for name, v in (("temperature", temperature), ("top_k", top_k), ("top_p", top_p), ("min_p", min_p)):
+        if isinstance(v, torch.Tensor):
+            setattr(p, name + "_dev", _values(v, name, torch.int32 if name == "top_k" else torch.float32, (B,), device))
         else:
             setattr(p, name, v)
     return p
@@ -474,13 +499,14 @@ def sample(ids, logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
     if ids.dim() != 2:
         raise ValueError("ids must be [B, k]")
     (B, k), dev = ids.shape, ids.device
-    ip = _values(ids, "ids", "int32", (B, k), dev)
-    lp = _values(logits, "logits", "float32", (B, k), dev)
-    up = _values(u, "u", "float32", (B,), dev)
+    ip = _values(ids, "ids", torch.int32, (B, k), dev)
+    lp = _values(logits, "logits", torch.float32, (B, k), dev)
+    up = _values(u, "u", torch.float32, (B,), dev)
     prm = _sampling(B, dev, temperature, top_k, top_p, min_p)
-    with torch.cuda.device(dev):
-        out = _drawn(B, dev)
-        _check(lib.vie_sample(ip, lp, B, k, C.byref(prm), up, *(C.c_void_p(t.data_ptr()) for t in out), _stream(ids)))
+    with _on(dev):
+        tok, prob, kept = out = _drawn(B, dev)
+        _check(lib.vie_sample(ip, lp, B, k, C.byref(prm), up, tok.data_ptr(), prob.data_ptr(), kept.data_ptr(),
+                              _raw_stream(dev)))
     return out
 
 
@@ -491,25 +517,26 @@ def sample_rows(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
         logits = logits.unsqueeze(0)
     lp, dt, B, V, ld = _matrix(logits, "logits")
     dev = logits.device
-    up = _values(u, "u", "float32", (B,), dev)
+    up = _values(u, "u", torch.float32, (B,), dev)
     prm = _sampling(B, dev, temperature, top_k, top_p, min_p)
-    n = C.c_size_t()
-    _check(lib.vie_sample_rows_workspace(V, B, C.byref(n)))
-    with torch.cuda.device(dev):
-        out = _drawn(B, dev)
-        ws, wp = _workspace(n.value, dev)
-        _check(lib.vie_sample_rows(lp, dt, V, ld, B, C.byref(prm), up, *(C.c_void_p(t.data_ptr()) for t in out), wp,
-                                   n.value, _stream(logits)))
+    n = _workspace_bytes("vie_sample_rows_workspace", V, B)
+    with _on(dev):
+        tok, prob, kept = out = _drawn(B, dev)
+        ws, wp = _workspace(n, dev)
+        _check(lib.vie_sample_rows(lp, dt, V, ld, B, C.byref(prm), up, tok.data_ptr(), prob.data_ptr(),
+                                   kept.data_ptr(), wp, n, _raw_stream(dev)))
     return out
 
 
 def _distill_inputs(logits, ids, teacher):
+    torch = _torch()
     m = _matrix(logits, "logits")
     N = m[2]
     if ids.dim() != 2:
         raise ValueError("ids must be [N, k]")
     k = ids.shape[1]
-    return m, _values(ids, "ids", "int32", (N, k), logits.device), _values(teacher, "teacher", "float32", (N, k), logits.device), k
+    return (m, _values(ids, "ids", torch.int32, (N, k), logits.device),
+            _values(teacher, "teacher", torch.float32, (N, k), logits.device), k)
 
 
 def _grad_of(logits, gloss, out):
@@ -521,7 +548,7 @@ def _grad_of(logits, gloss, out):
     gp, gd, rows, cols, ld = _matrix(out, "out")
     if (rows, cols) != (N, V) or out.dtype != logits.dtype or out.device != logits.device:
         raise ValueError("out must be like logits")
-    return out, gp, ld, None if gloss is None else _values(gloss, "gloss", "float32", (N,), logits.device)
+    return out, gp, ld, None if gloss is None else _values(gloss, "gloss", torch.float32, (N,), logits.device)
 
 
 def distill(logits, ids, teacher, tau: float = 1.0):
@@ -530,14 +557,13 @@ def distill(logits, ids, teacher, tau: float = 1.0):
     logits at the temperature tau (vie_distill); stats goes to distill_grad."""
     torch = _torch()
     (lp, dt, N, V, ld), ip, tp, k = _distill_inputs(logits, ids, teacher)
-    n = C.c_size_t()
-    _check(lib.vie_distill_workspace(V, N, C.byref(n)))
-    with torch.cuda.device(logits.device):
+    n = _workspace_bytes("vie_distill_workspace", V, N)
+    with _on(logits.device):
         loss = torch.empty(N, dtype=torch.float32, device=logits.device)
         stats = torch.empty((N, 2), dtype=torch.float32, device=logits.device)
-        ws, wp = _workspace(n.value, logits.device)
-        _check(lib.vie_distill(lp, dt, N, V, ld, ip, tp, k, tau, C.c_void_p(loss.data_ptr()),
-                               C.c_void_p(stats.data_ptr()), wp, n.value, _stream(logits)))
+        ws, wp = _workspace(n, logits.device)
+        _check(lib.vie_distill(lp, dt, N, V, ld, ip, tp, k, tau, loss.data_ptr(), stats.data_ptr(), wp, n,
+                               _raw_stream(logits.device)))
     return loss, stats
 
 
@@ -546,10 +572,11 @@ def distill_grad(logits, ids, teacher, stats, tau: float = 1.0, gloss=None, weig
     in the logits, in their type; out may be logits itself (vie_distill_grad)."""
     torch = _torch()
     (lp, dt, N, V, ld), ip, tp, k = _distill_inputs(logits, ids, teacher)
-    sp = _values(stats, "stats", "float32", (N, 2), logits.device)
-    with torch.cuda.device(logits.device):
+    sp = _values(stats, "stats", torch.float32, (N, 2), logits.device)
+    with _on(logits.device):
         out, gp, gld, glp = _grad_of(logits, gloss, out)
-        _check(lib.vie_distill_grad(lp, dt, N, V, ld, ip, tp, k, tau, sp, glp, weight, gp, gld, _stream(logits)))
+        _check(lib.vie_distill_grad(lp, dt, N, V, ld, ip, tp, k, tau, sp, glp, weight, gp, gld,
+                                    _raw_stream(logits.device)))
     return out
 
 
@@ -557,12 +584,11 @@ def distill_step(logits, ids, teacher, tau: float = 1.0, gloss=None, weight: flo
     """(loss, gradient): distill and distill_grad at once (vie_distill_step)."""
     torch = _torch()
     (lp, dt, N, V, ld), ip, tp, k = _distill_inputs(logits, ids, teacher)
-    n = C.c_size_t()
-    _check(lib.vie_distill_workspace(V, N, C.byref(n)))
-    with torch.cuda.device(logits.device):
+    n = _workspace_bytes("vie_distill_workspace", V, N)
+    with _on(logits.device):
         loss = torch.empty(N, dtype=torch.float32, device=logits.device)
         out, gp, gld, glp = _grad_of(logits, gloss, out)
-        ws, wp = _workspace(n.value, logits.device)
-        _check(lib.vie_distill_step(lp, dt, N, V, ld, ip, tp, k, tau, glp, weight, C.c_void_p(loss.data_ptr()), gp, gld,
-                                    wp, n.value, _stream(logits)))
+        ws, wp = _workspace(n, logits.device)
+        _check(lib.vie_distill_step(lp, dt, N, V, ld, ip, tp, k, tau, glp, weight, loss.data_ptr(), gp, gld, wp, n,
+                                    _raw_stream(logits.device)))
     return loss, out
