@@ -16,6 +16,7 @@
 // terms) and merged pairwise; the list's sums are fp64.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cfloat>
 
 #include "block.hpp"
@@ -25,231 +26,487 @@ namespace vie {
 
 namespace {
 
-constexpr int kRowThreads = 512;
-constexpr int kRowWaves = kRowThreads / kLanes;
-constexpr int kListPer = kMaxList / kRowThreads;  // list entries of a thread
-static_assert(kListPer * kRowThreads == kMaxList, "every list entry has a thread");
-
 // Maximum and sum of exp2((s - m) c) of a set of logits.  The empty set has
 // the lowest finite maximum, so that rows of -inf or of the lowest value make
 // no NaN on the way: s - m is then 0 or -inf.
 struct Part {
     float m, z;
 };
+__device__ __forceinline__ float term(float s, float m, float c) { return __builtin_amdgcn_exp2f((s - m) * c); }
 __device__ __forceinline__ Part merge(Part a, Part b, float c)
 {
     const float m = fmaxf(a.m, b.m);
-    return {m, a.z * exp2f((a.m - m) * c) + b.z * exp2f((b.m - m) * c)};
+    return {m, a.z * term(a.m, m, c) + b.z * term(b.m, m, c)};
 }
 template <int N> __device__ __forceinline__ void add(Part &p, const float *f, float c)
 {
-    float m = f[0];
+    float m = p.m;
 #pragma unroll
-    for (int i = 1; i < N; ++i) m = fmaxf(m, f[i]);
-    m = fmaxf(m, p.m);
-    float z = p.z * exp2f((p.m - m) * c);
+    for (int i = 0; i < N; ++i) m = fmaxf(m, f[i]);
+    float z = p.z * term(p.m, m, c);
 #pragma unroll
-    for (int i = 0; i < N; ++i) z += exp2f((f[i] - m) * c);
+    for (int i = 0; i < N; ++i) z += term(f[i], m, c);
     p = {m, z};
 }
-
-// The part of n logits from s on, in every thread.
-template <bool BF16> __device__ Part row_part(const typename Elem<BF16>::T *s, int64_t n, float c, Part *tmp)
+// The whole workgroup's part, in every thread; `tmp`: NT / 64 parts.
+template <int NT> __device__ __forceinline__ Part block_merge(Part p, float c, Part *tmp)
 {
-    typedef Elem<BF16> E;
-    const Span<typename E::T> sp(s, n);
-    Part p{-FLT_MAX, 0.0f};
-    const word4 *v = reinterpret_cast<const word4 *>(s + sp.head);
-    for (int64_t i = threadIdx.x; i < sp.vecs; i += kRowThreads) {
-        float f[E::kVec];
-        E::unpack(v[i], f);
-        add<E::kVec>(p, f, c);
-    }
-    for (int64_t i = threadIdx.x; i < sp.head + n - sp.tail0; i += kRowThreads) {
-        const float f = E::get(s[i < sp.head ? i : sp.tail0 + i - sp.head]);
-        add<1>(p, &f, c);
-    }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) p = merge(p, Part{__shfl_xor(p.m, o, kLanes), __shfl_xor(p.z, o, kLanes)}, c);
     __syncthreads();
     if ((threadIdx.x & (kLanes - 1)) == 0) tmp[threadIdx.x / kLanes] = p;
     __syncthreads();
-    p = tmp[0];
+    p = tmp[threadIdx.x & (NT / kLanes - 1)];  // lanes past the waves repeat them: the exchanges stay among NT / 64
 #pragma unroll
-    for (int w = 1; w < kRowWaves; ++w) p = merge(p, tmp[w], c);
+    for (int o = NT / kLanes / 2; o >= 1; o >>= 1)
+        p = merge(p, Part{__shfl_xor(p.m, o, kLanes), __shfl_xor(p.z, o, kLanes)}, c);
     return p;
 }
 
-// The teacher's list of a row: this thread's entries, and the list's maximum
-// and sum.  An entry counts if its id lies in [0, V) and its logit is not
-// -inf; the others have id -1.
-struct List {
-    int32_t id[kListPer];
-    float t[kListPer];
+// 16 bytes at any alignment of the elements
+template <typename T> __device__ __forceinline__ word4 load_vec(const T *p)
+{
+    word4 w;
+    __builtin_memcpy(&w, p, 16);
+    return w;
+}
+template <typename T> __device__ __forceinline__ void store_vec(T *p, word4 w) { __builtin_memcpy(p, &w, 16); }
+
+// The teacher's list of a row, in LDS: 16 bytes an entry.  An entry counts if
+// its id lies in [0, V) and its logit is not -inf; the others have id -1.
+// Entry j belongs to thread j % NT in every step, so the steps need no
+// barrier; its fp64 work is one entry at a time, whose registers the rows'
+// kernels could not spare for more.
+struct Entry {
+    int32_t id;
+    float t, at;  // the teacher's logit, the student's at that id
+    float e;      // exp((t - top) / tau)
+};
+template <int NT> struct List {
+    Entry *entry;
+    int k;
     float top;
     double total;  // 0: nothing listed
     double inv_tau;
-    __device__ __forceinline__ double x(int i) const { return ((double)t[i] - (double)top) * inv_tau; }
-    __device__ __forceinline__ double p(int i) const { return exp(x(i)) / total; }
+
+    static __device__ __forceinline__ Entry get(const int32_t *ids, const float *teacher, int j, int k, int64_t V)
+    {
+        Entry x{-1, 0.0f, 0.0f, 0.0f};
+        if (j < k) {
+            x.id = ids[j];
+            x.t = teacher[j];
+            if (x.id >= V || x.t == -__builtin_inff()) x.id = -1;
+        }
+        return x;
+    }
+    // `s` (of BF16 elements) nullptr: without the student's logits
+    template <bool BF16>
+    __device__ __forceinline__ void read(const int32_t *ids, const float *teacher, int64_t V, const typename Elem<BF16>::T *s)
+    {
+        for (int j = threadIdx.x; j < k; j += NT) {
+            Entry x = get(ids, teacher, j, k, V);
+            if (s && x.id >= 0) x.at = Elem<BF16>::get(s[x.id]);
+            entry[j] = x;
+        }
+    }
+    // the list's maximum and sum (the workgroup waits in here)
+    __device__ __forceinline__ void sum(float tau, double *tmp)
+    {
+        inv_tau = 1.0 / (double)tau;
+        float m = -FLT_MAX;
+        for (int j = threadIdx.x; j < k; j += NT) {
+            const float t = entry[j].t;
+            if (entry[j].id >= 0) m = m != m || t != t ? m + t : fmaxf(m, t);
+        }
+        top = block_reduce<NT>(m, reinterpret_cast<float *>(tmp),
+                               [](float a, float b) { return a != a || b != b ? a + b : fmaxf(a, b); });
+        double z = 0.0;
+#pragma unroll 1
+        for (int j = threadIdx.x; j < k; j += NT) {
+            const double e = entry[j].id >= 0 ? exp(x(j)) : 0.0;
+            entry[j].e = (float)e;
+            z += e;
+        }
+        total = block_reduce<NT>(z, tmp + NT / kLanes, [](double a, double b) { return a + b; });
+    }
+    __device__ __forceinline__ double x(int j) const { return ((double)entry[j].t - (double)top) * inv_tau; }
+    __device__ __forceinline__ double p(int j) const { return (double)entry[j].e / total; }
+
+    // The row's loss from its part and the student's logits, in every thread.
+    __device__ __forceinline__ float loss(Part r, float tau, double *tmp) const
+    {
+        double sum = 0.0;
+        if ((int)threadIdx.x < k) {
+            // log p - log q: the logarithms of the two sums together
+            const double log_ratio = log((double)r.z / total);
+#pragma unroll 1
+            for (int j = threadIdx.x; j < k; j += NT) {
+                if (entry[j].id < 0 || entry[j].e == 0.0f) continue;
+                sum += p(j) * (x(j) - ((double)entry[j].at - (double)r.m) * inv_tau + log_ratio);
+            }
+        }
+        sum = block_reduce<NT>(sum, tmp, [](double a, double b) { return a + b; });
+        return total == 0.0 ? 0.0f : (float)((double)tau * (double)tau * sum);
+    }
 };
 
-__device__ __forceinline__ void read_list(List &l, const int32_t *ids, const float *t, int k, int64_t V, float tau,
-                                          double *tmp)
-{
-    l.inv_tau = 1.0 / (double)tau;
-    float top = -FLT_MAX;
-    bool nan = false;
-#pragma unroll
-    for (int i = 0; i < kListPer; ++i) {
-        const int j = i * kRowThreads + threadIdx.x;
-        l.id[i] = -1;
-        l.t[i] = 0.0f;
-        if (j >= k) continue;
-        const int32_t id = ids[j];
-        const float v = t[j];
-        if (id < 0 || id >= V || v == -__builtin_inff()) continue;
-        l.id[i] = id;
-        l.t[i] = v;
-        nan |= v != v;
-        top = fmaxf(top, v);
+// The list's probabilities by id, for the ids of [v0, v0 + n): a hash table
+// of 2^bits places, at least twice the entries, and a bit for every 16 bytes
+// of logits that hold a listed id.
+constexpr int kMapWords = 1024;  // for up to 32768 groups of 16 bytes
+struct Table {
+    uint32_t *map;
+    int32_t *id;
+    float *prob;
+    int bits;
+    __device__ __forceinline__ Table(char *lds, int bits)
+        : map(reinterpret_cast<uint32_t *>(lds)), id(reinterpret_cast<int32_t *>(lds + kMapWords * 4)),
+          prob(reinterpret_cast<float *>(lds + kMapWords * 4 + (4 << bits))), bits(bits)
+    {
     }
-    top = nan ? __builtin_nanf("") : top;
-    l.top = block_reduce<kRowThreads>(top, reinterpret_cast<float *>(tmp),
-                                      [](float a, float b) { return a != a || b != b ? a + b : fmaxf(a, b); });
-    double total = 0.0;
-#pragma unroll
-    for (int i = 0; i < kListPer; ++i)
-        if (l.id[i] >= 0) total += exp(l.x(i));
-    __syncthreads();
-    l.total = block_reduce<kRowThreads>(total, tmp, [](double a, double b) { return a + b; });
-}
-
-// The loss of a row from its part and its list (in every thread).
-template <bool BF16>
-__device__ __forceinline__ float row_loss(const List &l, const typename Elem<BF16>::T *s, Part r, float tau, double *tmp)
-{
-    double sum = 0.0;
-    const double log_total = log(l.total), log_z = log((double)r.z);
-#pragma unroll
-    for (int i = 0; i < kListPer; ++i) {
-        if (l.id[i] < 0) continue;
-        const double p = l.p(i);
-        if (p == 0.0) continue;
-        const double logq = ((double)Elem<BF16>::get(s[l.id[i]]) - (double)r.m) * l.inv_tau - log_z;
-        sum += p * (l.x(i) - log_total - logq);
+    __device__ __forceinline__ uint32_t place(int32_t v) const { return (uint32_t)v * 2654435761u >> (32 - bits); }
+    template <int NT> __device__ __forceinline__ void clear()
+    {
+        for (int i = threadIdx.x; i < kMapWords; i += NT) map[i] = 0;
+        for (int i = threadIdx.x; i < 1 << bits; i += NT) id[i] = -1;
     }
-    __syncthreads();
-    sum = block_reduce<kRowThreads>(sum, tmp, [](double a, double b) { return a + b; });
-    return l.total == 0.0 ? 0.0f : (float)((double)tau * (double)tau * sum);
+    // (between clear and fill the workgroup waits; in fill it does so itself)
+    template <int NT> __device__ __forceinline__ void fill(const List<NT> &l, int64_t v0, int64_t n, int vec)
+    {
+        bool twice = false;
+#pragma unroll 1
+        for (int j = threadIdx.x; j < l.k; j += NT) {
+            const int32_t v = l.entry[j].id;
+            const int64_t off = (int64_t)v - v0;
+            if (v < 0 || off < 0 || off >= n) continue;
+            uint32_t h = place(v);
+            int32_t was;
+            while ((was = atomicCAS(&id[h], -1, v)) != -1 && was != v) h = (h + 1) & ((1u << bits) - 1);
+            twice |= was == v;
+            prob[h] = (float)l.p(j);
+            const uint32_t g = (uint32_t)off / vec;
+            atomicOr(&map[g / 32], 1u << (g % 32));
+        }
+        if (!__syncthreads_or(twice)) return;
+        // Ids listed more than once (no list of a head's): their first entry
+        // adds up all of them, in the list's order.
+#pragma unroll 1
+        for (int j = threadIdx.x; j < l.k; j += NT) {
+            const int32_t v = l.entry[j].id;
+            const int64_t off = (int64_t)v - v0;
+            if (v < 0 || off < 0 || off >= n) continue;
+            bool first = true;
+            double p = 0.0;
+            for (int e = 0; e < l.k; ++e) {
+                if (l.entry[e].id != v) continue;
+                first &= e >= j;
+                p += l.p(e);
+            }
+            if (!first) continue;
+            uint32_t h = place(v);
+            while (id[h] != v) h = (h + 1) & ((1u << bits) - 1);
+            prob[h] = (float)p;
+        }
+        __syncthreads();
+    }
+    __device__ __forceinline__ bool any(uint32_t group) const { return map[group / 32] >> (group % 32) & 1; }
+    __device__ __forceinline__ float p(int32_t v) const
+    {
+        for (uint32_t h = place(v);; h = (h + 1) & ((1u << bits) - 1)) {
+            if (id[h] == v) return prob[h];
+            if (id[h] == -1) return 0.0f;
+        }
+    }
+};
+__host__ __device__ inline int table_bits(int k)
+{
+    int b = 6;
+    while ((1 << b) < 2 * k) ++b;
+    return b;
 }
+__host__ __device__ inline size_t list_lds(int k) { return (size_t)k * sizeof(Entry); }
+inline size_t table_lds(int k) { return kMapWords * 4 + ((size_t)8 << table_bits(k)) + list_lds(k); }  // and the list
 
-// The gradient of n logits from v0 on: f = g tau, the row's part r.  `grad`
-// may be `s`: what the listed ids need of s is read before anything is
-// written.
+// The gradient of a row, value by value: f (q - p); of a row that lists
+// nothing 0, whatever its logits.
+struct Slope {
+    Part r;
+    float c, inv, f;
+    bool none;
+    __device__ __forceinline__ Slope(Part r, float c, float f, bool none) : r(r), c(c), inv(1.0f / r.z), f(f), none(none) {}
+    __device__ __forceinline__ float at(float s) const { return f * (term(s, r.m, c) * inv); }
+    __device__ __forceinline__ float at(float s, float p) const { return f * (term(s, r.m, c) * inv - p); }
+};
+// Element e of 16 bytes.
+template <bool BF16> __device__ __forceinline__ float element(word4 w, int e)
+{
+    const int k = BF16 ? e >> 1 : e;
+    const uint32_t word = k == 0 ? w.x : k == 1 ? w.y : k == 2 ? w.z : w.w;
+    return BF16 ? __uint_as_float(e & 1 ? word & 0xFFFF0000u : word << 16) : __uint_as_float(word);
+}
+// The gradient of a group of 16 bytes, from v on; the listed ids' values are
+// written over by the same thread.
 template <bool BF16>
-__device__ void row_grad(const List &l, const typename Elem<BF16>::T *s, typename Elem<BF16>::T *grad, int64_t v0,
-                         int64_t n, Part r, float c, float f, int32_t *s_id, float *s_p)
+__device__ __forceinline__ void put_group(const Slope &g, const Table &t, uint32_t group, int32_t v, word4 w,
+                                          typename Elem<BF16>::T *dst)
 {
     typedef Elem<BF16> E;
-    const int tid = threadIdx.x;
-    const float inv = 1.0f / r.z;
-    const bool none = l.total == 0.0;
-    if (none) f = 0.0f;
-    // listed ids: q - p, p summed over the entries of an id; its first entry writes it
-#pragma unroll
-    for (int i = 0; i < kListPer; ++i) {
-        const int j = i * kRowThreads + tid;
-        s_id[j] = l.id[i];
-        s_p[j] = l.id[i] >= 0 ? (float)l.p(i) : 0.0f;
+    if (g.none) {
+        store_vec(dst, word4{0, 0, 0, 0});
+        return;
     }
-    __syncthreads();
-    float val[kListPer];
-    bool mine[kListPer];
+    float x[E::kVec];
+    E::unpack(w, x);
 #pragma unroll
-    for (int i = 0; i < kListPer; ++i) {
-        const int j = i * kRowThreads + tid;
-        const int32_t id = l.id[i];
-        mine[i] = id >= v0 && id < v0 + n;
-        val[i] = 0.0f;
-        if (!mine[i]) continue;
-        double p = 0.0;  // (2048 fp32 additions would lose four digits)
-        for (int e = 0; e < kMaxList; ++e) {
-            if (s_id[e] != id) continue;
-            if (e < j) mine[i] = false;
-            p += (double)s_p[e];
-        }
-        val[i] = f * (exp2f((E::get(s[id]) - r.m) * c) * inv - (float)p);
-    }
-    __syncthreads();
-    auto one = [&](float x) { return none ? 0.0f : f * (exp2f((x - r.m) * c) * inv); };
-    const typename E::T *src = s + v0;
-    typename E::T *dst = grad + v0;
-    const Span<typename E::T> sp(src, n);
-    const word4 *v = reinterpret_cast<const word4 *>(src + sp.head);
-    const bool alike = (((uintptr_t)src ^ (uintptr_t)dst) & 15) == 0;
-    for (int64_t i = tid; i < sp.vecs; i += kRowThreads) {
-        float x[E::kVec];
-        E::unpack(v[i], x);
-#pragma unroll
-        for (int e = 0; e < E::kVec; ++e) x[e] = one(x[e]);
-        if (alike) {
-            reinterpret_cast<word4 *>(dst + sp.head)[i] = E::pack(x);
-        } else {
-#pragma unroll
-            for (int e = 0; e < E::kVec; ++e) dst[sp.head + i * E::kVec + e] = E::put(x[e]);
+    for (int e = 0; e < E::kVec; ++e) x[e] = g.at(x[e]);
+    store_vec(dst, E::pack(x));
+    if (t.any(group)) {
+#pragma unroll 1
+        for (int e = 0; e < E::kVec; ++e) {
+            const float p = t.p(v + e);
+            if (p != 0.0f) dst[e] = E::put(g.at(element<BF16>(w, e), p));
         }
     }
-    for (int64_t i = tid; i < sp.head + n - sp.tail0; i += kRowThreads) {
-        const int64_t at = i < sp.head ? i : sp.tail0 + i - sp.head;
-        dst[at] = E::put(one(E::get(src[at])));
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kListPer; ++i)
-        if (mine[i]) grad[l.id[i]] = E::put(val[i]);
+}
+template <bool BF16>
+__device__ __forceinline__ void put_one(const Slope &g, const Table &t, uint32_t group, int32_t v, float x,
+                                        typename Elem<BF16>::T *dst)
+{
+    *dst = Elem<BF16>::put(g.none ? 0.0f : g.at(x, t.any(group) ? t.p(v) : 0.0f));
 }
 
-// One workgroup per row: the loss and the row's part, and where GRAD the
-// gradient too, whose pass over the row follows at once.
-template <bool BF16, bool GRAD> __global__ __launch_bounds__(kRowThreads) void distill_row_kernel(DistillLaunch a)
+__device__ __forceinline__ float exponent_scale(float tau) { return (float)(1.4426950408889634 / (double)tau); }
+
+// ---------------------------------------------------------------------------
+// forward and backward apart: rows in parts, streamed
+// ---------------------------------------------------------------------------
+
+constexpr int kThreads = 512;
+constexpr int kWaves = kThreads / kLanes;
+constexpr int kFlight = 4;                       // 16-byte loads of a thread in flight
+constexpr int kMaxParts = 64;                    // of a row
+constexpr int kPartGroups = 32 * kMapWords;      // 16-byte groups of a part, at most
+
+template <bool BF16> __global__ __launch_bounds__(kThreads) void distill_forward_kernel(DistillLaunch a, int64_t len)
 {
-    typedef typename Elem<BF16>::T T;
-    __shared__ double s_tmp[kRowWaves];
-    __shared__ Part s_part[kRowWaves];
-    __shared__ int32_t s_id[GRAD ? kMaxList : 1];
-    __shared__ float s_p[GRAD ? kMaxList : 1];
+    typedef Elem<BF16> E;
+    extern __shared__ __align__(16) char smem[];
+    __shared__ double s_tmp[2 * kWaves];
+    __shared__ Part s_part[kWaves];
+    const int64_t row = blockIdx.y + (int64_t)blockIdx.z * 32768;
+    if (row >= a.N) return;
+    const int tid = threadIdx.x;
+    const typename E::T *s = static_cast<const typename E::T *>(a.logits) + row * a.ld;
+    const float c = exponent_scale(a.tau);
+    const int64_t v0 = blockIdx.x * len, n = min(len, a.V - v0), groups = n / E::kVec;
+    Part p{-FLT_MAX, 0.0f};
+    const typename E::T *src = s + v0;
+    int64_t i = tid;
+    for (; i + (kFlight - 1) * kThreads < groups; i += kFlight * kThreads) {
+        word4 w[kFlight];
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) w[u] = load_vec(src + (i + u * kThreads) * E::kVec);
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) {
+            float f[E::kVec];
+            E::unpack(w[u], f);
+            add<E::kVec>(p, f, c);
+        }
+    }
+    for (; i < groups; i += kThreads) {
+        float f[E::kVec];
+        E::unpack(load_vec(src + i * E::kVec), f);
+        add<E::kVec>(p, f, c);
+    }
+    if (groups * E::kVec + tid < n) {
+        const float f = E::get(src[groups * E::kVec + tid]);
+        add<1>(p, &f, c);
+    }
+    p = block_merge<kThreads>(p, c, s_part);
+    if (gridDim.x > 1) {
+        if (tid == 0) static_cast<Part *>(a.ws)[row * kMaxParts + blockIdx.x] = p;
+        return;
+    }
+    List<kThreads> l{reinterpret_cast<Entry *>(smem), a.k};
+    l.template read<BF16>(a.ids + row * a.k, a.teacher + row * a.k, a.V, s);
+    l.sum(a.tau, s_tmp);
+    const float loss = l.loss(p, a.tau, s_tmp);
+    if (tid == 0) {
+        a.loss[row] = loss;
+        a.stats[2 * row] = p.m;
+        a.stats[2 * row + 1] = p.z;
+    }
+}
+
+// The losses of rows that were taken in parts.
+template <bool BF16> __global__ __launch_bounds__(kThreads) void distill_join_kernel(DistillLaunch a, int parts)
+{
+    extern __shared__ __align__(16) char smem[];
+    __shared__ double s_tmp[2 * kWaves];
     const int64_t row = blockIdx.x;
-    const T *s = static_cast<const T *>(a.logits) + row * a.ld;
-    const float c = (float)(1.4426950408889634 / (double)a.tau);
-    List l;
-    read_list(l, a.ids + row * a.k, a.teacher + row * a.k, a.k, a.V, a.tau, s_tmp);
-    const Part r = row_part<BF16>(s, a.V, c, s_part);
-    const float loss = row_loss<BF16>(l, s, r, a.tau, s_tmp);
+    const float c = exponent_scale(a.tau);
+    List<kThreads> l{reinterpret_cast<Entry *>(smem), a.k};
+    l.template read<BF16>(a.ids + row * a.k, a.teacher + row * a.k, a.V,
+                          static_cast<const typename Elem<BF16>::T *>(a.logits) + row * a.ld);
+    const int lane = threadIdx.x & (kLanes - 1);
+    Part p{-FLT_MAX, 0.0f};
+    if (lane < parts) p = static_cast<const Part *>(a.ws)[row * kMaxParts + lane];
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) p = merge(p, Part{__shfl_xor(p.m, o, kLanes), __shfl_xor(p.z, o, kLanes)}, c);
+    l.sum(a.tau, s_tmp);
+    const float loss = l.loss(p, a.tau, s_tmp);
     if (threadIdx.x == 0) {
         a.loss[row] = loss;
-        if (a.stats) a.stats[2 * row] = r.m, a.stats[2 * row + 1] = r.z;
-    }
-    if constexpr (GRAD) {
-        const float g = a.weight * (a.gloss ? a.gloss[row] : 1.0f);
-        row_grad<BF16>(l, s, static_cast<T *>(a.grad) + row * a.grad_ld, 0, a.V, r, c, g * a.tau, s_id, s_p);
+        a.stats[2 * row] = p.m;
+        a.stats[2 * row + 1] = p.z;
     }
 }
 
-// The gradient from the part that the forward pass kept.
-template <bool BF16> __global__ __launch_bounds__(kRowThreads) void distill_grad_kernel(DistillLaunch a)
+template <bool BF16> __global__ __launch_bounds__(kThreads) void distill_backward_kernel(DistillLaunch a, int64_t len)
 {
-    typedef typename Elem<BF16>::T T;
-    __shared__ double s_tmp[kRowWaves];
-    __shared__ int32_t s_id[kMaxList];
-    __shared__ float s_p[kMaxList];
-    const int64_t row = blockIdx.x;
-    const float c = (float)(1.4426950408889634 / (double)a.tau);
-    List l;
-    read_list(l, a.ids + row * a.k, a.teacher + row * a.k, a.k, a.V, a.tau, s_tmp);
-    const Part r{a.stats[2 * row], a.stats[2 * row + 1]};
+    typedef Elem<BF16> E;
+    extern __shared__ __align__(16) char smem[];
+    __shared__ double s_tmp[2 * kWaves];
+    const int64_t row = blockIdx.y + (int64_t)blockIdx.z * 32768;
+    if (row >= a.N) return;
+    const int tid = threadIdx.x;
+    const int64_t v0 = blockIdx.x * len, n = min(len, a.V - v0), groups = n / E::kVec;
+    const typename E::T *src = static_cast<const typename E::T *>(a.logits) + row * a.ld + v0;
+    typename E::T *dst = static_cast<typename E::T *>(a.grad) + row * a.grad_ld + v0;
+    List<kThreads> l{reinterpret_cast<Entry *>(smem), a.k};
+    Table t(smem + list_lds(a.k), table_bits(a.k));
+    t.clear<kThreads>();
+    l.template read<BF16>(a.ids + row * a.k, a.teacher + row * a.k, a.V, nullptr);
+    l.sum(a.tau, s_tmp);  // (the workgroup waits in here)
+    t.fill(l, v0, n, E::kVec);
     const float g = a.weight * (a.gloss ? a.gloss[row] : 1.0f);
-    row_grad<BF16>(l, static_cast<const T *>(a.logits) + row * a.ld, static_cast<T *>(a.grad) + row * a.grad_ld, 0, a.V,
-                   r, c, g * a.tau, s_id, s_p);
+    const Slope sl({a.stats[2 * row], a.stats[2 * row + 1]}, exponent_scale(a.tau), g * a.tau, l.total == 0.0);
+    __syncthreads();
+    int64_t i = tid;
+    for (; i + (kFlight - 1) * kThreads < groups; i += kFlight * kThreads) {
+        word4 w[kFlight];
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) w[u] = load_vec(src + (i + u * kThreads) * E::kVec);
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) {
+            const int64_t at = i + u * kThreads;
+            put_group<BF16>(sl, t, (uint32_t)at, (int32_t)(v0 + at * E::kVec), w[u], dst + at * E::kVec);
+        }
+    }
+    for (; i < groups; i += kThreads) {
+        put_group<BF16>(sl, t, (uint32_t)i, (int32_t)(v0 + i * E::kVec), load_vec(src + i * E::kVec), dst + i * E::kVec);
+    }
+    if (groups * E::kVec + tid < n) {
+        const int64_t at = groups * E::kVec + tid;
+        put_one<BF16>(sl, t, (uint32_t)groups, (int32_t)(v0 + at), E::get(src[at]), dst + at);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// both at once: a row held in registers
+// ---------------------------------------------------------------------------
+//
+// A workgroup of 1024 threads holds a row, CHUNKS groups of 16 bytes a
+// thread, so that it is read from memory once: the row's part is taken from
+// the registers, and as the gradient of a group leaves, the next row's group
+// is loaded in its place, so that reads and writes go on together.  The list
+// of the next row and the logits at its ids are read a row ahead too.
+
+constexpr int kHeldThreads = 1024;
+constexpr int kHeldWaves = kHeldThreads / kLanes;
+
+template <bool BF16, int CHUNKS>
+__global__ __launch_bounds__(kHeldThreads) void distill_step_kernel(DistillLaunch a)
+{
+    typedef Elem<BF16> E;
+    typedef typename E::T T;
+    constexpr int kVec = E::kVec;
+    extern __shared__ __align__(16) char smem[];
+    __shared__ double s_tmp[2 * kHeldWaves];
+    __shared__ Part s_part[kHeldWaves];
+    const int tid = threadIdx.x;
+    const float c = exponent_scale(a.tau);
+    const int groups = (int)(a.V / kVec), rest = (int)(a.V - (int64_t)groups * kVec);
+    const T *logits = static_cast<const T *>(a.logits);
+    typedef List<kHeldThreads> TheList;
+    TheList l{reinterpret_cast<Entry *>(smem), a.k};
+    Table t(smem + list_lds(a.k), table_bits(a.k));
+    constexpr int kPer = kMaxList / kHeldThreads;
+    static_assert(kPer * kHeldThreads == kMaxList, "every list entry has a thread");
+    word4 w[CHUNKS];
+    float tail = 0.0f;
+    Entry ahead[kPer];
+    // (This thread's places are made anew in every pass: kept over the rows
+    // they would take the registers that hold the row.)
+    auto self = [&] {
+        int x = tid;
+        asm volatile("" : "+v"(x));
+        return x;
+    };
+    auto load = [&](const T *s, int group, int i) {
+        if (group < groups) w[i] = load_vec(s + (uint32_t)(group * kVec));
+    };
+    auto load_tail = [&](const T *s) {
+        if (tid < rest) tail = E::get(s[(int64_t)groups * kVec + tid]);
+    };
+    auto load_list = [&](int64_t row) {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            ahead[i] = TheList::get(a.ids + row * a.k, a.teacher + row * a.k, i * kHeldThreads + tid, a.k, a.V);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (ahead[i].id >= 0) ahead[i].at = E::get(logits[row * a.ld + ahead[i].id]);
+    };
+    int64_t row = blockIdx.x;
+    load_list(row);
+#pragma unroll
+    for (int i = 0; i < CHUNKS; ++i) load(logits + row * a.ld, i * kHeldThreads + tid, i);
+    load_tail(logits + row * a.ld);
+    for (;;) {
+        const float g = a.weight * (a.gloss ? a.gloss[row] : 1.0f);
+        t.clear<kHeldThreads>();
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (i * kHeldThreads + tid < a.k) l.entry[i * kHeldThreads + tid] = ahead[i];
+        l.sum(a.tau, s_tmp);
+        t.fill(l, 0, a.V, kVec);
+        Part p{-FLT_MAX, 0.0f};
+        const int mine = self();
+#pragma unroll
+        for (int i = 0; i < CHUNKS; ++i) {
+            if (i * kHeldThreads + mine >= groups) continue;
+            float f[kVec];
+            E::unpack(w[i], f);
+            add<kVec>(p, f, c);
+            __builtin_amdgcn_sched_barrier(0);  // (a group at a time: the row leaves no registers for more)
+        }
+        if (tid < rest) add<1>(p, &tail, c);
+        p = block_merge<kHeldThreads>(p, c, s_part);
+        const float loss = l.loss(p, a.tau, s_tmp);
+        if (tid == 0) a.loss[row] = loss;
+        const Slope sl(p, c, g * a.tau, l.total == 0.0);
+        T *dst = static_cast<T *>(a.grad) + row * a.grad_ld;
+        row += gridDim.x;
+        const bool more = row < a.N;
+        const T *s = logits + (more ? row : 0) * a.ld;
+        if (more) load_list(row);
+#pragma unroll
+        for (int i = 0; i < CHUNKS; ++i) {
+            const int group = i * kHeldThreads + self();
+            if (group >= groups) continue;
+            asm volatile("" : "+v"(w[i]));  // (unpacked again: the values of the pass before would not fit)
+            put_group<BF16>(sl, t, (uint32_t)group, group * kVec, w[i], dst + (uint32_t)(group * kVec));
+            if (more) load(s, group, i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (tid < rest) {
+            const int v = groups * kVec + tid;
+            put_one<BF16>(sl, t, (uint32_t)groups, v, tail, dst + v);
+        }
+        if (!more) return;
+        load_tail(s);
+        __syncthreads();  // (the table is read)
+    }
 }
 
 vie_status launched(const char *what)
@@ -258,29 +515,97 @@ vie_status launched(const char *what)
     return e == hipSuccess ? VIE_OK : fail(VIE_EHIP, "%s: %s", what, hipGetErrorString(e));
 }
 
+// LDS above 64 KB has to be asked for.
+vie_status allow_lds(const void *kernel, size_t lds)
+{
+    if (lds <= 64 * 1024) return VIE_OK;
+    const hipError_t e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    return e == hipSuccess ? VIE_OK : fail(VIE_EHIP, "distillation: %s", hipGetErrorString(e));
+}
+
+// Rows in parts: as many as give the device two workgroups a CU, of 8192
+// logits at least, and as many as a part's map of groups asks for.
+struct Split {
+    int parts;
+    int64_t len;
+    dim3 grid;
+};
+Split split_rows(const DistillLaunch &a, int most_groups)
+{
+    const int vec = a.dtype == VIE_BF16 ? 8 : 4;
+    int64_t parts = std::min<int64_t>((a.V + 8191) / 8192, 512 / a.N);
+    parts = std::max<int64_t>(parts, (a.V / vec + most_groups - 1) / most_groups);
+    parts = std::max<int64_t>(parts, 1);
+    Split s;
+    s.len = ((a.V + parts - 1) / parts + 63) / 64 * 64;
+    s.parts = (int)((a.V + s.len - 1) / s.len);
+    s.grid = dim3((unsigned)s.parts, (unsigned)std::min(a.N, 32768), (unsigned)((a.N + 32767) / 32768));
+    return s;
+}
+
+// The row's parts and, in a step that keeps none for the caller, its stats.
+size_t parts_bytes(int N) { return (size_t)N * kMaxParts * sizeof(Part); }
+
+template <bool BF16> vie_status forward(const DistillLaunch &a, hipStream_t s)
+{
+    Split sp = split_rows(a, INT32_MAX);
+    if (sp.parts > kMaxParts) {
+        sp.len = ((a.V + kMaxParts - 1) / kMaxParts + 63) / 64 * 64;
+        sp.parts = (int)((a.V + sp.len - 1) / sp.len);
+        sp.grid.x = (unsigned)sp.parts;
+    }
+    distill_forward_kernel<BF16><<<sp.grid, kThreads, list_lds(a.k), s>>>(a, sp.len);
+    if (sp.parts > 1) distill_join_kernel<BF16><<<a.N, kThreads, list_lds(a.k), s>>>(a, sp.parts);
+    return launched("distillation launch");
+}
+
+template <bool BF16> vie_status backward(const DistillLaunch &a, hipStream_t s)
+{
+    const Split sp = split_rows(a, kPartGroups - 1);
+    if (vie_status e = allow_lds((const void *)distill_backward_kernel<BF16>, table_lds(a.k))) return e;
+    distill_backward_kernel<BF16><<<sp.grid, kThreads, table_lds(a.k), s>>>(a, sp.len);
+    return launched("distillation gradient launch");
+}
+
+template <bool BF16, int CHUNKS> vie_status held(const DistillLaunch &a, hipStream_t s)
+{
+    if (vie_status e = allow_lds((const void *)distill_step_kernel<BF16, CHUNKS>, table_lds(a.k))) return e;
+    distill_step_kernel<BF16, CHUNKS><<<std::min(a.N, CHUNKS <= 6 ? 512 : 256), kHeldThreads, table_lds(a.k), s>>>(a);
+    return launched("distillation step launch");
+}
+
+template <bool BF16> vie_status step(const DistillLaunch &a, hipStream_t s)
+{
+    const int64_t chunks = (a.V / Elem<BF16>::kVec + kHeldThreads - 1) / kHeldThreads;
+    if (a.N >= 128 && chunks <= 22) {
+        if (chunks <= 6) return held<BF16, 6>(a, s);
+        if (chunks <= 11) return held<BF16, 11>(a, s);
+        if (chunks <= 16) return held<BF16, 16>(a, s);
+        return held<BF16, 22>(a, s);
+    }
+    DistillLaunch b = a;
+    b.stats = reinterpret_cast<float *>(static_cast<char *>(a.ws) + parts_bytes(a.N));
+    if (vie_status e = forward<BF16>(b, s)) return e;
+    return backward<BF16>(b, s);
+}
+
 }  // namespace
 
-size_t distill_workspace_bytes(int64_t, int) { return 0; }
+size_t distill_workspace_bytes(int64_t, int N) { return parts_bytes(N) + (size_t)N * 8; }
 
 vie_status launch_distill(const DistillLaunch &a, hipStream_t s)
 {
-    if (a.dtype == VIE_BF16) distill_row_kernel<true, false><<<a.N, kRowThreads, 0, s>>>(a);
-    else distill_row_kernel<false, false><<<a.N, kRowThreads, 0, s>>>(a);
-    return launched("distillation launch");
+    return a.dtype == VIE_BF16 ? forward<true>(a, s) : forward<false>(a, s);
 }
 
 vie_status launch_distill_grad(const DistillLaunch &a, hipStream_t s)
 {
-    if (a.dtype == VIE_BF16) distill_grad_kernel<true><<<a.N, kRowThreads, 0, s>>>(a);
-    else distill_grad_kernel<false><<<a.N, kRowThreads, 0, s>>>(a);
-    return launched("distillation gradient launch");
+    return a.dtype == VIE_BF16 ? backward<true>(a, s) : backward<false>(a, s);
 }
 
 vie_status launch_distill_step(const DistillLaunch &a, hipStream_t s)
 {
-    if (a.dtype == VIE_BF16) distill_row_kernel<true, true><<<a.N, kRowThreads, 0, s>>>(a);
-    else distill_row_kernel<false, true><<<a.N, kRowThreads, 0, s>>>(a);
-    return launched("distillation step launch");
+    return a.dtype == VIE_BF16 ? step<true>(a, s) : step<false>(a, s);
 }
 
 }  // namespace vie
