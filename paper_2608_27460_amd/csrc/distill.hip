@@ -403,110 +403,79 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void distill_backwar
 }
 
 // ---------------------------------------------------------------------------
-// both at once: a row held in registers
+// both at once
 // ---------------------------------------------------------------------------
 //
-// A workgroup of 1024 threads holds a row, CHUNKS groups of 16 bytes a
-// thread, so that it is read from memory once: the row's part is taken from
-// the registers, and as the gradient of a group leaves, the next row's group
-// is loaded in its place, so that reads and writes go on together.  The list
-// of the next row and the logits at its ids are read a row ahead too.
+// A workgroup of 1024 threads, two of them a CU, takes a row: its part first,
+// then its gradient, from the row's end to its beginning, so that the second
+// reading finds what the caches hold of the first.
 
-constexpr int kHeldThreads = 1024;
-constexpr int kHeldWaves = kHeldThreads / kLanes;
+constexpr int kBothThreads = 1024;
+constexpr int kBothWaves = kBothThreads / kLanes;
 
-template <bool BF16, int CHUNKS>
-__global__ __launch_bounds__(kHeldThreads) void distill_step_kernel(DistillLaunch a)
+template <bool BF16>
+__global__ __launch_bounds__(kBothThreads) __attribute__((amdgpu_waves_per_eu(8, 8))) void distill_both_kernel(DistillLaunch a)
 {
     typedef Elem<BF16> E;
-    typedef typename E::T T;
-    constexpr int kVec = E::kVec;
     extern __shared__ __align__(16) char smem[];
-    __shared__ double s_tmp[2 * kHeldWaves];
-    __shared__ Part s_part[kHeldWaves];
+    __shared__ double s_tmp[2 * kBothWaves];
+    __shared__ Part s_part[kBothWaves];
     const int tid = threadIdx.x;
+    const int64_t row = blockIdx.x;
     const float c = exponent_scale(a.tau);
-    const int groups = (int)(a.V / kVec), rest = (int)(a.V - (int64_t)groups * kVec);
-    const T *logits = static_cast<const T *>(a.logits);
-    typedef List<kHeldThreads> TheList;
-    TheList l{reinterpret_cast<Entry *>(smem), a.k};
+    const typename E::T *src = static_cast<const typename E::T *>(a.logits) + row * a.ld;
+    typename E::T *dst = static_cast<typename E::T *>(a.grad) + row * a.grad_ld;
+    const int groups = (int)(a.V / E::kVec), rest = (int)(a.V - (int64_t)groups * E::kVec);
+    List<kBothThreads> l{reinterpret_cast<Entry *>(smem), a.k};
     Table t(smem + list_lds(a.k), table_bits(a.k));
-    constexpr int kPer = kMaxList / kHeldThreads;
-    static_assert(kPer * kHeldThreads == kMaxList, "every list entry has a thread");
-    word4 w[CHUNKS];
-    float tail = 0.0f;
-    Entry ahead[kPer];
-    // (This thread's places are made anew in every pass: kept over the rows
-    // they would take the registers that hold the row.)
-    auto self = [&] {
-        int x = tid;
-        asm volatile("" : "+v"(x));
-        return x;
-    };
-    auto load = [&](const T *s, int group, int i) {
-        if (group < groups) w[i] = load_vec(s + (uint32_t)(group * kVec));
-    };
-    auto load_tail = [&](const T *s) {
-        if (tid < rest) tail = E::get(s[(int64_t)groups * kVec + tid]);
-    };
-    auto load_list = [&](int64_t row) {
+    t.clear<kBothThreads>();
+    l.template read<BF16>(a.ids + row * a.k, a.teacher + row * a.k, a.V, src);
+    Part p{-FLT_MAX, 0.0f};
+    int i = tid;
+    for (; i + (kFlight - 1) * kBothThreads < groups; i += kFlight * kBothThreads) {
+        word4 w[kFlight];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            ahead[i] = TheList::get(a.ids + row * a.k, a.teacher + row * a.k, i * kHeldThreads + tid, a.k, a.V);
+        for (int u = 0; u < kFlight; ++u) w[u] = load_vec(src + (int64_t)(i + u * kBothThreads) * E::kVec);
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (ahead[i].id >= 0) ahead[i].at = E::get(logits[row * a.ld + ahead[i].id]);
-    };
-    int64_t row = blockIdx.x;
-    load_list(row);
-#pragma unroll
-    for (int i = 0; i < CHUNKS; ++i) load(logits + row * a.ld, i * kHeldThreads + tid, i);
-    load_tail(logits + row * a.ld);
-    for (;;) {
-        const float g = a.weight * (a.gloss ? a.gloss[row] : 1.0f);
-        t.clear<kHeldThreads>();
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (i * kHeldThreads + tid < a.k) l.entry[i * kHeldThreads + tid] = ahead[i];
-        l.sum(a.tau, s_tmp);
-        t.fill(l, 0, a.V, kVec);
-        Part p{-FLT_MAX, 0.0f};
-        const int mine = self();
-#pragma unroll
-        for (int i = 0; i < CHUNKS; ++i) {
-            if (i * kHeldThreads + mine >= groups) continue;
-            float f[kVec];
-            E::unpack(w[i], f);
-            add<kVec>(p, f, c);
-            __builtin_amdgcn_sched_barrier(0);  // (a group at a time: the row leaves no registers for more)
+        for (int u = 0; u < kFlight; ++u) {
+            float f[E::kVec];
+            E::unpack(w[u], f);
+            add<E::kVec>(p, f, c);
         }
-        if (tid < rest) add<1>(p, &tail, c);
-        p = block_merge<kHeldThreads>(p, c, s_part);
-        const float loss = l.loss(p, a.tau, s_tmp);
-        if (tid == 0) a.loss[row] = loss;
-        const Slope sl(p, c, g * a.tau, l.total == 0.0);
-        T *dst = static_cast<T *>(a.grad) + row * a.grad_ld;
-        row += gridDim.x;
-        const bool more = row < a.N;
-        const T *s = logits + (more ? row : 0) * a.ld;
-        if (more) load_list(row);
-#pragma unroll
-        for (int i = 0; i < CHUNKS; ++i) {
-            const int group = i * kHeldThreads + self();
-            if (group >= groups) continue;
-            asm volatile("" : "+v"(w[i]));  // (unpacked again: the values of the pass before would not fit)
-            put_group<BF16>(sl, t, (uint32_t)group, group * kVec, w[i], dst + (uint32_t)(group * kVec));
-            if (more) load(s, group, i);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-        if (tid < rest) {
-            const int v = groups * kVec + tid;
-            put_one<BF16>(sl, t, (uint32_t)groups, v, tail, dst + v);
-        }
-        if (!more) return;
-        load_tail(s);
-        __syncthreads();  // (the table is read)
     }
+    for (; i < groups; i += kBothThreads) {
+        float f[E::kVec];
+        E::unpack(load_vec(src + (int64_t)i * E::kVec), f);
+        add<E::kVec>(p, f, c);
+    }
+    const int64_t last = (int64_t)groups * E::kVec + tid;
+    float tail = 0.0f;
+    if (tid < rest) {
+        tail = E::get(src[last]);
+        add<1>(p, &tail, c);
+    }
+    l.sum(a.tau, s_tmp);  // (the workgroup waits in here)
+    t.fill(l, 0, a.V, E::kVec);
+    p = block_merge<kBothThreads>(p, c, s_part);
+    const float loss = l.loss(p, a.tau, s_tmp);
+    if (tid == 0) a.loss[row] = loss;
+    const float g = a.weight * (a.gloss ? a.gloss[row] : 1.0f);
+    const Slope sl(p, c, g * a.tau, l.total == 0.0);
+    if (tid < rest) put_one<BF16>(sl, t, (uint32_t)groups, (int32_t)last, tail, dst + last);
+    // whole rounds from the end, then what is left of the first one
+    i = groups - 1 - tid;
+    for (; i - (kFlight - 1) * kBothThreads >= 0; i -= kFlight * kBothThreads) {
+        word4 w[kFlight];
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) w[u] = load_vec(src + (int64_t)(i - u * kBothThreads) * E::kVec);
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) {
+            const int at = i - u * kBothThreads;
+            put_group<BF16>(sl, t, (uint32_t)at, at * E::kVec, w[u], dst + (int64_t)at * E::kVec);
+        }
+    }
+    for (; i >= 0; i -= kBothThreads)
+        put_group<BF16>(sl, t, (uint32_t)i, i * E::kVec, load_vec(src + (int64_t)i * E::kVec), dst + (int64_t)i * E::kVec);
 }
 
 vie_status launched(const char *what)
@@ -523,17 +492,17 @@ vie_status allow_lds(const void *kernel, size_t lds)
     return e == hipSuccess ? VIE_OK : fail(VIE_EHIP, "distillation: %s", hipGetErrorString(e));
 }
 
-// Rows in parts: as many as give the device two workgroups a CU, of 8192
+// Rows in parts: as many as give the device two workgroups a CU, of `least`
 // logits at least, and as many as a part's map of groups asks for.
 struct Split {
     int parts;
     int64_t len;
     dim3 grid;
 };
-Split split_rows(const DistillLaunch &a, int most_groups)
+Split split_rows(const DistillLaunch &a, int64_t least, int most_groups)
 {
     const int vec = a.dtype == VIE_BF16 ? 8 : 4;
-    int64_t parts = std::min<int64_t>((a.V + 8191) / 8192, 512 / a.N);
+    int64_t parts = std::min<int64_t>((a.V + least - 1) / least, 512 / a.N);
     parts = std::max<int64_t>(parts, (a.V / vec + most_groups - 1) / most_groups);
     parts = std::max<int64_t>(parts, 1);
     Split s;
@@ -548,7 +517,8 @@ size_t parts_bytes(int N) { return (size_t)N * kMaxParts * sizeof(Part); }
 
 template <bool BF16> vie_status forward(const DistillLaunch &a, hipStream_t s)
 {
-    Split sp = split_rows(a, INT32_MAX);
+    // (joining parts is a launch more: 4 us, in which a workgroup reads some 200 KB)
+    Split sp = split_rows(a, 32768, INT32_MAX);
     if (sp.parts > kMaxParts) {
         sp.len = ((a.V + kMaxParts - 1) / kMaxParts + 63) / 64 * 64;
         sp.parts = (int)((a.V + sp.len - 1) / sp.len);
@@ -561,27 +531,18 @@ template <bool BF16> vie_status forward(const DistillLaunch &a, hipStream_t s)
 
 template <bool BF16> vie_status backward(const DistillLaunch &a, hipStream_t s)
 {
-    const Split sp = split_rows(a, kPartGroups - 1);
+    const Split sp = split_rows(a, 8192, kPartGroups - 1);
     if (vie_status e = allow_lds((const void *)distill_backward_kernel<BF16>, table_lds(a.k))) return e;
     distill_backward_kernel<BF16><<<sp.grid, kThreads, table_lds(a.k), s>>>(a, sp.len);
     return launched("distillation gradient launch");
 }
 
-template <bool BF16, int CHUNKS> vie_status held(const DistillLaunch &a, hipStream_t s)
-{
-    if (vie_status e = allow_lds((const void *)distill_step_kernel<BF16, CHUNKS>, table_lds(a.k))) return e;
-    distill_step_kernel<BF16, CHUNKS><<<std::min(a.N, CHUNKS <= 6 ? 512 : 256), kHeldThreads, table_lds(a.k), s>>>(a);
-    return launched("distillation step launch");
-}
-
 template <bool BF16> vie_status step(const DistillLaunch &a, hipStream_t s)
 {
-    const int64_t chunks = (a.V / Elem<BF16>::kVec + kHeldThreads - 1) / kHeldThreads;
-    if (a.N >= 128 && chunks <= 22) {
-        if (chunks <= 6) return held<BF16, 6>(a, s);
-        if (chunks <= 11) return held<BF16, 11>(a, s);
-        if (chunks <= 16) return held<BF16, 16>(a, s);
-        return held<BF16, 22>(a, s);
+    if (a.N >= 128 && a.V / Elem<BF16>::kVec < kPartGroups) {
+        if (vie_status e = allow_lds((const void *)distill_both_kernel<BF16>, table_lds(a.k))) return e;
+        distill_both_kernel<BF16><<<a.N, kBothThreads, table_lds(a.k), s>>>(a);
+        return launched("distillation step launch");
     }
     DistillLaunch b = a;
     b.stats = reinterpret_cast<float *>(static_cast<char *>(a.ws) + parts_bytes(a.N));
