@@ -19,6 +19,13 @@ __device__ __forceinline__ uint16_t to_bf16(float v)  // nearest, ties to even
     return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
+__device__ __forceinline__ uint32_t to_bf16x2(float lo, float hi)
+{
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f2{lo, hi}), b2));
+}
+
 // Element types of rows: fp32, and bf16 as raw bits.
 template <bool BF16> struct Elem {
     typedef float T;
@@ -55,7 +62,7 @@ template <> struct Elem<true> {
     {
         word4 w;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = (uint32_t)to_bf16(f[2 * i]) | (uint32_t)to_bf16(f[2 * i + 1]) << 16;
+        for (int i = 0; i < 4; ++i) w[i] = to_bf16x2(f[2 * i], f[2 * i + 1]);
         return w;
     }
 };

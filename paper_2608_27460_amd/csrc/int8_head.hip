@@ -326,8 +326,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
                     for (int i = 0; i < 4; ++i) f[i] = __int_as_float(acc[h * kPer + m][n][i]);
                     if constexpr (OUT_BF16) {
-                        const uint32_t w[2] = {(uint32_t)to_bf16(f[0]) | (uint32_t)to_bf16(f[1]) << 16,
-                                               (uint32_t)to_bf16(f[2]) | (uint32_t)to_bf16(f[3]) << 16};
+                        const uint32_t w[2] = {to_bf16x2(f[0], f[1]), to_bf16x2(f[2], f[3])};
                         char *p = tmp + r * (kUnits * 16) + 16 * ((2 * m + g / 2) ^ (r & (kUnits - 1))) + 8 * (g & 1);
                         *reinterpret_cast<uint64_t *>(p) = (uint64_t)w[1] << 32 | w[0];
                     } else {
