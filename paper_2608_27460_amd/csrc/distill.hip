@@ -296,7 +296,7 @@ constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kLanes;
 constexpr int kFlight = 4;                       // 16-byte loads of a thread in flight
 constexpr int kMaxParts = 64;                    // of a row
-constexpr int kPartGroups = 32 * kMapWords;      // 16-byte groups of a part, at most
+constexpr int kMapGroups = 32 * kMapWords;       // 16-byte groups that a map has bits for
 
 template <bool BF16> __global__ __launch_bounds__(kThreads) void distill_forward_kernel(DistillLaunch a, int64_t len)
 {
@@ -542,7 +542,9 @@ template <bool BF16> vie_status forward(const DistillLaunch &a, hipStream_t s)
 
 template <bool BF16> vie_status backward(const DistillLaunch &a, hipStream_t s)
 {
-    const Split sp = split_rows(a, 8192, kPartGroups - 1);
+    // (parts of 64 KB: more workgroups than fit at once, whose ends and lists
+    // others stream over; 2048 rows of 128256 bf16: 237 us as whole rows, 209)
+    const Split sp = split_rows(a, 8192, 4096);
     if (vie_status e = allow_lds((const void *)distill_backward_kernel<BF16>, table_lds(a.k))) return e;
     distill_backward_kernel<BF16><<<sp.grid, kThreads, table_lds(a.k), s>>>(a, sp.len);
     return launched("distillation gradient launch");
@@ -550,7 +552,7 @@ template <bool BF16> vie_status backward(const DistillLaunch &a, hipStream_t s)
 
 template <bool BF16> vie_status step(const DistillLaunch &a, hipStream_t s)
 {
-    if (a.N >= 128 && a.V / Elem<BF16>::kVec < kPartGroups) {
+    if (a.N >= 128 && a.V / Elem<BF16>::kVec < kMapGroups) {
         if (vie_status e = allow_lds((const void *)distill_both_kernel<BF16>, table_lds(a.k))) return e;
         distill_both_kernel<BF16><<<a.N, kBothThreads, table_lds(a.k), s>>>(a);
         return launched("distillation step launch");
