@@ -19,6 +19,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "block.hpp"
 #include "keys.hpp"
@@ -46,7 +47,7 @@ __host__ __device__ inline int fixed_shift(int64_t n)
     return 62 - lg;
 }
 
-// exp(x) for x <= 0 (or NaN, which gives 0), to 2^-49 relative: 2^(n / 64)
+// exp(x) for x <= 0 (or NaN, which gives 0), to 2^-50 relative: 2^(n / 64)
 // from the exponent and a 64-bit value per n % 64, times the Taylor sum of the rest, at
 // most ln 2 / 128 in size, to the fifth power (the sixth is below 2^-54).
 struct Exp2Table {
@@ -67,9 +68,11 @@ constexpr Exp2Table make_table()
 }
 __device__ constexpr Exp2Table kExp2 = make_table();
 
-__device__ __forceinline__ double exp_down(double x)
+// `table`: kExp2's values, or a copy of them in LDS.
+__device__ __forceinline__ double exp_down(double x, const double *table)
 {
-    const double k = rint(fmax(x, -800.0) * (64 * 1.4426950408889634074));  // (fmax: the number, if one is NaN)
+    x = fmax(x, -800.0);  // (2^-1154, which is 0; NaN too: fmax gives the number)
+    const double k = rint(x * (64 * 1.4426950408889634074));
     double r = fma(k, -0.69314718055994530942 / 64, x);
     r = fma(k, -2.3190468138462996e-17 / 64, r);
     double p = fma(r, 1.0 / 120, 1.0 / 24);
@@ -78,12 +81,15 @@ __device__ __forceinline__ double exp_down(double x)
     p = fma(p, r, 1.0);
     p = fma(p, r, 1.0);
     const int n = (int)k;
-    return x >= -745.0 ? ldexp(kExp2.v[n & 63] * p, n >> 6) : 0.0;
+    return ldexp(table[n & 63] * p, n >> 6);
 }
-__device__ __forceinline__ double weight(float l, float best, double inv_t)
+// (exactly 1 at the best logit, infinite or not; inv_t is finite)
+__device__ __forceinline__ double weight(float l, float best, double inv_t, const double *table = kExp2.v)
 {
-    return l == best ? 1.0 : exp_down(((double)l - (double)best) * inv_t);
+    const double d = (double)l - (double)best;
+    return exp_down((l == best ? 0.0 : d) * inv_t, table);
 }
+__device__ __forceinline__ double inverse(double t) { return fmin(1.0 / t, 1e300); }
 __device__ __forceinline__ uint64_t fixed(double w, double one) { return (uint64_t)(w * one + 0.5); }
 
 // Borders as integers: C >= p T iff C >= reach(p, T), C > u T iff C > below(u, T).
@@ -180,7 +186,7 @@ template <int NT> __global__ __launch_bounds__(NT) void sample_list_kernel(Sampl
         return;
     }
     const float best = key_logit(s_key[0]);
-    const double inv_t = 1.0 / st.t, one = ldexp(1.0, fixed_shift(kMaxList));
+    const double inv_t = inverse(st.t), one = ldexp(1.0, fixed_shift(kMaxList));
     const int K = st.k > 0 && st.k < live ? st.k : live;
     // sums in order, NT candidates at a time; the prefix that passes min-p
     uint64_t base = 0;
@@ -296,23 +302,35 @@ template <bool BF16> struct Row {
     float best;
     double inv_t, one;
 
-    // f(logit, id) for every candidate from i0 on, n of them, by the whole workgroup
+    // f(logit, id) for every candidate of the n logits from i0 on, by the whole workgroup
     template <typename F> __device__ __forceinline__ void each(int64_t i0, int64_t n, F f) const
+    {
+        groups(i0, n, [&](const float *x, int32_t id, auto count) {
+#pragma unroll
+            for (int e = 0; e < decltype(count)::value; ++e)
+                if (candidate(x[e])) f(x[e], id + e);
+        });
+    }
+    // f(logits, first id, how many) for groups of them: 16 bytes, or one at the ends
+    template <typename F> __device__ __forceinline__ void groups(int64_t i0, int64_t n, F f) const
     {
         const typename E::T *p = l + i0;
         const Span<typename E::T> sp(p, n);
         const word4 *v = reinterpret_cast<const word4 *>(p + sp.head);
+        // (the next 16 bytes are on their way while these are worked on)
+        word4 next = {0, 0, 0, 0};
+        if (threadIdx.x < sp.vecs) next = v[threadIdx.x];
         for (int64_t i = threadIdx.x; i < sp.vecs; i += kRowThreads) {
+            const word4 w = next;
+            if (i + kRowThreads < sp.vecs) next = v[i + kRowThreads];
             float x[E::kVec];
-            E::unpack(v[i], x);
-#pragma unroll
-            for (int e = 0; e < E::kVec; ++e)
-                if (candidate(x[e])) f(x[e], (int32_t)(i0 + sp.head + i * E::kVec + e));
+            E::unpack(w, x);
+            f(x, (int32_t)(i0 + sp.head + i * E::kVec), std::integral_constant<int, E::kVec>());
         }
         for (int64_t i = threadIdx.x; i < sp.head + n - sp.tail0; i += kRowThreads) {
             const int64_t at = i < sp.head ? i : sp.tail0 + i - sp.head;
             const float x = E::get(p[at]);
-            if (candidate(x)) f(x, (int32_t)(i0 + at));
+            f(&x, (int32_t)(i0 + at), std::integral_constant<int, 1>());
         }
     }
     __device__ __forceinline__ uint64_t units(float l) const { return fixed(weight(l, best, inv_t), one); }
@@ -449,7 +467,7 @@ template <bool BF16> __device__ __forceinline__ bool begin(Row<BF16> &row, uint6
 {
     if (best == 0 || !(st.t > 0.0)) return false;
     row.best = key_logit(best);
-    row.inv_t = 1.0 / st.t;
+    row.inv_t = inverse(st.t);
     row.one = ldexp(1.0, fixed_shift(n));
     return true;
 }
@@ -459,23 +477,37 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_bins_ke
     extern __shared__ __align__(16) char smem[];
     uint64_t *s_sum = reinterpret_cast<uint64_t *>(smem);
     uint32_t *s_count = reinterpret_cast<uint32_t *>(s_sum + kBins);
+    __shared__ double s_exp[64];
     __shared__ uint32_t s_pass;
     const int b = parts.b0 + blockIdx.y, tid = threadIdx.x;
     RowSpace &ws = parts.ws[blockIdx.y];
     const Settings st = settings(a.prm, b);
     Row<BF16> row = row_of<BF16>(a, b);
-    if (!begin(row, best_key(ws, gridDim.x), st, a.n)) return;
-    for (int i = tid; i < kBins; i += kRowThreads) s_sum[i] = 0, s_count[i] = 0;
+    for (int i = tid; i < kBins / 2; i += kRowThreads) reinterpret_cast<ulonglong2 *>(s_sum)[i] = {0, 0};
+    for (int i = tid; i < kBins / 4; i += kRowThreads) reinterpret_cast<uint4 *>(s_count)[i] = {0, 0, 0, 0};
+    if (tid < 64) s_exp[tid] = kExp2.v[tid];
     if (tid == 0) s_pass = 0;
+    if (!begin(row, best_key(ws, gridDim.x), st, a.n)) return;
     __syncthreads();
     uint32_t pass = 0;
     const int64_t i0 = blockIdx.x * parts.len;
-    row.each(i0, min(parts.len, a.n - i0), [&](float l, int32_t) {
-        const int bin = bin_of(row.best, l);
-        const double w = weight(l, row.best, row.inv_t);
-        pass += w >= st.m;
-        atomicAdd(&s_count[bin], 1u);
-        atomicAdd((unsigned long long *)&s_sum[bin], (unsigned long long)fixed(w, row.one));
+    row.groups(i0, min(parts.len, a.n - i0), [&](const float *l, int32_t, auto count) {
+        constexpr int N = decltype(count)::value;
+        int bin[N];
+        uint64_t units[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) {  // (without branches, so that their latencies overlap)
+            bin[e] = bin_of(row.best, l[e]);
+            const double w = weight(l[e], row.best, row.inv_t, s_exp);
+            pass += candidate(l[e]) & (w >= st.m);
+            units[e] = fixed(w, row.one);
+        }
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+            if (candidate(l[e])) {
+                atomicAdd(&s_count[bin[e]], 1u);
+                atomicAdd((unsigned long long *)&s_sum[bin[e]], (unsigned long long)units[e]);
+            }
     });
     pass = wave_sum(pass);
     if ((tid & (kLanes - 1)) == 0) atomicAdd(&s_pass, pass);
@@ -576,22 +608,31 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     DrawLds &s = *reinterpret_cast<DrawLds *>(smem);
     const int b = parts.b0 + blockIdx.y, tid = threadIdx.x, S = gridDim.x;
     RowSpace &ws = parts.ws[blockIdx.y];
+    // the bins, kBinsPer a thread (read while the row's settings are)
+    uint32_t cnt[kBinsPer], c = 0;
+    uint64_t sum[kBinsPer], x = 0;
+    static_assert(kBinsPer % 4 == 0, "read 16 bytes at a time");
+#pragma unroll
+    for (int i = 0; i < kBinsPer; i += 4) {
+        const uint4 v = *reinterpret_cast<const uint4 *>(&ws.count[tid * kBinsPer + i]);
+        cnt[i] = v.x, cnt[i + 1] = v.y, cnt[i + 2] = v.z, cnt[i + 3] = v.w;
+    }
+#pragma unroll
+    for (int i = 0; i < kBinsPer; i += 2) {
+        const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(&ws.sum[tid * kBinsPer + i]);
+        sum[i] = v.x, sum[i + 1] = v.y;
+    }
+    const uint32_t pass = ws.pass;
     const Settings st = settings(a.prm, b);
+    const float u = a.u[b];
     Row<BF16> row = row_of<BF16>(a, b);
     const uint64_t best = best_key(ws, S);
     if (!begin(row, best, st, a.n)) {
         if (blockIdx.x == 0 && tid == 0) put(a, b, best == 0 ? Result{-1, 0.0f, 0} : Result{key_id(best), 1.0f, 1});
         return;
     }
-    const float u = a.u[b];
-
-    // sums over the bins, kBinsPer a thread
-    uint32_t cnt[kBinsPer], c = 0;
-    uint64_t sum[kBinsPer], x = 0;
 #pragma unroll
     for (int i = 0; i < kBinsPer; ++i) {
-        cnt[i] = ws.count[tid * kBinsPer + i];
-        sum[i] = ws.sum[tid * kBinsPer + i];
         c += cnt[i];
         x += sum[i];
     }
@@ -601,7 +642,6 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     uint32_t live = 0;
     uint64_t total = 0;
     for (int w = 0; w < kRowWaves; ++w) live += s.wave_count[w], total += s.wave_sum[w];
-    const uint32_t pass = ws.pass;
     // before this thread's bins
     c -= call;
     x -= xall;
@@ -652,21 +692,23 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     // ... the number kept ...
     const uint32_t most = st.m > 0.0 ? max(min(K, pass), 1u) : K;
     uint32_t kmin = most, kmax = most;
+    int at_end = 0;
     if (st.p < 1.0) {
-        const int e = bins(false, reach(st.p, lo), reach(st.p, hi));
+        at_end = bins(false, reach(st.p, lo), reach(st.p, hi));
         kmin = min(most, s.at[0].count0 + 1);
-        kmax = min(most, s.at[e].count1);
-        collect(s.at[0].bin, s.at[e].bin);
+        kmax = min(most, s.at[at_end].count1);
+        collect(s.at[0].bin, s.at[at_end].bin);
     }
-    // ... their weight ...
-    lo = hi = total;
+    // ... their weight (the bins just found, unless another limit cuts in) ...
     bool exact_end = true;
-    if (kmin < live) {
-        const int e = bins(true, kmin, kmax);
-        hi = s.at[e].sum1;
+    if (kmin == live) {
+        lo = hi = total;
+    } else {
+        if (kmax == most) at_end = bins(true, kmin, kmax);
+        hi = s.at[at_end].sum1;
         exact_end = kmin == kmax && s.at[0].count1 == kmin;
         lo = exact_end ? hi : s.at[0].sum0;
-        if (!exact_end) collect(s.at[0].bin, s.at[e].bin);
+        if (!exact_end) collect(s.at[0].bin, s.at[at_end].bin);
     }
     const uint64_t sum_end = hi;
     // ... and the token.
@@ -746,6 +788,10 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     while (P < (int)M) P <<= 1;
     for (int i = (int)M + tid; i < P; i += kRowThreads) s.d.key[i] = 0;
     __syncthreads();
+    // Waves without a candidate end here: a barrier waits for the others only,
+    // and the sooner the fewer they are.
+    const int waves = min(P / kLanes, kRowWaves);
+    if (tid >= waves * kLanes) return;
     if (P <= kRowThreads) sort_row<1>(s.d.key, P);
     else sort_row<2>(s.d.key, P);
     uint64_t own[kCollect / kRowThreads];
@@ -754,11 +800,16 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
 #pragma unroll
     for (int h = 0; h < kCollect / kRowThreads; ++h) {
         const int i = h * kRowThreads + tid;
-        uint32_t none = 0;
-        uint64_t w = i < (int)M ? row.units(key_logit(s.d.key[i])) : 0ull;
-        block_scan(none, w, s.wave_count, s.wave_sum);
-        s.d.sum[i] = base + w;
-        for (int v = 0; v < kRowWaves; ++v) base += s.wave_sum[v];
+        if (h * kRowThreads >= P) break;
+        uint64_t w = wave_scan(i < (int)M ? row.units(key_logit(s.d.key[i])) : 0ull);
+        if ((tid & (kLanes - 1)) == kLanes - 1) s.wave_sum[tid / kLanes] = w;
+        __syncthreads();
+        w += base;
+        for (int v = 0; v < waves; ++v) {
+            if (v < tid / kLanes) w += s.wave_sum[v];
+            base += s.wave_sum[v];
+        }
+        s.d.sum[i] = w;
         __syncthreads();
     }
 #pragma unroll
