@@ -42,18 +42,16 @@ __device__ __forceinline__ Settings settings(const vie_sample_params &a, int b)
 
 __host__ __device__ inline int fixed_shift(int64_t n)
 {
-    int lg = 0;
+    int lg = 11;  // (at most 2^51 a weight, which fp64 holds with its rounding)
     while ((int64_t(1) << lg) < n) ++lg;
     return 62 - lg;
 }
 
-// exp(x) for x <= 0 (or NaN, which gives 0), to 2^-50 relative: 2^(n / 64)
-// from the exponent and a 64-bit value per n % 64, times the Taylor sum of the rest, at
-// most ln 2 / 128 in size, to the fifth power (the sixth is below 2^-54).
+// 2^(i / 64) by its series
 struct Exp2Table {
     double v[64];
 };
-constexpr double exp2_64(int i)  // 2^(i / 64) by its series
+constexpr double exp2_64(int i)
 {
     const double x = i * 0.69314718055994530942 / 64;
     double t = 1.0, s = 1.0;
@@ -68,29 +66,43 @@ constexpr Exp2Table make_table()
 }
 __device__ constexpr Exp2Table kExp2 = make_table();
 
-// `table`: kExp2's values, or a copy of them in LDS.
-__device__ __forceinline__ double exp_down(double x, const double *table)
-{
-    x = fmax(x, -800.0);  // (2^-1154, which is 0; NaN too: fmax gives the number)
-    const double k = rint(x * (64 * 1.4426950408889634074));
-    double r = fma(k, -0.69314718055994530942 / 64, x);
-    r = fma(k, -2.3190468138462996e-17 / 64, r);
-    double p = fma(r, 1.0 / 120, 1.0 / 24);
-    p = fma(p, r, 1.0 / 6);
-    p = fma(p, r, 0.5);
-    p = fma(p, r, 1.0);
-    p = fma(p, r, 1.0);
-    const int n = (int)k;
-    return ldexp(table[n & 63] * p, n >> 6);
-}
-// (exactly 1 at the best logit, infinite or not; inv_t is finite)
-__device__ __forceinline__ double weight(float l, float best, double inv_t, const double *table = kExp2.v)
-{
-    const double d = (double)l - (double)best;
-    return exp_down((l == best ? 0.0 : d) * inv_t, table);
-}
-__device__ __forceinline__ double inverse(double t) { return fmin(1.0 / t, 1e300); }
-__device__ __forceinline__ uint64_t fixed(double w, double one) { return (uint64_t)(w * one + 0.5); }
+// Weights in units of 2^-shift of the best one, without branches, so that the
+// latencies of several overlap: exp((l - best) / t) = 2^(y / 64), y the
+// difference times 64 log2(e) / t; a table gives the whole part of y, the
+// Taylor sum to the fifth power the rest (at most 1/2: the sixth power is
+// below 2^-55 of the sum).  The error is that of y, 2^-47 relative for the
+// smallest weights.  Exactly 1 at the best logit.  An infinite best logit is
+// 1e300 here, as are all infinite ones, so that no difference is NaN, and the
+// factor is kept where such a difference is still -inf or large.
+struct Weights {
+    double best, scale;
+    int shift;
+    const double *table;  // kExp2's values, or a copy of them in LDS
+    __device__ __forceinline__ Weights(float best, double t, int shift, const double *table = kExp2.v)
+        : best(fmin((double)best, 1e300)), scale(fmin(fmax(64 * 1.4426950408889634074 / t, 1e-290), 1e300)), shift(shift),
+          table(table)
+    {
+    }
+    __device__ __forceinline__ double real(float l) const  // times 2^shift
+    {
+        const double y = fmax((fmin((double)l, 1e300) - best) * scale, -64.0 * 1100.0);  // (2^-1100 is 0 in any units)
+        const double k = rint(y), f = y - k;
+        constexpr double c = 0.69314718055994530942 / 64;
+        double p = fma(f, c * c * c * c * c / 120, c * c * c * c / 24);
+        p = fma(p, f, c * c * c / 6);
+        p = fma(p, f, c * c / 2);
+        p = fma(p, f, c);
+        p = fma(p, f, 1.0);
+        const int n = (int)k;
+        return ldexp(table[n & 63] * p, (n >> 6) + shift);
+    }
+    static __device__ __forceinline__ uint64_t round(double w)  // to the nearest integer, from the bits of 2^52 + w
+    {
+        return __builtin_bit_cast(uint64_t, w + 4503599627370496.0) & 0xFFFFFFFFFFFFFull;
+    }
+    __device__ __forceinline__ uint64_t units(float l) const { return round(real(l)); }
+    __device__ __forceinline__ double least(double min_p) const { return ldexp(min_p, shift); }
+};
 
 // Borders as integers: C >= p T iff C >= reach(p, T), C > u T iff C > below(u, T).
 __device__ __forceinline__ uint64_t reach(double p, uint64_t total) { return p > 0.0 ? (uint64_t)ceil(p * (double)total) : 0ull; }
@@ -185,17 +197,17 @@ template <int NT> __global__ __launch_bounds__(NT) void sample_list_kernel(Sampl
         if (tid == 0) put(a, b, {key_id(s_key[0]), 1.0f, 1});
         return;
     }
-    const float best = key_logit(s_key[0]);
-    const double inv_t = inverse(st.t), one = ldexp(1.0, fixed_shift(kMaxList));
+    const Weights weights(key_logit(s_key[0]), st.t, fixed_shift(kMaxList));
+    const double least = weights.least(st.m);
     const int K = st.k > 0 && st.k < live ? st.k : live;
     // sums in order, NT candidates at a time; the prefix that passes min-p
     uint64_t base = 0;
     for (int j0 = 0; j0 < K; j0 += NT) {
         const int j = j0 + tid;
         double w = 0.0;
-        if (j < K) w = weight(key_logit(s_key[j]), best, inv_t);
-        const bool ok = j < K && w >= st.m;
-        uint64_t x = wave_scan(j < K ? fixed(w, one) : 0ull);
+        if (j < K) w = weights.real(key_logit(s_key[j]));
+        const bool ok = j < K && w >= least;
+        uint64_t x = wave_scan(j < K ? Weights::round(w) : 0ull);
         const unsigned long long pass = __ballot(ok);
         if (W > 1) {
             if ((tid & (kLanes - 1)) == kLanes - 1) s_wave[tid / kLanes] = x;
@@ -217,7 +229,7 @@ template <int NT> __global__ __launch_bounds__(NT) void sample_list_kernel(Sampl
     kept = max(kept, 1);
     const uint64_t total = s_sum[kept - 1];
     const int j = min(first_at<true>(s_sum, kept, below(u, total)), kept - 1);
-    put(a, b, {key_id(s_key[j]), (float)(weight(key_logit(s_key[j]), best, inv_t) * one / (double)total), kept});
+    put(a, b, {key_id(s_key[j]), (float)(weights.real(key_logit(s_key[j])) / (double)total), kept});
 }
 
 // ---------------------------------------------------------------------------
@@ -261,11 +273,13 @@ constexpr int kMaxParts = 128;
 constexpr int kMaxSlots = 256;             // bins that borders can fall into
 constexpr int kMaxRows = 1024;             // rows of one round of launches (114 KB of workspace each)
 
-// The bin of a logit: monotone, bin 0 the best.
-__device__ __forceinline__ int bin_of(float best, float l)
+// The bin of a logit: monotone, bin 0 the best (`top`: the best logit by
+// bin_best, so that infinite ones give no NaN; NaN gives the last bin).
+__device__ __forceinline__ float bin_best(uint64_t best) { return fminf(key_logit(best), __FLT_MAX__); }
+__device__ __forceinline__ int bin_of(float top, float l)
 {
     constexpr int kFirst = 124 << 10;  // 2^-3: exponent 124, ten mantissa bits
-    const int x = (int)(__float_as_uint(l == best ? 0.0f : best - l) >> 13) - kFirst + 1;
+    const int x = (int)(__float_as_uint(top - fminf(l, __FLT_MAX__)) >> 13) - kFirst + 1;
     return x < 0 ? 0 : x > kBins - 1 ? kBins - 1 : x;
 }
 
@@ -299,8 +313,6 @@ template <bool BF16> struct Row {
     typedef Elem<BF16> E;
     const typename E::T *l;
     int64_t n;
-    float best;
-    double inv_t, one;
 
     // f(logit, id) for every candidate of the n logits from i0 on, by the whole workgroup
     template <typename F> __device__ __forceinline__ void each(int64_t i0, int64_t n, F f) const
@@ -333,7 +345,6 @@ template <bool BF16> struct Row {
             f(&x, (int32_t)(i0 + at), std::integral_constant<int, 1>());
         }
     }
-    __device__ __forceinline__ uint64_t units(float l) const { return fixed(weight(l, best, inv_t), one); }
 };
 
 // Inclusive sums over the workgroup's threads of a count and a sum.
@@ -352,7 +363,7 @@ __device__ __forceinline__ void block_scan(uint32_t &c, uint64_t &s, uint32_t *w
 // by a histogram of the candidates that share the digits before.  If there is
 // none (`sum` above the total), the last candidate.
 template <bool BF16>
-__device__ __noinline__ Place find(const Row<BF16> &row, bool by_rank, int64_t rank, uint64_t sum, DigitLds &s)
+__device__ __noinline__ Place find(const Row<BF16> &row, const Weights &weights, bool by_rank, int64_t rank, uint64_t sum, DigitLds &s)
 {
     const int tid = threadIdx.x;
     uint64_t prefix = 0, before_sum = 0;
@@ -368,7 +379,7 @@ __device__ __noinline__ Place find(const Row<BF16> &row, bool by_rank, int64_t r
             if (shift + bits < 64 && (key >> (shift + bits)) != prefix) return;
             const int bin = (int)((key >> shift) & ((1u << bits) - 1));
             atomicAdd(&s.count[bin], 1u);
-            atomicAdd((unsigned long long *)&s.sum[bin], (unsigned long long)row.units(l));
+            atomicAdd((unsigned long long *)&s.sum[bin], (unsigned long long)weights.units(l));
         });
         __syncthreads();
         // bins from the top, two a thread
@@ -400,29 +411,29 @@ __device__ __noinline__ Place find(const Row<BF16> &row, bool by_rank, int64_t r
         before_sum = s.at.sum;
         before = s.at.rank;
     }
-    return {prefix, before_sum + row.units(key_logit(prefix)), before + 1};
+    return {prefix, before_sum + weights.units(key_logit(prefix)), before + 1};
 }
 
 // The drawn candidate as a result; `end` units of weight are kept.
-template <bool BF16> __device__ __forceinline__ Result drawn(const Row<BF16> &row, uint64_t key, uint64_t end, int64_t kept)
+__device__ __forceinline__ Result drawn(const Weights &weights, uint64_t key, uint64_t end, int64_t kept)
 {
-    return {key_id(key), (float)(weight(key_logit(key), row.best, row.inv_t) * row.one / (double)end), (int32_t)kept};
+    return {key_id(key), (float)(weights.real(key_logit(key)) / (double)end), (int32_t)kept};
 }
 
 // The borders one after the other, over the whole row: `live` candidates,
 // `total` units of weight, `pass` candidates within min-p.
 template <bool BF16>
-__device__ __noinline__ Result draw_by_digits(const Row<BF16> &row, Settings st, float u, uint32_t live, uint64_t total, uint32_t pass,
+__device__ __noinline__ Result draw_by_digits(const Row<BF16> &row, const Weights &weights, Settings st, float u, uint32_t live, uint64_t total, uint32_t pass,
                                  DigitLds &s)
 {
     Place end{0, total, (int64_t)live};  // the last candidate kept
-    if (st.k > 0 && st.k < live) end = find<BF16>(row, true, st.k, 0, s);
-    if (st.p < 1.0) end = find<BF16>(row, false, 0, reach(st.p, end.sum), s);
-    if (st.m > 0.0 && (int64_t)pass < end.rank) end = find<BF16>(row, true, max(pass, 1u), 0, s);
+    if (st.k > 0 && st.k < live) end = find<BF16>(row, weights, true, st.k, 0, s);
+    if (st.p < 1.0) end = find<BF16>(row, weights, false, 0, reach(st.p, end.sum), s);
+    if (st.m > 0.0 && (int64_t)pass < end.rank) end = find<BF16>(row, weights, true, max(pass, 1u), 0, s);
     // (never beyond the kept ones, also for u of 1 and above)
     const uint64_t past = below(u, end.sum) + 1;
-    const Place at = find<BF16>(row, false, 0, past < end.sum ? past : end.sum, s);
-    return drawn(row, at.key, end.sum, end.rank);
+    const Place at = find<BF16>(row, weights, false, 0, past < end.sum ? past : end.sum, s);
+    return drawn(weights, at.key, end.sum, end.rank);
 }
 
 // Workgroup (c, i) takes part c of row b0 + i in each of the three kernels.
@@ -433,7 +444,7 @@ struct Parts {
 };
 template <bool BF16> __device__ __forceinline__ Row<BF16> row_of(const SampleLaunch &a, int b)
 {
-    return {static_cast<const typename Elem<BF16>::T *>(a.logits) + (int64_t)b * a.ld, a.n, 0.0f, 0.0, 0.0};
+    return {static_cast<const typename Elem<BF16>::T *>(a.logits) + (int64_t)b * a.ld, a.n};
 }
 
 template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_best_kernel(SampleLaunch a, Parts parts)
@@ -461,16 +472,8 @@ __device__ __forceinline__ uint64_t best_key(const RowSpace &ws, int S)
     return wave_max(k);
 }
 
-// The row's best logit and scale; false if nothing is left to draw (no
-// candidate, or the best one).
-template <bool BF16> __device__ __forceinline__ bool begin(Row<BF16> &row, uint64_t best, Settings st, int64_t n)
-{
-    if (best == 0 || !(st.t > 0.0)) return false;
-    row.best = key_logit(best);
-    row.inv_t = inverse(st.t);
-    row.one = ldexp(1.0, fixed_shift(n));
-    return true;
-}
+// Whether a row has more to draw than its best candidate, or none.
+__device__ __forceinline__ bool open(uint64_t best, Settings st) { return best != 0 && st.t > 0.0; }
 
 template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_bins_kernel(SampleLaunch a, Parts parts)
 {
@@ -482,12 +485,16 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_bins_ke
     const int b = parts.b0 + blockIdx.y, tid = threadIdx.x;
     RowSpace &ws = parts.ws[blockIdx.y];
     const Settings st = settings(a.prm, b);
-    Row<BF16> row = row_of<BF16>(a, b);
+    const Row<BF16> row = row_of<BF16>(a, b);
     for (int i = tid; i < kBins / 2; i += kRowThreads) reinterpret_cast<ulonglong2 *>(s_sum)[i] = {0, 0};
     for (int i = tid; i < kBins / 4; i += kRowThreads) reinterpret_cast<uint4 *>(s_count)[i] = {0, 0, 0, 0};
     if (tid < 64) s_exp[tid] = kExp2.v[tid];
     if (tid == 0) s_pass = 0;
-    if (!begin(row, best_key(ws, gridDim.x), st, a.n)) return;
+    const uint64_t best = best_key(ws, gridDim.x);
+    if (!open(best, st)) return;
+    const Weights weights(key_logit(best), st.t, fixed_shift(a.n), s_exp);
+    const double least = weights.least(st.m);
+    const float top = bin_best(best);
     __syncthreads();
     uint32_t pass = 0;
     const int64_t i0 = blockIdx.x * parts.len;
@@ -497,10 +504,10 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_bins_ke
         uint64_t units[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) {  // (without branches, so that their latencies overlap)
-            bin[e] = bin_of(row.best, l[e]);
-            const double w = weight(l[e], row.best, row.inv_t, s_exp);
-            pass += candidate(l[e]) & (w >= st.m);
-            units[e] = fixed(w, row.one);
+            bin[e] = bin_of(top, l[e]);
+            const double w = weights.real(l[e]);
+            pass += candidate(l[e]) & (w >= least);
+            units[e] = Weights::round(w);
         }
 #pragma unroll
         for (int e = 0; e < N; ++e)
@@ -625,12 +632,14 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     const uint32_t pass = ws.pass;
     const Settings st = settings(a.prm, b);
     const float u = a.u[b];
-    Row<BF16> row = row_of<BF16>(a, b);
+    const Row<BF16> row = row_of<BF16>(a, b);
     const uint64_t best = best_key(ws, S);
-    if (!begin(row, best, st, a.n)) {
+    if (!open(best, st)) {
         if (blockIdx.x == 0 && tid == 0) put(a, b, best == 0 ? Result{-1, 0.0f, 0} : Result{key_id(best), 1.0f, 1});
         return;
     }
+    const Weights weights(key_logit(best), st.t, fixed_shift(a.n));
+    const float top = bin_best(best);
 #pragma unroll
     for (int i = 0; i < kBinsPer; ++i) {
         c += cnt[i];
@@ -750,16 +759,25 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     __syncthreads();
     if (M > kCollect || nslot > kMaxSlots) {  // (the same in every workgroup of the row)
         if (blockIdx.x != 0) return;
-        const Result r = draw_by_digits(row, st, u, live, total, pass, s.digits);
+        const Result r = draw_by_digits(row, weights, st, u, live, total, pass, s.digits);
         if (tid == 0) put(a, b, r);
         return;
     }
 
     // collect: this part's in LDS, then all parts' in the workspace
     const int64_t i0 = blockIdx.x * parts.len;
-    row.each(i0, min(parts.len, a.n - i0), [&](float l, int32_t id) {
-        const int bin = bin_of(row.best, l);
-        if (s.d.flag[bin / 32] >> (bin % 32) & 1) s.d.key[atomicAdd(&s.base, 1u)] = make_key(l, id);
+    row.groups(i0, min(parts.len, a.n - i0), [&](const float *l, int32_t id, auto count) {
+        constexpr int N = decltype(count)::value;
+        uint32_t hit = 0;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const int bin = bin_of(top, l[e]);
+            hit |= (s.d.flag[bin / 32] >> (bin % 32) & (uint32_t)candidate(l[e])) << e;
+        }
+        if (hit)
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (hit >> e & 1) s.d.key[atomicAdd(&s.base, 1u)] = make_key(l[e], id + e);
     });
     __syncthreads();
     if (S > 1) {
@@ -801,7 +819,7 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     for (int h = 0; h < kCollect / kRowThreads; ++h) {
         const int i = h * kRowThreads + tid;
         if (h * kRowThreads >= P) break;
-        uint64_t w = wave_scan(i < (int)M ? row.units(key_logit(s.d.key[i])) : 0ull);
+        uint64_t w = wave_scan(i < (int)M ? weights.units(key_logit(s.d.key[i])) : 0ull);
         if ((tid & (kLanes - 1)) == kLanes - 1) s.wave_sum[tid / kLanes] = w;
         __syncthreads();
         w += base;
@@ -859,7 +877,7 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
         end = s.found_sum;
     }
     first(false, past(end));
-    if (tid == 0) put(a, b, drawn(row, s.found_key, end, kept));
+    if (tid == 0) put(a, b, drawn(weights, s.found_key, end, kept));
 }
 
 vie_status launched(const char *what)
