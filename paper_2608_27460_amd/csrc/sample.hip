@@ -254,10 +254,11 @@ template <int NT> __global__ __launch_bounds__(NT) void sample_list_kernel(Sampl
 //                      sums, from those of the bins before, give the exact
 //                      borders.
 //
-// A bin is the leading bits of the fp32 distance: 1024 to the octave from 1/8
-// to 32, so that the bins are finest where the candidates are few and weigh
-// most.  A border in the bulk of 262144 normal logits meets some 400
-// candidates of its bin.  Rows whose border bins hold more than kCollect
+// A bin of an fp32 row is the leading bits of the distance: 1024 to the
+// octave from 1/8 to 32, so that the bins are finest where the candidates are
+// few and weigh most.  A bf16 row has few enough values for a bin each; its
+// candidates are counted only, and weighed by the bin.  A border in the bulk
+// of 262144 normal logits meets some 400 candidates of its bin.  Rows whose border bins hold more than kCollect
 // (constant rows, or spreads far from a model's) take the borders one after
 // the other from histograms of the keys' digits: exact too, in up to 24
 // passes of one workgroup.
@@ -273,15 +274,43 @@ constexpr int kMaxParts = 128;
 constexpr int kMaxSlots = 256;             // bins that borders can fall into
 constexpr int kMaxRows = 1024;             // rows of one round of launches (114 KB of workspace each)
 
-// The bin of a logit: monotone, bin 0 the best (`top`: the best logit by
-// bin_best, so that infinite ones give no NaN; NaN gives the last bin).
-__device__ __forceinline__ float bin_best(uint64_t best) { return fminf(key_logit(best), __FLT_MAX__); }
-__device__ __forceinline__ int bin_of(float top, float l)
-{
-    constexpr int kFirst = 124 << 10;  // 2^-3: exponent 124, ten mantissa bits
-    const int x = (int)(__float_as_uint(top - fminf(l, __FLT_MAX__)) >> 13) - kFirst + 1;
-    return x < 0 ? 0 : x > kBins - 1 ? kBins - 1 : x;
-}
+// Bins of a row of this best key: `of` is monotone in the logit and 0 at the
+// best one.
+template <bool BF16> struct Bins;
+
+// fp32: the distance's leading bits.  Infinite logits count as the largest
+// finite one, so that none is NaN; a NaN falls into the last bin.
+template <> struct Bins<false> {
+    float top;
+    __device__ __forceinline__ explicit Bins(uint64_t best) : top(fminf(key_logit(best), __FLT_MAX__)) {}
+    __device__ __forceinline__ int of(float l) const
+    {
+        constexpr int kFirst = 124 << 10;  // 2^-3: exponent 124, ten mantissa bits
+        const int x = (int)(__float_as_uint(top - fminf(l, __FLT_MAX__)) >> 13) - kFirst + 1;
+        return x < 0 ? 0 : x > kBins - 1 ? kBins - 1 : x;
+    }
+};
+
+// bf16: a bin for each value of 2^-6 and more in size, one for those between,
+// the last one for all from 8191 values below the best.
+template <> struct Bins<true> {
+    static constexpr int kSmall = 121 << 7;  // the bits of 2^-6
+    int top;
+    __device__ __forceinline__ explicit Bins(uint64_t best) : top(place(key_logit(best))) {}
+    static __device__ __forceinline__ int place(float l)
+    {
+        const int m = max((int)(__float_as_uint(l) >> 16 & 0x7FFF) - kSmall + 1, 0);
+        return __float_as_int(l) < 0 ? -m : m;
+    }
+    __device__ __forceinline__ int of(float l) const { return min(max(top - place(l), 0), kBins - 1); }
+    // whether a bin holds one value, and that value
+    __device__ __forceinline__ bool one(int bin) const { return bin != top && bin != kBins - 1; }
+    __device__ __forceinline__ float value(int bin) const
+    {
+        const int at = top - bin;
+        return from_bf16((uint32_t)(at < 0 ? 0x8000 - at - 1 + kSmall : at - 1 + kSmall));
+    }
+};
 
 // A row's part of the workspace.
 struct RowSpace {
@@ -478,15 +507,16 @@ __device__ __forceinline__ bool open(uint64_t best, Settings st) { return best !
 template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_bins_kernel(SampleLaunch a, Parts parts)
 {
     extern __shared__ __align__(16) char smem[];
+    constexpr int kSums = BF16 ? 2 : kBins;  // (bf16: of the bins of more than one value)
     uint64_t *s_sum = reinterpret_cast<uint64_t *>(smem);
-    uint32_t *s_count = reinterpret_cast<uint32_t *>(s_sum + kBins);
+    uint32_t *s_count = reinterpret_cast<uint32_t *>(s_sum + kSums);
     __shared__ double s_exp[64];
     __shared__ uint32_t s_pass;
     const int b = parts.b0 + blockIdx.y, tid = threadIdx.x;
     RowSpace &ws = parts.ws[blockIdx.y];
     const Settings st = settings(a.prm, b);
     const Row<BF16> row = row_of<BF16>(a, b);
-    for (int i = tid; i < kBins / 2; i += kRowThreads) reinterpret_cast<ulonglong2 *>(s_sum)[i] = {0, 0};
+    for (int i = tid; i < kSums / 2; i += kRowThreads) reinterpret_cast<ulonglong2 *>(s_sum)[i] = {0, 0};
     for (int i = tid; i < kBins / 4; i += kRowThreads) reinterpret_cast<uint4 *>(s_count)[i] = {0, 0, 0, 0};
     if (tid < 64) s_exp[tid] = kExp2.v[tid];
     if (tid == 0) s_pass = 0;
@@ -494,7 +524,7 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_bins_ke
     if (!open(best, st)) return;
     const Weights weights(key_logit(best), st.t, fixed_shift(a.n), s_exp);
     const double least = weights.least(st.m);
-    const float top = bin_best(best);
+    const Bins<BF16> bin_map(best);
     __syncthreads();
     uint32_t pass = 0;
     const int64_t i0 = blockIdx.x * parts.len;
@@ -502,28 +532,58 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_bins_ke
         constexpr int N = decltype(count)::value;
         int bin[N];
         uint64_t units[N];
+        if constexpr (BF16) {
 #pragma unroll
-        for (int e = 0; e < N; ++e) {  // (without branches, so that their latencies overlap)
-            bin[e] = bin_of(top, l[e]);
-            const double w = weights.real(l[e]);
-            pass += candidate(l[e]) & (w >= least);
-            units[e] = Weights::round(w);
-        }
+            for (int e = 0; e < N; ++e) bin[e] = bin_map.of(l[e]);
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-            if (candidate(l[e])) {
+            for (int e = 0; e < N; ++e) {
+                if (!candidate(l[e])) continue;
                 atomicAdd(&s_count[bin[e]], 1u);
-                atomicAdd((unsigned long long *)&s_sum[bin[e]], (unsigned long long)units[e]);
+                if (!bin_map.one(bin[e])) {
+                    const double w = weights.real(l[e]);
+                    pass += w >= least;
+                    atomicAdd((unsigned long long *)&s_sum[bin[e] != bin_map.top], (unsigned long long)Weights::round(w));
+                }
             }
-    });
-    pass = wave_sum(pass);
-    if ((tid & (kLanes - 1)) == 0) atomicAdd(&s_pass, pass);
-    __syncthreads();
-    for (int i = tid; i < kBins; i += kRowThreads)
-        if (s_count[i]) {
-            atomicAdd(&ws.count[i], s_count[i]);
-            atomicAdd((unsigned long long *)&ws.sum[i], (unsigned long long)s_sum[i]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {  // (without branches, so that their latencies overlap)
+                bin[e] = bin_map.of(l[e]);
+                const double w = weights.real(l[e]);
+                pass += candidate(l[e]) & (w >= least);
+                units[e] = Weights::round(w);
+            }
+#pragma unroll
+            for (int e = 0; e < N; ++e)
+                if (candidate(l[e])) {
+                    atomicAdd(&s_count[bin[e]], 1u);
+                    atomicAdd((unsigned long long *)&s_sum[bin[e]], (unsigned long long)units[e]);
+                }
         }
+    });
+    __syncthreads();
+#pragma unroll 1
+    for (int i = tid; i < kBins; i += kRowThreads) {
+        const uint32_t n = s_count[i];
+        if (n == 0) continue;
+        uint64_t sum;
+        if constexpr (BF16) {
+            if (bin_map.one(i)) {
+                const double w = weights.real(bin_map.value(i));
+                if (w >= least) pass += n;
+                sum = Weights::round(w) * n;
+            } else {
+                sum = s_sum[i != bin_map.top];
+            }
+        } else {
+            sum = s_sum[i];
+        }
+        atomicAdd(&ws.count[i], n);
+        atomicAdd((unsigned long long *)&ws.sum[i], (unsigned long long)sum);
+    }
+    pass = wave_sum(pass);
+    if ((tid & (kLanes - 1)) == 0 && pass) atomicAdd(&s_pass, pass);
+    __syncthreads();
     if (tid == 0) atomicAdd(&ws.pass, s_pass);
 }
 
@@ -639,7 +699,7 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
         return;
     }
     const Weights weights(key_logit(best), st.t, fixed_shift(a.n));
-    const float top = bin_best(best);
+    const Bins<BF16> bin_map(best);
 #pragma unroll
     for (int i = 0; i < kBinsPer; ++i) {
         c += cnt[i];
@@ -771,7 +831,7 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
         uint32_t hit = 0;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const int bin = bin_of(top, l[e]);
+            const int bin = bin_map.of(l[e]);
             hit |= (s.d.flag[bin / 32] >> (bin % 32) & (uint32_t)candidate(l[e])) << e;
         }
         if (hit)
@@ -907,7 +967,7 @@ template <bool BF16> vie_status rows_launch(const SampleLaunch &a, hipStream_t s
     const int64_t want = std::min<int64_t>((a.n + 4095) / 4096, 256 / a.B);
     const int S = (int)std::max<int64_t>(1, std::min<int64_t>(want, kMaxParts));
     const int64_t len = ((a.n + S - 1) / S + 63) / 64 * 64;
-    constexpr int kBinsLds = kBins * 12;
+    constexpr int kBinsLds = kBins * 4 + (BF16 ? 2 : kBins) * 8;
     hipError_t e = hipFuncSetAttribute((const void *)rows_draw_kernel<BF16>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                        (int)sizeof(DrawLds));
     if (e == hipSuccess)
