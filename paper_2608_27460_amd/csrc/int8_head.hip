@@ -148,6 +148,11 @@ __global__ __launch_bounds__(256) void int8_simple_kernel(const int8_t *__restri
 // rows and tokens past the tile re-read its last one, and their results are
 // not stored.
 //
+// A few tokens (HELD) stay in LDS throughout, quantized there by every
+// workgroup while its first rows are on their way, which saves the launch of
+// tokens_kernel and the tokens' staging.  Rows that are not 16-byte aligned
+// (DMA false) go to LDS by way of registers, two stages ahead.
+//
 // The logits leave through 4 KB of LDS of each wave's own, 16 tokens at a
 // time, so that a store covers runs of 256 bytes of a token's row; the
 // stages of the next tile go on arriving meanwhile.
@@ -165,8 +170,56 @@ __device__ __forceinline__ void load_lds16(const int8_t *src, char *dst)
                                      (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
 }
 
+constexpr int kHeldLds = 32 * 1024;  // for the held tokens and their scales
+constexpr int kHeldPad = 16;         // bytes between them: 16 rows' reads hit every bank once
 constexpr int tile_stage(int BT, int KC) { return (kTileRows + BT) * KC; }
-constexpr int tile_lds(int BT, int KC, int NBUF) { return tile_stage(BT, KC) * NBUF + kWaves * 4096; }
+constexpr int tile_lds(int stage, int NBUF, bool held) { return stage * NBUF + kWaves * 4096 + (held ? kHeldLds : 0); }
+__host__ __device__ inline bool tokens_fit(int B, int d) { return B <= 16 && B * (padded(d) + kHeldPad) + 64 <= kHeldLds; }
+
+// The tokens' int8 values at tok + b (padded(d) + kHeldPad) and their scales
+// behind them, by tokens_kernel's rule: a wave per token at a time.
+template <bool BF16> __device__ void hold_tokens(const void *h, int B, int d, char *tok, float *s_xs)
+{
+    typedef Elem<BF16> E;
+    const int lane = threadIdx.x & (kLanes - 1), dp = padded(d);
+    for (int b = threadIdx.x / kLanes; b < B; b += kWaves) {
+        const typename E::T *row = static_cast<const typename E::T *>(h) + (int64_t)b * d;
+        auto load8 = [&](int j, float *v) {
+            if (j + 8 <= d) {
+                word4 w[8 / E::kVec];
+                __builtin_memcpy(w, row + j, sizeof w);  // (at any alignment)
+#pragma unroll
+                for (int k = 0; k < 8 / E::kVec; ++k) E::unpack(w[k], v + k * E::kVec);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = j + e < d ? E::get(row[j + e]) : 0.0f;
+            }
+        };
+        float top = 0.0f;
+        bool bad = false;
+        for (int j = 8 * lane; j < d; j += 8 * kLanes) {
+            float v[8];
+            load8(j, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                bad |= !(fabsf(v[e]) < __builtin_inff());
+                top = fmaxf(top, fabsf(v[e]));
+            }
+        }
+        top = wave_max(top);
+        bad = __any(bad);
+        const float scale = bad ? 0.0f : __fdiv_rn(top, 127.0f);
+        for (int j = 8 * lane; j < dp; j += 8 * kLanes) {
+            float v[8];
+            load8(j, v);
+            uint64_t w = 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) w |= (uint64_t)(uint8_t)quantized(v[e], scale) << 8 * e;
+            *reinterpret_cast<uint64_t *>(tok + b * (dp + kHeldPad) + j) = w;
+        }
+        if (lane == 0) s_xs[b] = bad ? __builtin_nanf("") : scale;
+    }
+}
 
 // Tile t of a workgroup: XCD blockIdx.x % 8 takes a run of the tiles, its
 // workgroups take every 32nd of them, and the order goes over up to eight
@@ -177,19 +230,23 @@ struct Tiles {
     int per_xcd, step; // tiles of an XCD's run, its workgroups
 };
 
-template <int MT, int NT, int WB, int KC, int NBUF, bool AHEAD, bool OUT_BF16>
+template <int MT, int NT, int WB, int KC, int NBUF, bool AHEAD, bool HELD, bool DMA, bool OUT_BF16>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void int8_tile_kernel(
     const int8_t *__restrict__ q, int pitch, const float *__restrict__ scale, int64_t V, const int8_t *__restrict__ x,
-    int dp, const float *__restrict__ xs, int B, typename Elem<OUT_BF16>::T *__restrict__ out, int64_t ld, Tiles tiles)
+    int dp, const float *__restrict__ xs, const void *__restrict__ h, int h_bf16, int d, int B, typename Elem<OUT_BF16>::T *__restrict__ out, int64_t ld, Tiles tiles)
 {
     typedef Elem<OUT_BF16> E;
     extern __shared__ __align__(16) char smem[];
     constexpr int BT = 16 * NT * WB;
     static_assert(kWaves / WB * MT * 16 == kTileRows, "the waves cover a tile");
-    constexpr int kStage = tile_stage(BT, KC), P = KC / 16, LR = kLanes / P, KS = KC / kStep;
-    constexpr int WL = kTileRows / kWaves / LR;                      // loads of a wave's rows per stage
-    constexpr int XR = BT / kWaves, XL = (XR + LR - 1) / LR;         // tokens a wave stages, their loads
+    static_assert(DMA || (HELD && !AHEAD && NBUF == 2), "rows by way of registers take two buffers");
+    static_assert(!HELD || BT == 16, "held tokens are one operand");
+    constexpr int kStage = tile_stage(HELD ? 0 : BT, KC), P = KC / 16, LR = kLanes / P, KS = KC / kStep;
+    constexpr int WL = kTileRows / kWaves / LR;                              // loads of a wave's rows per stage
+    constexpr int XR = BT / kWaves, XL = HELD ? 0 : (XR + LR - 1) / LR;      // tokens a wave stages, their loads
     constexpr int L = WL + XL;
+    char *tok = smem + NBUF * kStage + kWaves * 4096;                        // (HELD)
+    float *s_xs = reinterpret_cast<float *>(tok + B * (dp + kHeldPad));
     const int tid = threadIdx.x, lane = tid & (kLanes - 1), r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kLanes);
     const int wv = wave / WB, wb = wave % WB;
@@ -207,8 +264,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     };
 
     const int lrow = lane / P, slot = lane % P;
-    const int8_t *wsrc[WL], *xsrc[XL];
-    int wcol[WL], xcol[XL];
+    const int8_t *wsrc[WL], *xsrc[XL + 1];
+    int wcol[WL], xcol[XL + 1];
 #pragma unroll
     for (int t = 0; t < WL; ++t) wcol[t] = 16 * (slot ^ swizzle<KC>(LR * t + lrow));
 #pragma unroll
@@ -225,16 +282,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         for (int i = 0; i < XL; ++i) xsrc[i] = x + (int64_t)min(b0 + wave * XR + LR * i + lrow, B - 1) * dp;
     };
     int lt = first, lst = 0;  // the stage to load next
+    word4 hold[DMA ? 1 : 2][WL];
     auto load_next = [&](int buf) {
         char *dst = smem + buf * kStage;
         const int c = lst * KC;
+        if constexpr (DMA) {
 #pragma unroll
-        for (int i = 0; i < WL; ++i)
-            load_lds16(wsrc[i] + min(c + wcol[i], pitch - 16), dst + (wave * (kTileRows / kWaves) + LR * i) * KC);
+            for (int i = 0; i < WL; ++i)
+                load_lds16(wsrc[i] + min(c + wcol[i], pitch - 16), dst + (wave * (kTileRows / kWaves) + LR * i) * KC);
 #pragma unroll
-        for (int i = 0; i < XL; ++i)
-            if (XR >= LR || lane < XR * P)
-                load_lds16(xsrc[i] + c + xcol[i], dst + (kTileRows + wave * XR + LR * i) * KC);
+            for (int i = 0; i < XL; ++i)
+                if (XR >= LR || lane < XR * P)
+                    load_lds16(xsrc[i] + c + xcol[i], dst + (kTileRows + wave * XR + LR * i) * KC);
+        } else {  // (pieces past a row: any bytes)
+#pragma unroll
+            for (int i = 0; i < WL; ++i) hold[buf][i] = load16(wsrc[i] + (c + wcol[i] < pitch ? c + wcol[i] : 0), q + V * pitch);
+        }
         if (++lst == nstage) {  // past the last tile: its stages again, unused
             lst = 0;
             if (lt + tiles.step < end) lt += tiles.step;
@@ -244,14 +307,18 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     struct Operands {
         word4 a[KS][MT], b[KS][NT];
     };
+    int rst = 0;  // the stage to read next
     auto read = [&](int buf, Operands &o) {
         const char *A = smem + buf * kStage + (wv * MT * 16 + r) * KC;
-        const char *X = smem + buf * kStage + (kTileRows + wb * NT * 16 + r) * KC;
+        const char *X = HELD ? tok + min(r, B - 1) * (dp + kHeldPad) + rst * KC
+                             : smem + buf * kStage + (kTileRows + wb * NT * 16 + r) * KC;
+        rst = rst == nstage - 1 ? 0 : rst + 1;
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             const int at = 16 * ((4 * k + g) ^ swizzle<KC>(r));
 #pragma unroll
-            for (int n = 0; n < NT; ++n) o.b[k][n] = *reinterpret_cast<const word4 *>(X + n * 16 * KC + at);
+            for (int n = 0; n < NT; ++n)
+                o.b[k][n] = *reinterpret_cast<const word4 *>(X + (HELD ? kStep * k + 16 * g : n * 16 * KC + at));
 #pragma unroll
             for (int m = 0; m < MT; ++m) o.a[k][m] = *reinterpret_cast<const word4 *>(A + m * 16 * KC + at);
         }
@@ -283,7 +350,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
         for (int i = 0; i < kScales; ++i) sc[i] = scale[min<int64_t>(v0 + wv * MT * 16 + i * kLanes + lane, V - 1)];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) xf[n] = xs[min(b0 + (wb * NT + n) * 16 + r, B - 1)];
+        for (int n = 0; n < NT; ++n) xf[n] = HELD ? s_xs[min(r, B - 1)] : xs[min(b0 + (wb * NT + n) * 16 + r, B - 1)];
     };
     // lane (r, g) holds rows 4 g + i of row tile m for token 16 n + r
     constexpr int kHalves = OUT_BF16 ? 1 : 2, kPer = MT / kHalves;  // a token's run: kPer row tiles
@@ -363,9 +430,43 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 
     set_tile(first);
 #pragma unroll
-    for (int i = 0; i < NBUF - !AHEAD; ++i) load_next(i);
+    for (int i = 0; i < (DMA ? NBUF - !AHEAD : 2); ++i) load_next(i);
+    if constexpr (HELD) {
+        if (h_bf16) hold_tokens<true>(h, B, d, tok, s_xs);
+        else hold_tokens<false>(h, B, d, tok, s_xs);
+        __syncthreads();
+    }
     int buf = 0, stored = 0, t = first, st = 0;
     Operands now, next;
+    if constexpr (!DMA) {
+        // Stage s is read from buffer s % 2 while stage s + 1 goes from its
+        // registers to the other one and s + 3 is loaded into them.
+        auto put = [&](int to) {
+            char *dst = smem + to * kStage + wave * (kTileRows / kWaves) * KC + 16 * lane;
+#pragma unroll
+            for (int i = 0; i < WL; ++i) *reinterpret_cast<word4 *>(dst + LR * i * KC) = hold[to][i];
+        };
+        put(0);
+        load_next(0);
+        auto step = [&](int b) {
+            __syncthreads();
+            if (st == nstage - 1) load_scales(t);
+            read(b, now);
+            put(1 - b);
+            load_next(1 - b);
+            multiply(now);
+            if (++st == nstage) {
+                store(t);
+                st = 0;
+                t += tiles.step;
+                return t < end;
+            }
+            return true;
+        };
+        while (step(0) && step(1)) {
+        }
+        return;
+    }
     if constexpr (AHEAD) {
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"((NBUF - 1) * L) : "memory");
         __builtin_amdgcn_s_barrier();
@@ -423,16 +524,14 @@ size_t tokens_bytes(int d, int B) { return ((size_t)B * padded(d) + 255) & ~(siz
 
 }  // namespace
 
-// The tokens' int8 values and scales.
-size_t int8_workspace_bytes(int64_t, int d, int B) { return tokens_bytes(d, B) + (size_t)B * 4; }
-
 namespace {
-template <int MT, int NT, int WB, int KC, int NBUF, bool AHEAD, bool OUT_BF16>
-hipError_t tile_launch(const Int8Launch &a, const int8_t *x, const float *xs, bool even, hipStream_t s)
+// `q`: rows of `pitch` bytes, a.q's own or copies of them.
+template <int MT, int NT, int WB, int KC, int NBUF, bool AHEAD, bool HELD, bool DMA, bool OUT_BF16>
+hipError_t tile_launch(const Int8Launch &a, const int8_t *q, int pitch, const int8_t *x, const float *xs, bool even, hipStream_t s)
 {
-    constexpr int BT = 16 * NT * WB, lds = tile_lds(BT, KC, NBUF);
+    constexpr int BT = 16 * NT * WB, lds = tile_lds(tile_stage(HELD ? 0 : BT, KC), NBUF, HELD);
     static_assert(lds <= 160 * 1024, "a tile's stages fit LDS");
-    auto kern = int8_tile_kernel<MT, NT, WB, KC, NBUF, AHEAD, OUT_BF16>;
+    auto kern = int8_tile_kernel<MT, NT, WB, KC, NBUF, AHEAD, HELD, DMA, OUT_BF16>;
     hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
     Tiles t;
@@ -447,38 +546,78 @@ hipError_t tile_launch(const Int8Launch &a, const int8_t *x, const float *xs, bo
     const int64_t n = (int64_t)t.nv * t.nb;
     t.per_xcd = (int)((n + 7) / 8);
     t.step = std::min(kWorkgroups / 8, t.per_xcd);
-    kern<<<8 * t.step, kThreads, lds, s>>>(a.q, a.d, a.scale, a.V, x, padded(a.d), xs, a.B,
+    kern<<<8 * t.step, kThreads, lds, s>>>(q, pitch, a.scale, a.V, x, padded(a.d), xs, a.h, a.h_dtype == VIE_BF16, a.d, a.B,
                                            static_cast<typename Elem<OUT_BF16>::T *>(a.out), a.ld, t);
     return hipGetLastError();
 }
 
-template <bool OUT_BF16> hipError_t tiles_launch(const Int8Launch &a, const int8_t *x, const float *xs, hipStream_t s)
+template <bool OUT_BF16>
+hipError_t tiles_launch(const Int8Launch &a, const int8_t *q, int pitch, const int8_t *x, const float *xs, hipStream_t s)
 {
-    if (a.B <= 16) return tile_launch<2, 1, 1, 128, 3, true, OUT_BF16>(a, x, xs, true, s);
-    if (a.B <= 32) return tile_launch<2, 2, 1, 128, 3, true, OUT_BF16>(a, x, xs, true, s);
-    if (a.B <= 64) return tile_launch<2, 4, 1, 128, 3, true, OUT_BF16>(a, x, xs, true, s);
-    if (a.B <= 128) return tile_launch<4, 4, 2, 64, 4, true, OUT_BF16>(a, x, xs, false, s);
-    return tile_launch<8, 4, 4, 64, 4, false, OUT_BF16>(a, x, xs, false, s);
+    if (a.B <= 16) return tile_launch<2, 1, 1, 128, 3, true, false, true, OUT_BF16>(a, q, pitch, x, xs, true, s);
+    if (a.B <= 32) return tile_launch<2, 2, 1, 128, 3, true, false, true, OUT_BF16>(a, q, pitch, x, xs, true, s);
+    if (a.B <= 64) return tile_launch<2, 4, 1, 128, 3, true, false, true, OUT_BF16>(a, q, pitch, x, xs, true, s);
+    if (a.B <= 128) return tile_launch<4, 4, 2, 64, 4, true, false, true, OUT_BF16>(a, q, pitch, x, xs, false, s);
+    return tile_launch<8, 4, 4, 64, 4, false, false, true, OUT_BF16>(a, q, pitch, x, xs, false, s);
 }
+template <bool OUT_BF16> hipError_t few_launch(const Int8Launch &a, bool aligned, hipStream_t s)
+{
+    if (aligned) return tile_launch<2, 1, 1, 128, 3, true, true, true, OUT_BF16>(a, a.q, a.d, nullptr, nullptr, true, s);
+    return tile_launch<2, 1, 1, 128, 2, false, true, false, OUT_BF16>(a, a.q, a.d, nullptr, nullptr, true, s);
+}
+
+// Rows of d bytes copied to rows of `pitch` bytes, a multiple of 16 (what
+// lies past d meets zeros of the tokens): a wave per row.
+__global__ __launch_bounds__(256) void repack_kernel(const int8_t *__restrict__ q, int64_t V, int d, int8_t *__restrict__ to, int pitch)
+{
+    const int64_t v = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
+    if (v >= V) return;
+    for (int c = 16 * (threadIdx.x & (kLanes - 1)); c < pitch; c += 16 * kLanes)
+        *reinterpret_cast<word4 *>(to + v * pitch + c) = load16(q + v * d + c, q + V * d);
+}
+int row_pitch(int d) { return (d + 15) / 16 * 16; }
+// From so many tokens on, unaligned rows are copied first: read and written
+// once for it, where int8_simple_kernel would read them for every 16 tokens.
+constexpr int kRepackTokens = 33;
 }  // namespace
+
+// The tokens' int8 values and scales, and unaligned rows copied.
+size_t int8_workspace_bytes(int64_t V, int d, int B)
+{
+    if (tokens_fit(B, d)) return 0;
+    const size_t tokens = (tokens_bytes(d, B) + (size_t)B * 4 + 255) & ~(size_t)255;
+    return tokens + (d % 16 && B >= kRepackTokens ? (size_t)V * row_pitch(d) : 0);
+}
 
 vie_status launch_int8_logits(const Int8Launch &a, hipStream_t s)
 {
+    auto done = [](hipError_t e) {
+        return e == hipSuccess ? VIE_OK : fail(VIE_EHIP, "int8 head launch: %s", hipGetErrorString(e));
+    };
+    const bool bf16 = a.out_dtype == VIE_BF16, aligned = a.d % 16 == 0 && (uintptr_t)a.q % 16 == 0;
+    if (tokens_fit(a.B, a.d)) return done(bf16 ? few_launch<true>(a, aligned, s) : few_launch<false>(a, aligned, s));
     int8_t *x = static_cast<int8_t *>(a.ws);
     float *xs = reinterpret_cast<float *>(x + tokens_bytes(a.d, a.B));
     if (a.h_dtype == VIE_BF16) tokens_kernel<true><<<a.B, kTokenThreads, 0, s>>>(static_cast<const uint16_t *>(a.h), a.d, x, xs);
     else tokens_kernel<false><<<a.B, kTokenThreads, 0, s>>>(static_cast<const float *>(a.h), a.d, x, xs);
     if (vie_status e = launched("token quantization launch")) return e;
-    if (a.d % 16 == 0 && (uintptr_t)a.q % 16 == 0) {
-        const hipError_t e = a.out_dtype == VIE_BF16 ? tiles_launch<true>(a, x, xs, s) : tiles_launch<false>(a, x, xs, s);
-        return e == hipSuccess ? VIE_OK : fail(VIE_EHIP, "int8 head launch: %s", hipGetErrorString(e));
+    const int8_t *q = a.q;
+    int pitch = a.d;
+    if (a.d % 16 && a.B >= kRepackTokens) {
+        int8_t *to = x + ((tokens_bytes(a.d, a.B) + (size_t)a.B * 4 + 255) & ~(size_t)255);
+        pitch = row_pitch(a.d);
+        repack_kernel<<<(unsigned)((a.V + 3) / 4), 256, 0, s>>>(a.q, a.V, a.d, to, pitch);
+        if (vie_status e = launched("int8 row copy launch")) return e;
+        q = to;
+    } else if (!aligned) {
+        const dim3 grid((unsigned)((a.V + 63) / 64), (unsigned)((a.B + 15) / 16));
+        if (bf16)
+            int8_simple_kernel<true><<<grid, 256, 0, s>>>(a.q, a.scale, a.V, a.d, x, xs, a.B, static_cast<uint16_t *>(a.out), a.ld);
+        else
+            int8_simple_kernel<false><<<grid, 256, 0, s>>>(a.q, a.scale, a.V, a.d, x, xs, a.B, static_cast<float *>(a.out), a.ld);
+        return launched("int8 head launch");
     }
-    const dim3 grid((unsigned)((a.V + 63) / 64), (unsigned)((a.B + 15) / 16));
-    if (a.out_dtype == VIE_BF16)
-        int8_simple_kernel<true><<<grid, 256, 0, s>>>(a.q, a.scale, a.V, a.d, x, xs, a.B, static_cast<uint16_t *>(a.out), a.ld);
-    else
-        int8_simple_kernel<false><<<grid, 256, 0, s>>>(a.q, a.scale, a.V, a.d, x, xs, a.B, static_cast<float *>(a.out), a.ld);
-    return launched("int8 head launch");
+    return done(bf16 ? tiles_launch<true>(a, q, pitch, x, xs, s) : tiles_launch<false>(a, q, pitch, x, xs, s));
 }
 
 }  // namespace vie

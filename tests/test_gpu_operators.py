@@ -86,6 +86,9 @@ INT8_CASES = [
     (3333, 272, 65, BF16, F32), (1031, 512, 130, F32, BF16), (2111, 640, 300, BF16, BF16), (513, 96, 1000, BF16, F32),
     (300, 33, 2100, F32, BF16), (140000, 48, 9, BF16, F32), (6007, 1536, 33, BF16, F32), (257, 2048, 257, BF16, BF16),
     (129, 4096, 48, BF16, F32), (8200, 128, 8, F32, F32),
+    (4099, 65, 40, F32, BF16), (3001, 1001, 200, BF16, F32), (1500, 8191, 20, F32, F32), (5000, 1000, 16, BF16, BF16),
+    (777, 2040, 16, F32, F32), (9000, 4100, 3, BF16, BF16), (70000, 33, 2, F32, BF16), (3000, 4096, 8, F32, F32),
+    (131073, 16, 1, BF16, F32), (500, 8192, 16, BF16, F32),
 ]
 
 

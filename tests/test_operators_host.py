@@ -14,7 +14,7 @@ PRM = vie.SamplingParams(1.0, 1.0, 0.0, 0)
 BIG = 1 << 40
 
 
-def _int8(q=P, scale=P, V=100, d=64, h=P, ht=vie.BF16, B=2, out=P, ot=vie.F32, ld=100, ws=P, n=BIG):
+def _int8(q=P, scale=P, V=100, d=64, h=P, ht=vie.BF16, B=40, out=P, ot=vie.F32, ld=100, ws=P, n=BIG):
     return L.vie_int8_logits(q, scale, V, d, h, ht, B, out, ot, ld, ws, n, None)
 
 
@@ -85,7 +85,8 @@ def test_distill_refuses_results_and_overlaps():
 
 def test_workspace_queries():
     n = C.c_size_t()
-    assert L.vie_int8_logits_workspace(1000, 64, 3, C.byref(n)) == vie.OK and n.value >= 3 * 64
+    assert L.vie_int8_logits_workspace(1000, 64, 40, C.byref(n)) == vie.OK and n.value >= 40 * 64
+    assert L.vie_int8_logits_workspace(1000, 64, 3, C.byref(n)) == vie.OK and n.value == 0
     assert L.vie_sample_rows_workspace(1000, 3, C.byref(n)) == vie.OK
     assert L.vie_distill_workspace(1000, 3, C.byref(n)) == vie.OK
     for f, args in ((L.vie_int8_logits_workspace, (0, 64, 3)), (L.vie_int8_logits_workspace, (10, 0, 3)),
