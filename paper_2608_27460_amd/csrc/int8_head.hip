@@ -153,9 +153,8 @@ __global__ __launch_bounds__(256) void int8_simple_kernel(const int8_t *__restri
 // tokens_kernel and the tokens' staging.  Rows that are not 16-byte aligned
 // (DMA false) go to LDS by way of registers, two stages ahead.
 //
-// The logits leave through 4 KB of LDS of each wave's own, 16 tokens at a
-// time, so that a store covers runs of 256 bytes of a token's row; the
-// stages of the next tile go on arriving meanwhile.
+// The logits leave through LDS of each wave's own, 16 tokens at a time, so
+// that a store covers runs of up to 256 bytes of a token's row; the stages of the next tile go on arriving meanwhile.
 
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kLanes;
@@ -170,11 +169,15 @@ __device__ __forceinline__ void load_lds16(const int8_t *src, char *dst)
                                      (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
 }
 
-constexpr int kHeldLds = 32 * 1024;  // for the held tokens and their scales
+constexpr int kHeldLds = 56 * 1024;  // for the held tokens and their scales
 constexpr int kHeldPad = 16;         // bytes between them: 16 rows' reads hit every bank once
 constexpr int tile_stage(int BT, int KC) { return (kTileRows + BT) * KC; }
-constexpr int tile_lds(int stage, int NBUF, bool held) { return stage * NBUF + kWaves * 4096 + (held ? kHeldLds : 0); }
-__host__ __device__ inline bool tokens_fit(int B, int d) { return B <= 16 && B * (padded(d) + kHeldPad) + 64 <= kHeldLds; }
+constexpr int tile_out(int MT) { return 512 * MT; }  // of a wave, for its logits on their way out
+constexpr int tile_lds(int stage, int NBUF, int MT, bool held) { return stage * NBUF + kWaves * tile_out(MT) + (held ? kHeldLds : 0); }
+inline bool tokens_fit(int64_t V, int B, int d)  // (and there are 16 bytes of rows, a load)
+{
+    return B <= 16 && B * (padded(d) + kHeldPad) + 64 <= kHeldLds && V * d >= 16;
+}
 
 // The tokens' int8 values at tok + b (padded(d) + kHeldPad) and their scales
 // behind them, by tokens_kernel's rule: a wave per token at a time.
@@ -245,7 +248,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     constexpr int WL = kTileRows / kWaves / LR;                              // loads of a wave's rows per stage
     constexpr int XR = BT / kWaves, XL = HELD ? 0 : (XR + LR - 1) / LR;      // tokens a wave stages, their loads
     constexpr int L = WL + XL;
-    char *tok = smem + NBUF * kStage + kWaves * 4096;                        // (HELD)
+    char *tok = smem + NBUF * kStage + kWaves * tile_out(MT);                // (HELD)
     float *s_xs = reinterpret_cast<float *>(tok + B * (dp + kHeldPad));
     const int tid = threadIdx.x, lane = tid & (kLanes - 1), r = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid / kLanes);
@@ -296,7 +299,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
                     load_lds16(xsrc[i] + c + xcol[i], dst + (kTileRows + wave * XR + LR * i) * KC);
         } else {  // (pieces past a row: any bytes)
 #pragma unroll
-            for (int i = 0; i < WL; ++i) hold[buf][i] = load16(wsrc[i] + (c + wcol[i] < pitch ? c + wcol[i] : 0), q + V * pitch);
+            for (int i = 0; i < WL; ++i) {
+                const int8_t *p = wsrc[i] + (c + wcol[i] < pitch ? c + wcol[i] : 0), *last = q + V * pitch - 16;
+                __builtin_memcpy(&hold[buf][i], p < last ? p : last, 16);
+            }
         }
         if (++lst == nstage) {  // past the last tile: its stages again, unused
             lst = 0;
@@ -363,7 +369,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         const int64_t vend = min<int64_t>(V, v0 + tiles.rows);
         v0 += wv * MT * 16;
         b0 += wb * NT * 16;
-        char *tmp = smem + NBUF * kStage + wave * 4096;
+        char *tmp = smem + NBUF * kStage + wave * tile_out(MT);
         // (this lane's addresses are made here: kept over the stages they
         // would take the registers that the operands need)
         int lane = threadIdx.x & (kLanes - 1);
@@ -441,10 +447,34 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
     if constexpr (!DMA) {
         // Stage s is read from buffer s % 2 while stage s + 1 goes from its
         // registers to the other one and s + 3 is loaded into them.
+        int pt = first, pst = 0;  // the stage to put
         auto put = [&](int to) {
             char *dst = smem + to * kStage + wave * (kTileRows / kWaves) * KC + 16 * lane;
+            int64_t v0;
+            int b0;
+            place(pt, v0, b0);
+            if (v0 + tiles.rows >= V) {
+                // Pieces that would end past the matrix were loaded before its
+                // end: their bytes move to where they belong.
+#pragma unroll
+                for (int i = 0; i < WL; ++i) {
+                    const int64_t v = min<int64_t>(v0 + wave * (kTileRows / kWaves) + LR * i + lrow, V - 1);
+                    const int col = pst * KC + wcol[i];
+                    const int64_t by = v * pitch + (col < pitch ? col : 0) - (V * pitch - 16);
+                    if (by <= 0) continue;
+                    word4 w = hold[to][i];
+                    for (int64_t k = 0; k < by; ++k) {
+                        w.x = w.x >> 8 | w.y << 24;
+                        w.y = w.y >> 8 | w.z << 24;
+                        w.z = w.z >> 8 | w.w << 24;
+                        w.w >>= 8;
+                    }
+                    hold[to][i] = w;
+                }
+            }
 #pragma unroll
             for (int i = 0; i < WL; ++i) *reinterpret_cast<word4 *>(dst + LR * i * KC) = hold[to][i];
+            if (++pst == nstage) pst = 0, pt += tiles.step;
         };
         put(0);
         load_next(0);
@@ -529,7 +559,7 @@ namespace {
 template <int MT, int NT, int WB, int KC, int NBUF, bool AHEAD, bool HELD, bool DMA, bool OUT_BF16>
 hipError_t tile_launch(const Int8Launch &a, const int8_t *q, int pitch, const int8_t *x, const float *xs, bool even, hipStream_t s)
 {
-    constexpr int BT = 16 * NT * WB, lds = tile_lds(tile_stage(HELD ? 0 : BT, KC), NBUF, HELD);
+    constexpr int BT = 16 * NT * WB, lds = tile_lds(tile_stage(HELD ? 0 : BT, KC), NBUF, MT, HELD);
     static_assert(lds <= 160 * 1024, "a tile's stages fit LDS");
     auto kern = int8_tile_kernel<MT, NT, WB, KC, NBUF, AHEAD, HELD, DMA, OUT_BF16>;
     hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
@@ -558,7 +588,7 @@ hipError_t tiles_launch(const Int8Launch &a, const int8_t *q, int pitch, const i
     if (a.B <= 32) return tile_launch<2, 2, 1, 128, 3, true, false, true, OUT_BF16>(a, q, pitch, x, xs, true, s);
     if (a.B <= 64) return tile_launch<2, 4, 1, 128, 3, true, false, true, OUT_BF16>(a, q, pitch, x, xs, true, s);
     if (a.B <= 128) return tile_launch<4, 4, 2, 64, 4, true, false, true, OUT_BF16>(a, q, pitch, x, xs, false, s);
-    return tile_launch<8, 4, 4, 64, 4, false, false, true, OUT_BF16>(a, q, pitch, x, xs, false, s);
+    return tile_launch<8, 4, 4, 128, 2, false, false, true, OUT_BF16>(a, q, pitch, x, xs, false, s);
 }
 template <bool OUT_BF16> hipError_t few_launch(const Int8Launch &a, bool aligned, hipStream_t s)
 {
@@ -584,7 +614,7 @@ constexpr int kRepackTokens = 33;
 // The tokens' int8 values and scales, and unaligned rows copied.
 size_t int8_workspace_bytes(int64_t V, int d, int B)
 {
-    if (tokens_fit(B, d)) return 0;
+    if (tokens_fit(V, B, d)) return 0;
     const size_t tokens = (tokens_bytes(d, B) + (size_t)B * 4 + 255) & ~(size_t)255;
     return tokens + (d % 16 && B >= kRepackTokens ? (size_t)V * row_pitch(d) : 0);
 }
@@ -595,7 +625,7 @@ vie_status launch_int8_logits(const Int8Launch &a, hipStream_t s)
         return e == hipSuccess ? VIE_OK : fail(VIE_EHIP, "int8 head launch: %s", hipGetErrorString(e));
     };
     const bool bf16 = a.out_dtype == VIE_BF16, aligned = a.d % 16 == 0 && (uintptr_t)a.q % 16 == 0;
-    if (tokens_fit(a.B, a.d)) return done(bf16 ? few_launch<true>(a, aligned, s) : few_launch<false>(a, aligned, s));
+    if (tokens_fit(a.V, a.B, a.d)) return done(bf16 ? few_launch<true>(a, aligned, s) : few_launch<false>(a, aligned, s));
     int8_t *x = static_cast<int8_t *>(a.ws);
     float *xs = reinterpret_cast<float *>(x + tokens_bytes(a.d, a.B));
     if (a.h_dtype == VIE_BF16) tokens_kernel<true><<<a.B, kTokenThreads, 0, s>>>(static_cast<const uint16_t *>(a.h), a.d, x, xs);
