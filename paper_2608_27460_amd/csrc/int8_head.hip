@@ -169,6 +169,16 @@ __device__ __forceinline__ void load_lds16(const int8_t *src, char *dst)
                                      (__attribute__((address_space(3))) void *)dst, 16, 0, 0);
 }
 
+// 16 bytes to any alignment.  PAST: past the caches' keeping, for logits of
+// many tokens, which would push the rows and tokens out of L2 (2048 tokens:
+// 559 us without, 535 with).
+template <bool PAST> __device__ __forceinline__ void store16(char *o, word4 w)
+{
+    typedef word4 any_word4 __attribute__((aligned(2)));
+    if constexpr (PAST) __builtin_nontemporal_store(w, reinterpret_cast<any_word4 *>(o));
+    else __builtin_memcpy(o, &w, 16);
+}
+
 constexpr int kHeldLds = 56 * 1024;  // for the held tokens and their scales
 constexpr int kHeldPad = 16;         // bytes between them: 16 rows' reads hit every bank once
 constexpr int tile_stage(int BT, int KC) { return (kTileRows + BT) * KC; }
@@ -375,6 +385,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         int lane = threadIdx.x & (kLanes - 1);
         asm volatile("" : "+v"(lane));
         const int r = lane & 15, g = lane >> 4;
+        // (a whole tile's stores: one offset a lane, the rest is the wave's)
+        const bool full = v0 + MT * 16 <= vend && b0 + 16 * NT <= B && ld < (1 << 24);
+        char *to = reinterpret_cast<char *>(out + (int64_t)b0 * ld + v0);
+        const uint32_t lane_to = (uint32_t)((lane / kUnits) * (int)ld + lane % kUnits * E::kVec) * (uint32_t)sizeof(typename E::T);
         // the scales to their lanes; the sums become logits in place
 #pragma unroll
         for (int i = 0; i < kScales; ++i) reinterpret_cast<float *>(tmp)[i * kLanes + lane] = sc[i];
@@ -411,16 +425,22 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
                 for (int i = 0; i < 16 * kUnits / kLanes; ++i) {
                     const int row = (i * kLanes + lane) / kUnits, unit = lane % kUnits;
-                    const word4 w = *reinterpret_cast<const word4 *>(tmp + row * (kUnits * 16) + 16 * (unit ^ (row & (kUnits - 1))));
+                    const char *from = tmp + row * (kUnits * 16) + 16 * (unit ^ (row & (kUnits - 1)));
+                    const word4 w = *reinterpret_cast<const word4 *>(from);
+                    if (full) {
+                        char *o = to + ((int64_t)(16 * n + i * (kLanes / kUnits)) * ld + h * kPer * 16) * (int)sizeof(typename E::T);
+                        store16<(WB > 1)>(o + lane_to, w);
+                        continue;
+                    }
                     const int b = b0 + 16 * n + row;
                     const int64_t v = v0 + h * kPer * 16 + unit * E::kVec;
                     typename E::T *o = out + (int64_t)b * ld + v;
                     if (b < B && v + E::kVec <= vend) {
-                        __builtin_memcpy(o, &w, 16);  // (at any alignment)
+                        store16<false>(reinterpret_cast<char *>(o), w);
                     } else if (b < B) {
                         for (int e = 0; e < E::kVec && v + e < vend; ++e) {
                             typename E::T val;
-                            __builtin_memcpy(&val, reinterpret_cast<const char *>(tmp + row * (kUnits * 16) + 16 * (unit ^ (row & (kUnits - 1)))) + e * sizeof val, sizeof val);
+                            __builtin_memcpy(&val, from + e * sizeof val, sizeof val);
                             o[e] = val;
                         }
                     }
@@ -431,7 +451,7 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int n = 0; n < NT; ++n) acc[m][n] = i32x4{0, 0, 0, 0};
-        return v0 + MT * 16 <= vend && b0 + 16 * NT <= B;
+        return full;
     };
 
     set_tile(first);
