@@ -439,26 +439,33 @@ __global__ __launch_bounds__(kBothThreads) __attribute__((amdgpu_waves_per_eu(8,
     const int groups = (int)(a.V / E::kVec), rest = (int)(a.V - (int64_t)groups * E::kVec);
     List<kBothThreads> l{reinterpret_cast<Entry *>(smem), a.k};
     Table t(smem + list_lds(a.k), table_bits(a.k));
+    // (the first loads of either pass are on their way while the list is
+    // worked on)
+    const int step = kFlight * kBothThreads;
+    word4 w[kFlight];
+    auto load_up = [&](int i) {
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) w[u] = load_vec(src + (int64_t)min(i + u * kBothThreads, groups - 1) * E::kVec);
+    };
+    auto load_down = [&](int i) {
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) w[u] = load_last(src + (int64_t)max(i - u * kBothThreads, 0) * E::kVec);
+    };
+    if (groups) load_up(tid);
     t.clear<kBothThreads>();
     l.template read<BF16>(a.ids + row * a.k, a.teacher + row * a.k, a.V, src);
     Part p{-FLT_MAX, 0.0f};
-    int i = tid;
-    for (; i + (kFlight - 1) * kBothThreads < groups; i += kFlight * kBothThreads) {
-        word4 w[kFlight];
-#pragma unroll
-        for (int u = 0; u < kFlight; ++u) w[u] = load_vec(src + (int64_t)(i + u * kBothThreads) * E::kVec);
+    for (int i = tid; i < groups; i += step) {
 #pragma unroll
         for (int u = 0; u < kFlight; ++u) {
             float f[E::kVec];
             E::unpack(w[u], f);
-            add<E::kVec>(p, f, c);
+            if (i + u * kBothThreads < groups) add<E::kVec>(p, f, c);
         }
+        if (i + step < groups) load_up(i + step);
     }
-    for (; i < groups; i += kBothThreads) {
-        float f[E::kVec];
-        E::unpack(load_vec(src + (int64_t)i * E::kVec), f);
-        add<E::kVec>(p, f, c);
-    }
+    const int down = groups - 1 - tid;
+    if (groups) load_down(down);
     const int64_t last = (int64_t)groups * E::kVec + tid;
     float tail = 0.0f;
     if (tid < rest) {
@@ -473,20 +480,14 @@ __global__ __launch_bounds__(kBothThreads) __attribute__((amdgpu_waves_per_eu(8,
     const float g = a.weight * (a.gloss ? a.gloss[row] : 1.0f);
     const Slope sl(p, c, g * a.tau, l.total == 0.0);
     if (tid < rest) put_one<BF16>(sl, t, (uint32_t)groups, (int32_t)last, tail, dst + last);
-    // whole rounds from the end, then what is left of the first one
-    i = groups - 1 - tid;
-    for (; i - (kFlight - 1) * kBothThreads >= 0; i -= kFlight * kBothThreads) {
-        word4 w[kFlight];
-#pragma unroll
-        for (int u = 0; u < kFlight; ++u) w[u] = load_last(src + (int64_t)(i - u * kBothThreads) * E::kVec);
+    for (int i = down; i >= 0; i -= step) {
 #pragma unroll
         for (int u = 0; u < kFlight; ++u) {
             const int at = i - u * kBothThreads;
-            put_group<BF16>(sl, t, (uint32_t)at, at * E::kVec, w[u], dst + (int64_t)at * E::kVec);
+            if (at >= 0) put_group<BF16>(sl, t, (uint32_t)at, at * E::kVec, w[u], dst + (int64_t)at * E::kVec);
         }
+        if (i - step >= 0) load_down(i - step);
     }
-    for (; i >= 0; i -= kBothThreads)
-        put_group<BF16>(sl, t, (uint32_t)i, i * E::kVec, load_last(src + (int64_t)i * E::kVec), dst + (int64_t)i * E::kVec);
 }
 
 vie_status launched(const char *what)
