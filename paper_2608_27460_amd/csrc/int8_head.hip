@@ -28,10 +28,24 @@ constexpr int kPad = 128;   // tokens are padded to whole stages
 
 __host__ __device__ inline int padded(int d) { return (d + kPad - 1) / kPad * kPad; }
 
-__device__ __forceinline__ int quantized(float x, float scale)
-{
-    return scale == 0.0f ? 0 : (int)fminf(fmaxf(rintf(__fdiv_rn(x, scale)), -127.0f), 127.0f);
-}
+// rint(fp32(x / scale)) clamped to [-127, 127], 0 for scale 0.  The product
+// with the reciprocal is off by 4e-5 at most here, so that the division
+// itself is only needed near the middle between two integers (and where the
+// reciprocal is no number to use).
+struct Quantizer {
+    float scale, inverse;
+    __device__ __forceinline__ explicit Quantizer(float scale)
+        : scale(scale), inverse(scale == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(scale))
+    {
+    }
+    __device__ __forceinline__ int operator()(float x) const
+    {
+        const float q = x * inverse;
+        float n = rintf(q);
+        if (!(fabsf(q - n) < 0.499f)) n = rintf(__fdiv_rn(x, scale));
+        return (int)fminf(fmaxf(n, -127.0f), 127.0f);
+    }
+};
 
 // The tokens' int8 values [B][padded(d)] (zero past d) and their scales: a
 // workgroup per token, whose values it holds in registers, eight to a chunk.
@@ -75,13 +89,14 @@ __global__ __launch_bounds__(kTokenThreads) void tokens_kernel(const typename El
     top = block_reduce<kTokenThreads>(top, s_top, [](float a, float b) { return fmaxf(a, b); });
     bad = top == __builtin_inff();
     const float scale = bad ? 0.0f : __fdiv_rn(top, 127.0f);
+    const Quantizer quantized(scale);
 #pragma unroll
     for (int i = 0; i < kChunks; ++i) {
         const int j = (i * kTokenThreads + tid) * 8;
         if (j >= padded(d)) break;
         uint64_t w = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w |= (uint64_t)(uint8_t)quantized(v[i][e], scale) << 8 * e;
+        for (int e = 0; e < 8; ++e) w |= (uint64_t)(uint8_t)quantized(v[i][e]) << 8 * e;
         *reinterpret_cast<uint64_t *>(x + (int64_t)b * padded(d) + j) = w;
     }
     if (tid == 0) xs[b] = bad ? __builtin_nanf("") : scale;
@@ -190,49 +205,94 @@ inline bool tokens_fit(int64_t V, int B, int d)  // (and there are 16 bytes of r
 }
 
 // The tokens' int8 values at tok + b (padded(d) + kHeldPad) and their scales
-// behind them, by tokens_kernel's rule: a wave per token at a time.
-template <bool BF16> __device__ void hold_tokens(const void *h, int B, int d, char *tok, float *s_xs)
-{
-    typedef Elem<BF16> E;
-    const int lane = threadIdx.x & (kLanes - 1), dp = padded(d);
-    for (int b = threadIdx.x / kLanes; b < B; b += kWaves) {
-        const typename E::T *row = static_cast<const typename E::T *>(h) + (int64_t)b * d;
-        auto load8 = [&](int j, float *v) {
-            if (j + 8 <= d) {
-                word4 w[8 / E::kVec];
-                __builtin_memcpy(w, row + j, sizeof w);  // (at any alignment)
+// behind them, by tokens_kernel's rule: a wave per token at a time.  A wave's
+// first token is fetched before the first rows are, so that it does not wait
+// for them, and up to 2048 values of a token are held in registers between
+// the search for their largest and their quantization.
+constexpr int kTokenChunks = 4;  // of eight values a lane
+template <bool BF16> struct Chunk {  // eight values as they are stored
+    static constexpr int kWords = 8 / Elem<BF16>::kVec;
+    word4 w[kWords];
+    // (without branches of the lanes, which would wait for the loads: what
+    // lies past d is loaded from before it, and dropped by `values`)
+    __device__ __forceinline__ void fetch(const typename Elem<BF16>::T *row, int d, int j)
+    {
+        if (d % 8 == 0) {
+            __builtin_memcpy(w, row + min(j, d - 8), sizeof w);  // (at any alignment)
+        } else {
+            typename Elem<BF16>::T e[8];
 #pragma unroll
-                for (int k = 0; k < 8 / E::kVec; ++k) E::unpack(w[k], v + k * E::kVec);
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = j + e < d ? E::get(row[j + e]) : 0.0f;
-            }
-        };
-        float top = 0.0f;
-        bool bad = false;
-        for (int j = 8 * lane; j < d; j += 8 * kLanes) {
-            float v[8];
-            load8(j, v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                bad |= !(fabsf(v[e]) < __builtin_inff());
-                top = fmaxf(top, fabsf(v[e]));
-            }
+            for (int i = 0; i < 8; ++i) e[i] = row[min(j + i, d - 1)];
+            __builtin_memcpy(w, e, sizeof w);
         }
-        top = wave_max(top);
-        bad = __any(bad);
-        const float scale = bad ? 0.0f : __fdiv_rn(top, 127.0f);
-        for (int j = 8 * lane; j < dp; j += 8 * kLanes) {
-            float v[8];
-            load8(j, v);
-            uint64_t w = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) w |= (uint64_t)(uint8_t)quantized(v[e], scale) << 8 * e;
-            *reinterpret_cast<uint64_t *>(tok + b * (dp + kHeldPad) + j) = w;
-        }
-        if (lane == 0) s_xs[b] = bad ? __builtin_nanf("") : scale;
     }
-}
+    __device__ __forceinline__ void values(float *v, int d, int j) const
+    {
+#pragma unroll
+        for (int k = 0; k < kWords; ++k) Elem<BF16>::unpack(w[k], v + k * Elem<BF16>::kVec);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = j + e < d ? v[e] : 0.0f;
+    }
+};
+template <bool BF16> struct Token {
+    Chunk<BF16> c[kTokenChunks];
+    __device__ __forceinline__ void fetch(const void *h, int b, int d)
+    {
+        const typename Elem<BF16>::T *row = static_cast<const typename Elem<BF16>::T *>(h) + (int64_t)b * d;
+#pragma unroll
+        for (int i = 0; i < kTokenChunks; ++i)
+            if (8 * i * kLanes < d) c[i].fetch(row, d, 8 * (i * kLanes + (threadIdx.x & (kLanes - 1))));
+    }
+    // All tokens; the wave's first one is fetched.
+    __device__ void hold(const void *h, int B, int d, char *tok, float *s_xs)
+    {
+        const int lane = threadIdx.x & (kLanes - 1), wave = threadIdx.x / kLanes, dp = padded(d);
+        constexpr int kHeld = 8 * kTokenChunks * kLanes;
+        for (int b = wave; b < B; b += kWaves) {
+            const typename Elem<BF16>::T *row = static_cast<const typename Elem<BF16>::T *>(h) + (int64_t)b * d;
+            if (b != wave) fetch(h, b, d);
+            float top = 0.0f;
+            bool bad = false;
+            auto look = [&](int j, const Chunk<BF16> &x) {
+                float v[8];
+                x.values(v, d, j);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    bad |= !(fabsf(v[e]) < __builtin_inff());
+                    top = fmaxf(top, fabsf(v[e]));
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < kTokenChunks; ++i)
+                if (8 * i * kLanes < d) look(8 * (i * kLanes + lane), c[i]);
+            for (int j = kHeld + 8 * lane; j < d; j += 8 * kLanes) {
+                Chunk<BF16> x;
+                x.fetch(row, d, j);
+                look(j, x);
+            }
+            top = wave_max(top);
+            bad = __any(bad);
+            const Quantizer quantized(bad ? 0.0f : __fdiv_rn(top, 127.0f));
+            auto write = [&](int j, const Chunk<BF16> &x) {
+                float v[8];
+                x.values(v, d, j);
+                uint64_t w = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) w |= (uint64_t)(uint8_t)quantized(v[e]) << 8 * e;
+                if (j < dp) *reinterpret_cast<uint64_t *>(tok + b * (dp + kHeldPad) + j) = w;
+            };
+#pragma unroll
+            for (int i = 0; i < kTokenChunks; ++i)
+                if (8 * i * kLanes < d) write(8 * (i * kLanes + lane), c[i]);
+            for (int j = kHeld + 8 * lane; j < dp; j += 8 * kLanes) {
+                Chunk<BF16> x;
+                x.fetch(row, d, j);
+                write(j, x);
+            }
+            if (lane == 0) s_xs[b] = bad ? __builtin_nanf("") : quantized.scale;
+        }
+    }
+};
 
 // Tile t of a workgroup: XCD blockIdx.x % 8 takes a run of the tiles, its
 // workgroups take every 32nd of them, and the order goes over up to eight
@@ -243,10 +303,10 @@ struct Tiles {
     int per_xcd, step; // tiles of an XCD's run, its workgroups
 };
 
-template <int MT, int NT, int WB, int KC, int NBUF, bool AHEAD, bool HELD, bool DMA, bool OUT_BF16>
+template <int MT, int NT, int WB, int KC, int NBUF, bool AHEAD, bool HELD, bool H_BF16, bool DMA, bool OUT_BF16>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void int8_tile_kernel(
     const int8_t *__restrict__ q, int pitch, const float *__restrict__ scale, int64_t V, const int8_t *__restrict__ x,
-    int dp, const float *__restrict__ xs, const void *__restrict__ h, int h_bf16, int d, int B, typename Elem<OUT_BF16>::T *__restrict__ out, int64_t ld, Tiles tiles)
+    int dp, const float *__restrict__ xs, const void *__restrict__ h, int d, int B, typename Elem<OUT_BF16>::T *__restrict__ out, int64_t ld, Tiles tiles)
 {
     typedef Elem<OUT_BF16> E;
     extern __shared__ __align__(16) char smem[];
@@ -454,12 +514,14 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         return full;
     };
 
+    Token<H_BF16> token;
+    if constexpr (HELD)
+        if (wave < B) token.fetch(h, wave, d);
     set_tile(first);
 #pragma unroll
     for (int i = 0; i < (DMA ? NBUF - !AHEAD : 2); ++i) load_next(i);
     if constexpr (HELD) {
-        if (h_bf16) hold_tokens<true>(h, B, d, tok, s_xs);
-        else hold_tokens<false>(h, B, d, tok, s_xs);
+        token.hold(h, B, d, tok, s_xs);
         __syncthreads();
     }
     int buf = 0, stored = 0, t = first, st = 0;
@@ -589,12 +651,12 @@ size_t tokens_bytes(int d, int B) { return ((size_t)B * padded(d) + 255) & ~(siz
 
 namespace {
 // `q`: rows of `pitch` bytes, a.q's own or copies of them.
-template <int MT, int NT, int WB, int KC, int NBUF, bool AHEAD, bool HELD, bool DMA, bool OUT_BF16>
+template <int MT, int NT, int WB, int KC, int NBUF, bool AHEAD, bool HELD, bool H_BF16, bool DMA, bool OUT_BF16>
 hipError_t tile_launch(const Int8Launch &a, const int8_t *q, int pitch, const int8_t *x, const float *xs, bool even, hipStream_t s)
 {
     constexpr int BT = 16 * NT * WB, lds = tile_lds(tile_stage(HELD ? 0 : BT, KC), NBUF, MT, HELD);
     static_assert(lds <= 160 * 1024, "a tile's stages fit LDS");
-    auto kern = int8_tile_kernel<MT, NT, WB, KC, NBUF, AHEAD, HELD, DMA, OUT_BF16>;
+    auto kern = int8_tile_kernel<MT, NT, WB, KC, NBUF, AHEAD, HELD, H_BF16, DMA, OUT_BF16>;
     hipError_t e = hipFuncSetAttribute((const void *)kern, hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (e != hipSuccess) return e;
     Tiles t;
@@ -609,7 +671,7 @@ hipError_t tile_launch(const Int8Launch &a, const int8_t *q, int pitch, const in
     const int64_t n = (int64_t)t.nv * t.nb;
     t.per_xcd = (int)((n + 7) / 8);
     t.step = std::min(kWorkgroups / 8, t.per_xcd);
-    kern<<<8 * t.step, kThreads, lds, s>>>(q, pitch, a.scale, a.V, x, padded(a.d), xs, a.h, a.h_dtype == VIE_BF16, a.d, a.B,
+    kern<<<8 * t.step, kThreads, lds, s>>>(q, pitch, a.scale, a.V, x, padded(a.d), xs, a.h, a.d, a.B,
                                            static_cast<typename Elem<OUT_BF16>::T *>(a.out), a.ld, t);
     return hipGetLastError();
 }
@@ -617,16 +679,20 @@ hipError_t tile_launch(const Int8Launch &a, const int8_t *q, int pitch, const in
 template <bool OUT_BF16>
 hipError_t tiles_launch(const Int8Launch &a, const int8_t *q, int pitch, const int8_t *x, const float *xs, hipStream_t s)
 {
-    if (a.B <= 16) return tile_launch<2, 1, 1, 128, 3, true, false, true, OUT_BF16>(a, q, pitch, x, xs, true, s);
-    if (a.B <= 32) return tile_launch<2, 2, 1, 128, 3, true, false, true, OUT_BF16>(a, q, pitch, x, xs, true, s);
-    if (a.B <= 64) return tile_launch<2, 4, 1, 128, 3, true, false, true, OUT_BF16>(a, q, pitch, x, xs, true, s);
-    if (a.B <= 128) return tile_launch<4, 4, 2, 64, 4, true, false, true, OUT_BF16>(a, q, pitch, x, xs, false, s);
-    return tile_launch<8, 4, 4, 128, 2, false, false, true, OUT_BF16>(a, q, pitch, x, xs, false, s);
+    if (a.B <= 16) return tile_launch<2, 1, 1, 128, 3, true, false, false, true, OUT_BF16>(a, q, pitch, x, xs, true, s);
+    if (a.B <= 32) return tile_launch<2, 2, 1, 128, 3, true, false, false, true, OUT_BF16>(a, q, pitch, x, xs, true, s);
+    if (a.B <= 64) return tile_launch<2, 4, 1, 128, 3, true, false, false, true, OUT_BF16>(a, q, pitch, x, xs, true, s);
+    if (a.B <= 128) return tile_launch<4, 4, 2, 64, 4, true, false, false, true, OUT_BF16>(a, q, pitch, x, xs, false, s);
+    return tile_launch<8, 4, 4, 128, 2, false, false, false, true, OUT_BF16>(a, q, pitch, x, xs, false, s);
 }
-template <bool OUT_BF16> hipError_t few_launch(const Int8Launch &a, bool aligned, hipStream_t s)
+template <bool H_BF16, bool OUT_BF16> hipError_t few_launch(const Int8Launch &a, bool aligned, hipStream_t s)
 {
-    if (aligned) return tile_launch<2, 1, 1, 128, 3, true, true, true, OUT_BF16>(a, a.q, a.d, nullptr, nullptr, true, s);
-    return tile_launch<2, 1, 1, 128, 2, false, true, false, OUT_BF16>(a, a.q, a.d, nullptr, nullptr, true, s);
+    if (aligned) return tile_launch<2, 1, 1, 128, 3, true, true, H_BF16, true, OUT_BF16>(a, a.q, a.d, nullptr, nullptr, true, s);
+    return tile_launch<2, 1, 1, 128, 2, false, true, H_BF16, false, OUT_BF16>(a, a.q, a.d, nullptr, nullptr, true, s);
+}
+template <bool H_BF16> hipError_t few_launch(const Int8Launch &a, bool aligned, hipStream_t s)
+{
+    return a.out_dtype == VIE_BF16 ? few_launch<H_BF16, true>(a, aligned, s) : few_launch<H_BF16, false>(a, aligned, s);
 }
 
 // Rows of d bytes copied to rows of `pitch` bytes, a multiple of 16 (what
@@ -658,7 +724,7 @@ vie_status launch_int8_logits(const Int8Launch &a, hipStream_t s)
         return e == hipSuccess ? VIE_OK : fail(VIE_EHIP, "int8 head launch: %s", hipGetErrorString(e));
     };
     const bool bf16 = a.out_dtype == VIE_BF16, aligned = a.d % 16 == 0 && (uintptr_t)a.q % 16 == 0;
-    if (tokens_fit(a.V, a.B, a.d)) return done(bf16 ? few_launch<true>(a, aligned, s) : few_launch<false>(a, aligned, s));
+    if (tokens_fit(a.V, a.B, a.d)) return done(a.h_dtype == VIE_BF16 ? few_launch<true>(a, aligned, s) : few_launch<false>(a, aligned, s));
     int8_t *x = static_cast<int8_t *>(a.ws);
     float *xs = reinterpret_cast<float *>(x + tokens_bytes(a.d, a.B));
     if (a.h_dtype == VIE_BF16) tokens_kernel<true><<<a.B, kTokenThreads, 0, s>>>(static_cast<const uint16_t *>(a.h), a.d, x, xs);
