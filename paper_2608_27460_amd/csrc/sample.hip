@@ -258,10 +258,14 @@ template <int NT> __global__ __launch_bounds__(NT) void sample_list_kernel(Sampl
 // octave from 1/8 to 32, so that the bins are finest where the candidates are
 // few and weigh most.  A bf16 row has few enough values for a bin each; its
 // candidates are counted only, and weighed by the bin.  A border in the bulk
-// of 262144 normal logits meets some 400 candidates of its bin.  Rows whose border bins hold more than kCollect
-// (constant rows, or spreads far from a model's) take the borders one after
-// the other from histograms of the keys' digits: exact too, in up to 24
-// passes of one workgroup.
+// of 262144 normal logits meets some 400 candidates of its bin.
+//
+// Rows whose border bins hold more than kCollect candidates take one of two
+// other ways.  Where each of these bins holds one value (logits that were
+// rounded to bf16 somewhere, constant rows), its candidates weigh the same,
+// and borders and the token's place among them follow from their number.
+// Otherwise the borders are found one after the other from histograms of the
+// keys' digits: exact too, in up to 24 passes of one workgroup.
 
 constexpr int kRowThreads = 1024;
 constexpr int kRowWaves = kRowThreads / kLanes;
@@ -291,10 +295,10 @@ template <> struct Bins<false> {
     }
 };
 
-// bf16: a bin for each value of 2^-6 and more in size, one for those between,
+// bf16: a bin for each value of 2^-12 and more in size, one for those between,
 // the last one for all from 8191 values below the best.
 template <> struct Bins<true> {
-    static constexpr int kSmall = 121 << 7;  // the bits of 2^-6
+    static constexpr int kSmall = 115 << 7;  // the bits of 2^-12
     int top;
     __device__ __forceinline__ explicit Bins(uint64_t best) : top(place(key_logit(best))) {}
     static __device__ __forceinline__ int place(float l)
@@ -407,8 +411,19 @@ __device__ __noinline__ Place find(const Row<BF16> &row, const Weights &weights,
             const uint64_t key = make_key(l, id);
             if (shift + bits < 64 && (key >> (shift + bits)) != prefix) return;
             const int bin = (int)((key >> shift) & ((1u << bits) - 1));
-            atomicAdd(&s.count[bin], 1u);
-            atomicAdd((unsigned long long *)&s.sum[bin], (unsigned long long)weights.units(l));
+            const uint64_t units = weights.units(l);
+            // (where a wave's candidates share a digit and a weight, as equal
+            // logits do, one of them adds for all)
+            const unsigned long long active = __ballot(1);
+            if (__all(bin == __builtin_amdgcn_readfirstlane(bin)) && __all(l == __shfl(l, __ffsll(active) - 1, kLanes))) {
+                if ((threadIdx.x & (kLanes - 1)) == __ffsll(active) - 1) {
+                    atomicAdd(&s.count[bin], (uint32_t)__popcll(active));
+                    atomicAdd((unsigned long long *)&s.sum[bin], (unsigned long long)(units * __popcll(active)));
+                }
+            } else {
+                atomicAdd(&s.count[bin], 1u);
+                atomicAdd((unsigned long long *)&s.sum[bin], (unsigned long long)units);
+            }
         });
         __syncthreads();
         // bins from the top, two a thread
@@ -599,6 +614,7 @@ struct Bin {
 struct Slot {
     uint64_t base;
     uint32_t rank, first;
+    int bin;
 };
 
 struct DrawLds {
@@ -667,6 +683,134 @@ template <int E> __device__ void sort_row(uint64_t *key, int P)
     for (int e = 0; e < E; ++e)
         if (e * kRowThreads + tid < P) key[e * kRowThreads + tid] = v[e];
     __syncthreads();
+}
+
+// What the draw knows of a row's borders: the limits, and the weight of the
+// first K candidates and of the kept ones where the bins gave it exactly.
+struct Borders {
+    uint32_t K, most;
+    bool exact_k, exact_end;
+    uint64_t sum_k, sum_end;
+};
+
+// The draw where the border bins (at most kTies of them) are too full to be
+// collected: every part of the row calls it.  The part's candidates of each
+// bin are counted, and the lowest and the highest of them kept; the last part
+// to finish has those of all.  Returns 0 in the others, 1 with the result,
+// and 2, in the last part, if a bin holds more than one value.
+constexpr int kTies = 8;
+static_assert(kMaxParts * kTies * 2 <= kCollect, "the parts' counts take the place of the collected keys");
+template <bool BF16>
+__device__ __noinline__ int draw_ties(const Row<BF16> &row, const Weights &weights, const Bins<BF16> &bin_map,
+                                      const Settings &st, float u, const Borders &known, int nslot, int64_t len,
+                                      RowSpace &ws, DrawLds &s, Result &out)
+{
+    typedef Elem<BF16> E;
+    const int tid = threadIdx.x, S = gridDim.x, part = blockIdx.x;
+    for (int j = 0; j < nslot; ++j) {
+        const int bin = s.d.slot[j].bin;
+        uint32_t low = ~0u, high = 0, n = 0;
+        const int64_t i0 = part * len;
+        row.each(i0, min(len, row.n - i0), [&](float l, int32_t) {
+            if (bin_map.of(l) != bin) return;
+            const uint32_t o = f2ord(l);
+            low = min(low, o);
+            high = max(high, o);
+            ++n;
+        });
+        low = block_reduce<kRowThreads>(low, s.wave_count, [](uint32_t a, uint32_t b) { return min(a, b); });
+        high = block_reduce<kRowThreads>(high, s.wave_count, [](uint32_t a, uint32_t b) { return max(a, b); });
+        n = block_reduce<kRowThreads>(n, s.wave_count, [](uint32_t a, uint32_t b) { return a + b; });
+        if (tid == 0) {
+            uint64_t *to = &ws.key[(part * kTies + j) * 2];
+            __hip_atomic_store(to, (uint64_t)high << 32 | low, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __hip_atomic_store(to + 1, (uint64_t)n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0) s.last = __hip_atomic_fetch_add(&ws.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (s.last != (uint32_t)S - 1) return 0;
+    // all parts' counts, and a bin's value and number
+    uint64_t *all = s.d.key;
+    for (int i = tid; i < S * kTies * 2; i += kRowThreads)
+        all[i] = i / 2 % kTies < nslot ? __hip_atomic_load(&ws.key[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0ull;
+    __syncthreads();
+    bool one = true;
+    for (int j = 0; j < nslot; ++j) {
+        uint32_t low = ~0u, high = 0, n = 0;
+        for (int c = 0; c < S; ++c) {
+            const uint64_t v = all[(c * kTies + j) * 2], m = all[(c * kTies + j) * 2 + 1];
+            if (m == 0) continue;
+            low = min(low, (uint32_t)v);
+            high = max(high, (uint32_t)(v >> 32));
+            n += (uint32_t)m;
+        }
+        one &= low == high;
+        s.d.sum[2 * j] = high;  // (every thread writes the same)
+        s.d.sum[2 * j + 1] = n;
+    }
+    __syncthreads();
+    if (!one) return 2;
+    // the place of a rank or a sum: its bin, and how many of it up to there
+    struct At {
+        int slot;
+        uint64_t count, sum;
+        int64_t rank;
+    };
+    auto at = [&](bool by_rank, uint64_t v) {
+        int j = 0;
+        for (;; ++j) {
+            const uint64_t n = s.d.sum[2 * j + 1], unit = weights.units(ord2f((uint32_t)s.d.sum[2 * j]));
+            const Slot sl = s.d.slot[j];
+            const uint64_t end = by_rank ? sl.rank + n : sl.base + n * unit;
+            if (end < v && j + 1 < nslot) continue;
+            uint64_t k = by_rank ? v - sl.rank : v > sl.base && unit ? (v - sl.base + unit - 1) / unit : 1;
+            k = k < 1 ? 1 : k > n ? n : k;
+            return At{j, k, sl.base + k * unit, (int64_t)(sl.rank + k)};
+        }
+    };
+    const uint64_t ck = known.exact_k ? known.sum_k : at(true, known.K).sum;
+    int64_t kept = known.most;
+    if (st.p < 1.0) kept = min(kept, at(false, reach(st.p, ck)).rank);
+    const uint64_t end = known.exact_end ? known.sum_end : at(true, kept).sum;
+    const At t = at(false, min(below(u, end) + 1, end));
+    // the token: number t.count of its bin, by id; first its part
+    uint64_t left = t.count;
+    int c = 0;
+    for (; c < S - 1 && left > all[(c * kTies + t.slot) * 2 + 1]; ++c) left -= all[(c * kTies + t.slot) * 2 + 1];
+    const int64_t i0 = c * len, n = min(len, row.n - i0);
+    const int bin = s.d.slot[t.slot].bin;
+    const float l = ord2f((uint32_t)s.d.sum[2 * t.slot]);
+    if (tid == 0) s.found_rank = 0;
+    uint64_t before = 0;
+    for (int64_t i = 0; i < n; i += kRowThreads * E::kVec) {
+        const int64_t mine = i + tid * E::kVec;
+        uint32_t hits = 0;
+#pragma unroll
+        for (int e = 0; e < E::kVec; ++e) {
+            const float x = mine + e < n ? E::get(row.l[i0 + mine + e]) : -__builtin_inff();
+            hits |= (uint32_t)(candidate(x) && bin_map.of(x) == bin) << e;
+        }
+        uint32_t upto = __popc(hits);
+        uint64_t none = 0;
+        __syncthreads();
+        block_scan(upto, none, s.wave_count, s.wave_sum);
+        uint32_t sum = 0;
+        for (int w = 0; w < kRowWaves; ++w) sum += s.wave_count[w];
+        const uint64_t from = before + upto - __popc(hits);
+        if (from < left && left <= before + upto) {
+            uint32_t h = hits;
+            for (uint64_t k = from + 1; k < left; ++k) h &= h - 1;
+            s.found_rank = i0 + mine + __ffs(h) - 1;
+        }
+        before += sum;
+        if (before >= left) break;
+    }
+    __syncthreads();
+    out = {(int32_t)s.found_rank, (float)(weights.real(l) / (double)end), (int32_t)kept};
+    return 1;
 }
 
 template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_kernel(SampleLaunch a, Parts parts)
@@ -807,7 +951,7 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
 #pragma unroll
         for (int i = 0; i < kBinsPer; ++i) {
             if (flags >> i & 1 && cnt[i]) {
-                if (slots < kMaxSlots) s.d.slot[slots] = Slot{xi, ci, fi};
+                if (slots < kMaxSlots) s.d.slot[slots] = Slot{xi, ci, fi, tid * kBinsPer + i};
                 fi += cnt[i];
                 ++slots;
             }
@@ -818,8 +962,15 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     if (tid == 0) s.base = 0;
     __syncthreads();
     if (M > kCollect || nslot > kMaxSlots) {  // (the same in every workgroup of the row)
-        if (blockIdx.x != 0) return;
-        const Result r = draw_by_digits(row, weights, st, u, live, total, pass, s.digits);
+        Result r;
+        int how = 2;
+        if (nslot <= kTies)
+            how = draw_ties(row, weights, bin_map, st, u, Borders{K, most, exact_k, exact_end, sum_k, sum_end}, (int)nslot,
+                            parts.len, ws, s, r);
+        else if (blockIdx.x != 0)
+            return;
+        if (how == 0) return;
+        if (how == 2) r = draw_by_digits(row, weights, st, u, live, total, pass, s.digits);
         if (tid == 0) put(a, b, r);
         return;
     }

@@ -310,6 +310,21 @@ def test_sample_rows_ties_and_special_values(vie, V, dtype):
         check_draws(got, z.float().numpy(), np.arange(V), u.numpy(), t, tk, tp, mp, "ties")
 
 
+@pytest.mark.parametrize("B,V,dtype", [(1, 262144, F32), (3, 151936, BF16), (2, 100003, F32), (70, 40000, BF16)])
+@pytest.mark.parametrize("mean,spread", [(20, 2), (0, 0.02), (300, 8)])
+def test_sample_rows_rounded_logits(vie, B, V, dtype, mean, spread):
+    """Logits of few distinct values (bf16 ones, also held in fp32): thousands of ties at every border."""
+    say("rounded", B, V, dtype, mean, spread)
+    g = torch.Generator().manual_seed(V + mean)
+    z = (mean + spread * torch.randn(B, V, generator=g)).to(BF16).to(dtype)
+    z[-1, ::3] = -INF
+    u = torch.rand(B, generator=g)
+    for t, tk, tp, mp in [(1.0, 0, 0.9, 0.0), (1.0, 0, 1.0, 0.0), (2.0, 9999, 0.95, 0.0), (5.0, 0, 0.99, 0.3), (0.7, 20000, 1.0, 0.0)]:
+        say("  ", t, tk, tp, mp)
+        got = vie.sample_rows(z.cuda(), u.cuda(), temperature=t, top_k=tk, top_p=tp, min_p=mp)
+        check_draws(got, z.float().numpy(), np.arange(V), u.numpy(), t, tk, tp, mp, "rounded")
+
+
 def test_sample_frequencies(vie):
     """Tokens drawn with evenly spread uniform numbers: each as often as its weight says, to one draw."""
     say("frequencies")
