@@ -524,13 +524,17 @@ Split split_rows(const DistillLaunch &a, int64_t least, int most_groups)
     return s;
 }
 
-// The row's parts and, in a step that keeps none for the caller, its stats.
-size_t parts_bytes(int N) { return (size_t)N * kMaxParts * sizeof(Part); }
+// The rows' parts (more than 256 rows have none: split_rows) and, in a step
+// that keeps none for the caller, their stats.
+size_t parts_bytes(int N) { return N > 256 ? 0 : (size_t)N * kMaxParts * sizeof(Part); }
 
 template <bool BF16> vie_status forward(const DistillLaunch &a, hipStream_t s)
 {
-    // (joining parts is a launch more: 4 us, in which a workgroup reads some 200 KB)
-    Split sp = split_rows(a, 32768, INT32_MAX);
+    // Joining parts is a launch more, in which a workgroup reads some 200 KB
+    // of a row (one row of 65536 bf16: 12 us whole, 14 in parts; of 262144:
+    // 18 and 15).
+    const bool whole = a.V * elem_bytes(a.dtype) <= 192 * 1024;
+    Split sp = split_rows(a, whole ? a.V : 32768, INT32_MAX);
     if (sp.parts > kMaxParts) {
         sp.len = ((a.V + kMaxParts - 1) / kMaxParts + 63) / 64 * 64;
         sp.parts = (int)((a.V + sp.len - 1) / sp.len);
@@ -553,7 +557,11 @@ template <bool BF16> vie_status backward(const DistillLaunch &a, hipStream_t s)
 
 template <bool BF16> vie_status step(const DistillLaunch &a, hipStream_t s)
 {
-    if (a.N >= 128 && a.V / Elem<BF16>::kVec < kMapGroups) {
+    // One kernel where its workgroups fill half of the CUs, or where the row
+    // is read in less time than another launch takes (8 rows of 8000 bf16: 15
+    // us so, 22 as two kernels; of 32000: 21 and 16).
+    const bool one = a.N >= 128 || a.V * elem_bytes(a.dtype) <= 32 * 1024;
+    if (one && a.V / Elem<BF16>::kVec < kMapGroups) {
         if (vie_status e = allow_lds((const void *)distill_both_kernel<BF16>, table_lds(a.k))) return e;
         distill_both_kernel<BF16><<<a.N, kBothThreads, table_lds(a.k), s>>>(a);
         return launched("distillation step launch");
