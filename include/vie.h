@@ -379,8 +379,8 @@ vie_status vie_int8_logits_workspace(int64_t V, int32_t d, int32_t B, size_t *by
  * the scale NaN), and
  *   out[b][v] = fp32(fp32(fp32(sum_j q[v][j] x[b][j]) scale[v]) xs[b])
  * with an exact integer sum, rounded to nearest even if out_dtype is
- * VIE_BF16.  out_dev [B][out_ld] must not overlap the inputs.
- * Errors: VIE_EINVAL, VIE_EHIP. */
+ * VIE_BF16.  out_dev [B][out_ld] does not overlap the inputs.
+ * Errors: VIE_EINVAL (overlaps among them), VIE_EHIP. */
 vie_status vie_int8_logits(const int8_t *q_dev, const float *scale_dev, int64_t V, int32_t d, const void *h_dev,
                            vie_dtype h_dtype, int32_t B, void *out_dev, vie_dtype out_dtype, int64_t out_ld,
                            void *workspace_dev, size_t workspace_bytes, void *hip_stream);

@@ -58,6 +58,17 @@ vie_status check_distill(const void *logits, int32_t dtype, int32_t N, int64_t V
     return VIE_OK;
 }
 
+bool overlap(const void *a, size_t an, const void *b, size_t bn)
+{
+    return (uintptr_t)a < (uintptr_t)b + bn && (uintptr_t)b < (uintptr_t)a + an;
+}
+
+// Bytes from the first to the last of `rows` rows of V values, ld apart.
+size_t matrix_bytes(int32_t rows, int64_t V, int64_t ld, int32_t dtype)
+{
+    return ((size_t)(rows - 1) * ld + V) * elem_bytes(dtype);
+}
+
 // The gradient's rows are the logits' own or apart from them.
 vie_status check_apart(const DistillLaunch &a)
 {
@@ -66,10 +77,8 @@ vie_status check_apart(const DistillLaunch &a)
             return fail(VIE_EINVAL, "a gradient in place of the logits needs their row stride");
         return VIE_OK;
     }
-    const size_t e = (size_t)elem_bytes(a.dtype);
-    const uintptr_t p = (uintptr_t)a.logits, pe = p + ((size_t)(a.N - 1) * a.ld + a.V) * e;
-    const uintptr_t g = (uintptr_t)a.grad, ge = g + ((size_t)(a.N - 1) * a.grad_ld + a.V) * e;
-    if (p < ge && g < pe) return fail(VIE_EINVAL, "the gradient overlaps the logits without being in their place");
+    if (overlap(a.logits, matrix_bytes(a.N, a.V, a.ld, a.dtype), a.grad, matrix_bytes(a.N, a.V, a.grad_ld, a.dtype)))
+        return fail(VIE_EINVAL, "the gradient overlaps the logits without being in their place");
     return VIE_OK;
 }
 
@@ -98,6 +107,10 @@ vie_status vie_int8_logits(const int8_t *q_dev, const float *scale_dev, int64_t 
     if (vie_status s = check_matrix(h_dev, h_dtype, d, d, "h")) return s;
     if (vie_status s = check_matrix(out_dev, out_dtype, V, out_ld, "the logits")) return s;
     if ((uintptr_t)scale_dev % 4) return fail(VIE_EINVAL, "scale is not aligned to its type");
+    const size_t n = matrix_bytes(B, V, out_ld, out_dtype);
+    if (overlap(out_dev, n, q_dev, (size_t)V * d) || overlap(out_dev, n, scale_dev, (size_t)V * 4) ||
+        overlap(out_dev, n, h_dev, (size_t)B * d * elem_bytes(h_dtype)))
+        return fail(VIE_EINVAL, "the logits overlap the inputs");
     if (vie_status s = check_workspace(workspace_dev, workspace_bytes, int8_workspace_bytes(V, d, B))) return s;
     const Int8Launch a{q_dev, scale_dev, V, d, h_dev, h_dtype, B, out_dev, out_dtype, out_ld, workspace_dev};
     return launch_int8_logits(a, static_cast<hipStream_t>(hip_stream));

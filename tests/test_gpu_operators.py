@@ -578,3 +578,81 @@ def test_results_do_not_change_between_runs(vie):
         if first is None:
             first = got
         assert all(torch.equal(x, y) for x, y in zip(got, first))
+
+
+def test_streams_at_once(vie):
+    """Calls on two streams that run at the same time do not meet in a workspace."""
+    say("two streams")
+    work = []
+    for k in range(2):
+        z, u = row_logits(4, 60000, F32, 20 + k, False)
+        q, scale, h = int8_inputs(20000, 200, 70, BF16, 30 + k)
+        s, ids, t = distill_inputs(6, 150000, 30, BF16, 40 + k)
+        work.append([x.cuda() for x in (z, u, q, scale, h, s, *(torch.from_numpy(np.ascontiguousarray(y)) for y in (ids, t)))])
+
+    def calls(z, u, q, scale, h, s, ids, t):
+        return [*vie.sample_rows(z, u, top_p=0.9), vie.Int8Head(q, scale)(h), *vie.distill_step(s, ids, t, 2.0)]
+
+    want = [calls(*w) for w in work]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        got = []
+        for st, w in zip(streams, work):
+            with torch.cuda.stream(st):
+                got.append(calls(*w))
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_offsets_past_32_bits(vie):
+    """Rows 2.4 GB apart, and int8 rows of 2.5 GB in all."""
+    V, R, ld = 5003, 3, 1_200_000_000
+    say("offsets: rows", V, R, ld)
+    buf = torch.empty(ld * (R - 1) + V, dtype=BF16, device="cuda")
+    far = buf.as_strided((R, V), (ld, 1))
+    z, u = row_logits(R, V, BF16, 3, False)
+    far.copy_(z)
+    got = vie.sample_rows(far, u.cuda(), top_p=0.9)
+    assert all(torch.equal(x, y) for x, y in zip(got, vie.sample_rows(z.cuda(), u.cuda(), top_p=0.9)))
+    s, ids, t = distill_inputs(R, V, 20, BF16, 4)
+    idd, td = dev(ids, t)
+    want = vie.distill_step(s.cuda(), idd, td, 2.0)
+    far.copy_(s)
+    loss, grad = vie.distill_step(far, idd, td, 2.0, out=far)
+    assert torch.equal(loss, want[0]) and torch.equal(grad, want[1])
+    q, scale, h = int8_inputs(V, 96, R, BF16, 5)
+    vie.Int8Head(q.cuda(), scale.cuda())(h.cuda(), out=far)
+    same_bits(far, int8_reference(q, scale, h, BF16))
+    del buf, far, grad
+    V, d = 300007, 8192
+    say("offsets: int8 rows", V, d)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    q = torch.randint(-127, 128, (V, d), dtype=torch.int8, device="cuda", generator=g)
+    scale = torch.rand(V, device="cuda", generator=g) * 1e-3
+    for B in (2, 70):
+        h = torch.randn(B, d, generator=torch.Generator().manual_seed(B))
+        out = vie.Int8Head(q, scale)(h.cuda())
+        for part in (slice(0, 700), slice(262100, 262200), slice(V - 700, V)):
+            same_bits(out[:, part].contiguous(), int8_reference(q[part].cpu(), scale[part].cpu(), h, F32))
+
+
+def test_many_short_rows(vie):
+    """More rows than a launch dimension takes at once."""
+    N, V, k = 40000, 17, 3
+    say("many rows", N, V)
+    s, ids, t = distill_inputs(N, V, k, F32, 9)
+    idd, td = dev(ids, t)
+    ref, grad, Q, P = distill_reference(s.numpy(), ids, t, 1.0, np.ones(N))
+    loss, stats = vie.distill(s.cuda(), idd, td, 1.0)
+    back = vie.distill_grad(s.cuda(), idd, td, stats, 1.0)
+    loss2, grad2 = vie.distill_step(s.cuda(), idd, td, 1.0)
+    for x, y in ((loss, back), (loss2, grad2)):
+        check_loss(x.cpu().numpy(), ref, 1.0, V, "many rows")
+        check_grad(y.cpu().numpy(), grad, Q, P, s.numpy(), 1.0, np.ones(N), F32, "many rows")
+    z, u = row_logits(3000, 40, F32, 1, False)
+    got = vie.sample_rows(z.cuda(), u.cuda(), top_k=7, top_p=0.8)
+    check_draws(got, z.numpy(), np.arange(40), u.numpy(), 1.0, 7, 0.8, 0.0, "many rows")
+    lg, li, un = lists(20000, 9, 2)
+    check_draws(vie.sample(*dev(li, lg, un), top_p=0.7), lg, li, un, 1.0, 0, 0.7, 0.0, "many lists")

@@ -14,14 +14,15 @@ PRM = vie.SamplingParams(1.0, 1.0, 0.0, 0)
 BIG = 1 << 40
 
 
-def _int8(q=P, scale=P, V=100, d=64, h=P, ht=vie.BF16, B=40, out=P, ot=vie.F32, ld=100, ws=P, n=BIG):
+def _int8(q=P, scale=P, V=100, d=64, h=P, ht=vie.BF16, B=40, out=C.c_void_p(1 << 20), ot=vie.F32, ld=100, ws=P, n=BIG):
     return L.vie_int8_logits(q, scale, V, d, h, ht, B, out, ot, ld, ws, n, None)
 
 
 @pytest.mark.parametrize("change", [
     {"q": None}, {"scale": None}, {"h": None}, {"out": None}, {"V": 0}, {"V": 1 << 31, "ld": 1 << 31}, {"d": 0}, {"d": 8193},
     {"B": 0}, {"B": 65536}, {"ht": 2}, {"ot": -1}, {"ld": 99}, {"ws": None}, {"ws": C.c_void_p(4096 + 128)}, {"n": 10},
-    {"h": ODD}, {"out": ODD}, {"scale": ODD},
+    {"h": ODD}, {"out": C.c_void_p((1 << 20) + 1)}, {"scale": ODD},
+    {"out": P}, {"out": C.c_void_p(4096 + 6396)}, {"h": C.c_void_p((1 << 20) + 15996)}, {"scale": C.c_void_p((1 << 20) - 4)},  # overlaps
 ])
 def test_int8_logits_refuses(change):
     assert _int8(**change) == vie.EINVAL
