@@ -111,31 +111,76 @@ __device__ __forceinline__ uint64_t lane_xor(uint64_t v, int s)
     return ((uint64_t)lane_xor((uint32_t)(v >> 32), s) << 32) | lane_xor((uint32_t)v, s);
 }
 
+// lane_xor of values of any type of 4 or 8 bytes.
+template <typename T> __device__ __forceinline__ T lane_xor_as(T v, int s)
+{
+    if constexpr (sizeof(T) == 8) return __builtin_bit_cast(T, lane_xor(__builtin_bit_cast(uint64_t, v), s));
+    else return __builtin_bit_cast(T, lane_xor(__builtin_bit_cast(uint32_t, v), s));
+}
+// What `combine` (of any order) makes of the lanes' values, in every lane.
+template <typename T, typename F> __device__ __forceinline__ T wave_reduce(T v, F combine)
+{
+    v = combine(v, lane_xor_as(v, 32));
+    v = combine(v, lane_xor_as(v, 16));
+    v = combine(v, lane_xor_as(v, 8));
+    v = combine(v, lane_xor_as(v, 4));
+    v = combine(v, lane_xor_as(v, 2));
+    return combine(v, lane_xor_as(v, 1));
+}
 template <typename T> __device__ __forceinline__ T wave_sum(T v)
 {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v += __shfl_xor(v, o, kLanes);
-    return v;
+    return wave_reduce(v, [](T a, T b) { return a + b; });
 }
 template <typename T> __device__ __forceinline__ T wave_max(T v)
 {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) {
-        const T x = __shfl_xor(v, o, kLanes);
-        v = x > v ? x : v;
-    }
-    return v;
+    return wave_reduce(v, [](T a, T b) { return b > a ? b : a; });
 }
-// Inclusive sums over the lanes of a wave.
+
+// The value of the lane that the DPP pattern CTRL names, 0 where there is
+// none and in the rows of 16 lanes outside ROWS.
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t lane_from(uint32_t v)
+{
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, ROWS == 0xF);
+}
+template <int CTRL, int ROWS> __device__ __forceinline__ uint64_t lane_from(uint64_t v)
+{
+    return (uint64_t)lane_from<CTRL, ROWS>((uint32_t)(v >> 32)) << 32 | lane_from<CTRL, ROWS>((uint32_t)v);
+}
+// Inclusive sums over each row of 16 lanes, and over the wave: shifts by 1,
+// 2, 4 and 8 within a row, then each row's last lane into the rows after it.
+template <typename T> __device__ __forceinline__ T row_scan(T v)
+{
+    v += lane_from<0x111, 0xF>(v);
+    v += lane_from<0x112, 0xF>(v);
+    v += lane_from<0x114, 0xF>(v);
+    return v + lane_from<0x118, 0xF>(v);
+}
 template <typename T> __device__ __forceinline__ T wave_scan(T v)
 {
-    const int lane = threadIdx.x & (kLanes - 1);
-#pragma unroll
-    for (int o = 1; o < kLanes; o <<= 1) {
-        const T x = __shfl_up(v, o, kLanes);
-        if (lane >= o) v += x;
-    }
-    return v;
+    v = row_scan(v);
+    v += lane_from<0x142, 0xA>(v);
+    return v + lane_from<0x143, 0xC>(v);
+}
+__device__ __forceinline__ uint32_t read_lane(uint32_t v, int lane) { return (uint32_t)__builtin_amdgcn_readlane((int)v, lane); }
+__device__ __forceinline__ uint64_t read_lane(uint64_t v, int lane)
+{
+    return (uint64_t)read_lane((uint32_t)(v >> 32), lane) << 32 | read_lane((uint32_t)v, lane);
+}
+// Inclusive sums over a workgroup of `waves` (at most 16) waves, and the
+// total, from each wave's inclusive sums.  `tmp`: 16 values of LDS, free
+// again after the next barrier.
+template <typename T> struct Sums {
+    T upto, total;
+};
+template <typename T> __device__ __forceinline__ void wave_total(T upto, T *tmp)
+{
+    if ((threadIdx.x & (kLanes - 1)) == kLanes - 1) tmp[threadIdx.x / kLanes] = upto;
+}
+template <typename T> __device__ __forceinline__ Sums<T> after_waves(T upto, const T *tmp, int waves)
+{
+    const int at = threadIdx.x & 15, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kLanes);
+    const T v = row_scan(at < waves ? tmp[at] : T(0));
+    return {upto + (wave ? read_lane(v, wave - 1) : T(0)), read_lane(v, 15)};
 }
 
 // The value `combine` makes of every thread's v, in every thread; the order
@@ -144,8 +189,7 @@ template <typename T> __device__ __forceinline__ T wave_scan(T v)
 template <int NT, typename T, typename F> __device__ __forceinline__ T block_reduce(T v, T *tmp, F combine)
 {
     constexpr int W = NT / kLanes;
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) v = combine(v, __shfl_xor(v, o, kLanes));
+    v = wave_reduce(v, combine);
     if constexpr (W > 1) {
         __syncthreads();
         if ((threadIdx.x & (kLanes - 1)) == 0) tmp[threadIdx.x / kLanes] = v;

@@ -207,7 +207,7 @@ template <int NT> __global__ __launch_bounds__(NT) void sample_list_kernel(Sampl
         double w = 0.0;
         if (j < K) w = weights.real(key_logit(s_key[j]));
         const bool ok = j < K && w >= least;
-        uint64_t x = wave_scan(j < K ? Weights::round(w) : 0ull);
+        uint64_t x = wave_scan<uint64_t>(j < K ? Weights::round(w) : 0ull);
         const unsigned long long pass = __ballot(ok);
         if (W > 1) {
             if ((tid & (kLanes - 1)) == kLanes - 1) s_wave[tid / kLanes] = x;
@@ -380,15 +380,19 @@ template <bool BF16> struct Row {
     }
 };
 
-// Inclusive sums over the workgroup's threads of a count and a sum.
-__device__ __forceinline__ void block_scan(uint32_t &c, uint64_t &s, uint32_t *wave_count, uint64_t *wave_sum)
+// Inclusive sums over the workgroup's threads of a count and a sum, and the
+// totals.
+__device__ __forceinline__ void block_scan(uint32_t &c, uint64_t &s, uint32_t &c_total, uint64_t &s_total,
+                                           uint32_t *wave_count, uint64_t *wave_sum)
 {
-    const int wave = threadIdx.x / kLanes;
     c = wave_scan(c);
     s = wave_scan(s);
-    if ((threadIdx.x & (kLanes - 1)) == kLanes - 1) wave_count[wave] = c, wave_sum[wave] = s;
+    wave_total(c, wave_count);
+    wave_total(s, wave_sum);
     __syncthreads();
-    for (int w = 0; w < wave; ++w) c += wave_count[w], s += wave_sum[w];
+    const auto cs = after_waves(c, wave_count, kRowWaves);
+    const auto ss = after_waves(s, wave_sum, kRowWaves);
+    c = cs.upto, c_total = cs.total, s = ss.upto, s_total = ss.total;
 }
 
 // The first candidate in the order whose rank is at least `rank` (by_rank),
@@ -433,7 +437,9 @@ __device__ __noinline__ Place find(const Row<BF16> &row, const Weights &weights,
         uint64_t cs = s0 + s1;
         uint32_t cc = c0 + c1;
         if (tid == 0) s.bin = -1;
-        block_scan(cc, cs, s.wave_count, s.wave_sum);
+        uint32_t all_count;
+        uint64_t all_sum;
+        block_scan(cc, cs, all_count, all_sum, s.wave_count, s.wave_sum);
         cs += before_sum;
         const int64_t rc = before + cc;
         // (the places after bins `top` and `top - 1`)
@@ -512,7 +518,7 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_best_ke
 __device__ __forceinline__ uint64_t best_key(const RowSpace &ws, int S)
 {
     uint64_t k = 0;
-    for (int i = threadIdx.x & (kLanes - 1); i < S; i += kLanes) k = max(k, ws.best[i]);
+    for (int i = threadIdx.x & (kLanes - 1); i < S; i += kLanes) k = ws.best[i] > k ? ws.best[i] : k;
     return wave_max(k);
 }
 
@@ -796,9 +802,9 @@ __device__ __noinline__ int draw_ties(const Row<BF16> &row, const Weights &weigh
         uint32_t upto = __popc(hits);
         uint64_t none = 0;
         __syncthreads();
-        block_scan(upto, none, s.wave_count, s.wave_sum);
-        uint32_t sum = 0;
-        for (int w = 0; w < kRowWaves; ++w) sum += s.wave_count[w];
+        uint32_t sum;
+        uint64_t no_sum;
+        block_scan(upto, none, sum, no_sum, s.wave_count, s.wave_sum);
         const uint64_t from = before + upto - __popc(hits);
         if (from < left && left <= before + upto) {
             uint32_t h = hits;
@@ -851,10 +857,9 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     }
     const uint32_t call = c;
     const uint64_t xall = x;
-    block_scan(c, x, s.wave_count, s.wave_sum);
-    uint32_t live = 0;
-    uint64_t total = 0;
-    for (int w = 0; w < kRowWaves; ++w) live += s.wave_count[w], total += s.wave_sum[w];
+    uint32_t live;
+    uint64_t total;
+    block_scan(c, x, live, total, s.wave_count, s.wave_sum);
     // before this thread's bins
     c -= call;
     x -= xall;
@@ -940,11 +945,11 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     }
     uint64_t slots = n;
     uint32_t fi = f;
-    block_scan(fi, slots, s.wave_count, s.wave_sum);
+    uint32_t M;
+    uint64_t nslot;
+    block_scan(fi, slots, M, nslot, s.wave_count, s.wave_sum);
     fi -= f;
     slots -= n;
-    uint32_t M = 0, nslot = 0;
-    for (int w = 0; w < kRowWaves; ++w) M += s.wave_count[w], nslot += (uint32_t)s.wave_sum[w];
     if (n) {
         uint32_t ci = c;
         uint64_t xi = x;
@@ -1030,15 +1035,12 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     for (int h = 0; h < kCollect / kRowThreads; ++h) {
         const int i = h * kRowThreads + tid;
         if (h * kRowThreads >= P) break;
-        uint64_t w = wave_scan(i < (int)M ? weights.units(key_logit(s.d.key[i])) : 0ull);
-        if ((tid & (kLanes - 1)) == kLanes - 1) s.wave_sum[tid / kLanes] = w;
+        const uint64_t w = wave_scan<uint64_t>(i < (int)M ? weights.units(key_logit(s.d.key[i])) : 0ull);
+        wave_total(w, s.wave_sum);
         __syncthreads();
-        w += base;
-        for (int v = 0; v < waves; ++v) {
-            if (v < tid / kLanes) w += s.wave_sum[v];
-            base += s.wave_sum[v];
-        }
-        s.d.sum[i] = w;
+        const auto sums = after_waves(w, s.wave_sum, waves);
+        s.d.sum[i] = base + sums.upto;
+        base += sums.total;
         __syncthreads();
     }
 #pragma unroll
