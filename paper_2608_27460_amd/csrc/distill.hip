@@ -48,19 +48,24 @@ template <int N> __device__ __forceinline__ void add(Part &p, const float *f, fl
     for (int i = 0; i < N; ++i) z += term(f[i], m, c);
     p = {m, z};
 }
+// The part of W lanes, in each of them.
+template <int W> __device__ __forceinline__ Part wave_merge(Part p, float c)
+{
+    if constexpr (W > 1) {
+        p = merge(p, Part{lane_xor_as(p.m, W / 2), lane_xor_as(p.z, W / 2)}, c);
+        return wave_merge<W / 2>(p, c);
+    }
+    return p;
+}
 // The whole workgroup's part, in every thread; `tmp`: NT / 64 parts.
 template <int NT> __device__ __forceinline__ Part block_merge(Part p, float c, Part *tmp)
 {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) p = merge(p, Part{__shfl_xor(p.m, o, kLanes), __shfl_xor(p.z, o, kLanes)}, c);
+    p = wave_merge<kLanes>(p, c);
     __syncthreads();
     if ((threadIdx.x & (kLanes - 1)) == 0) tmp[threadIdx.x / kLanes] = p;
     __syncthreads();
-    p = tmp[threadIdx.x & (NT / kLanes - 1)];  // lanes past the waves repeat them: the exchanges stay among NT / 64
-#pragma unroll
-    for (int o = NT / kLanes / 2; o >= 1; o >>= 1)
-        p = merge(p, Part{__shfl_xor(p.m, o, kLanes), __shfl_xor(p.z, o, kLanes)}, c);
-    return p;
+    // (lanes past the waves repeat them: the exchanges stay among NT / 64)
+    return wave_merge<NT / kLanes>(tmp[threadIdx.x & (NT / kLanes - 1)], c);
 }
 
 // 16 bytes at any alignment of the elements
@@ -362,8 +367,7 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void distill_join_ke
     const int lane = threadIdx.x & (kLanes - 1);
     Part p{-FLT_MAX, 0.0f};
     if (lane < parts) p = static_cast<const Part *>(a.ws)[row * kMaxParts + lane];
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) p = merge(p, Part{__shfl_xor(p.m, o, kLanes), __shfl_xor(p.z, o, kLanes)}, c);
+    p = wave_merge<kLanes>(p, c);
     l.sum(a.tau, s_tmp);
     const float loss = l.loss(p, a.tau, s_tmp);
     if (threadIdx.x == 0) {
