@@ -18,6 +18,7 @@
 
 #include <algorithm>
 #include <cfloat>
+#include <type_traits>
 
 #include "block.hpp"
 #include "operators.hpp"
@@ -92,12 +93,24 @@ template <typename T> __device__ __forceinline__ void store_vec(T *p, word4 w)
 // its id lies in [0, V) and its logit is not -inf; the others have id -1.
 // Entry j belongs to thread j % NT in every step, so the steps need no
 // barrier; its fp64 work is one entry at a time, whose registers the rows'
-// kernels could not spare for more.
+// kernels could not spare for more.  NT = 64: the workgroup's first wave
+// works on the list, while the others stream the row (4096 rows of 8000 bf16
+// with 50 entries, forward: 22.5 us, 30 where all waves met in the list's
+// reductions).
 struct Entry {
     int32_t id;
     float t, at;  // the teacher's logit, the student's at that id
     float e;      // exp((t - top) / tau)
 };
+template <int NT> __device__ __forceinline__ void list_barrier()
+{
+    if constexpr (NT > kLanes) {
+        __syncthreads();
+    } else {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
 template <int NT> struct List {
     Entry *entry;
     int k;
@@ -115,17 +128,19 @@ template <int NT> struct List {
         }
         return x;
     }
-    // `s` (of BF16 elements) nullptr: without the student's logits
+    // with the student's logits s (of BF16 elements) of the ids in [v0, v0 + n)
     template <bool BF16>
-    __device__ __forceinline__ void read(const int32_t *ids, const float *teacher, int64_t V, const typename Elem<BF16>::T *s)
+    __device__ __forceinline__ void read(const int32_t *ids, const float *teacher, int64_t V, const typename Elem<BF16>::T *s,
+                                         int64_t v0, int64_t n)
     {
         for (int j = threadIdx.x; j < k; j += NT) {
             Entry x = get(ids, teacher, j, k, V);
-            if (s && x.id >= 0) x.at = Elem<BF16>::get(s[x.id]);
+            if (in(x.id, v0, n)) x.at = Elem<BF16>::get(s[x.id]);
             entry[j] = x;
         }
     }
-    // the list's maximum and sum (the workgroup waits in here)
+    static __device__ __forceinline__ bool in(int32_t id, int64_t v0, int64_t n) { return id >= 0 && id >= v0 && id - v0 < n; }
+    // the list's maximum and sum
     __device__ __forceinline__ void sum(float tau, double *tmp)
     {
         inv_tau = 1.0 / (double)tau;
@@ -144,11 +159,12 @@ template <int NT> struct List {
             z += e;
         }
         total = block_reduce<NT>(z, tmp + NT / kLanes, [](double a, double b) { return a + b; });
+        list_barrier<NT>();
     }
     __device__ __forceinline__ double x(int j) const { return ((double)entry[j].t - (double)top) * inv_tau; }
     __device__ __forceinline__ double p(int j) const { return (double)entry[j].e / total; }
 
-    // The row's loss from its part and the student's logits, in every thread.
+    // The row's loss from its part and the student's logits.
     __device__ __forceinline__ float loss(Part r, float tau, double *tmp) const
     {
         double sum = 0.0;
@@ -164,73 +180,50 @@ template <int NT> struct List {
         sum = block_reduce<NT>(sum, tmp, [](double a, double b) { return a + b; });
         return total == 0.0 ? 0.0f : (float)((double)tau * (double)tau * sum);
     }
-};
 
-// The list's probabilities by id, for the ids of [v0, v0 + n): a hash table
-// of 2^bits places, at least twice the entries, and a bit for every 16 bytes
-// of logits that hold a listed id.
-constexpr int kMapWords = 1024;  // for up to 32768 groups of 16 bytes
-struct Table {
-    uint32_t *map;
-    int32_t *id;
-    float *prob;
-    int bits;
-    __device__ __forceinline__ Table(char *lds, int bits)
-        : map(reinterpret_cast<uint32_t *>(lds)), id(reinterpret_cast<int32_t *>(lds + kMapWords * 4)),
-          prob(reinterpret_cast<float *>(lds + kMapWords * 4 + (4 << bits))), bits(bits)
+    // Whether an id of [v0, v0 + n) is listed more than once (the list of a
+    // head has no such id).  `place`: 2^bits words of LDS, at least twice the
+    // entries, a hash table.
+    __device__ __forceinline__ void clear(int32_t *place, int bits) const
     {
+        for (int i = threadIdx.x; i < 1 << bits; i += NT) place[i] = -1;
     }
-    __device__ __forceinline__ uint32_t place(int32_t v) const { return (uint32_t)v * 2654435761u >> (32 - bits); }
-    template <int NT> __device__ __forceinline__ void clear()
+    __device__ __forceinline__ bool twice(int32_t *place, int bits, int64_t v0, int64_t n) const
     {
-        for (int i = threadIdx.x; i < kMapWords; i += NT) map[i] = 0;
-        for (int i = threadIdx.x; i < 1 << bits; i += NT) id[i] = -1;
-    }
-    // (between clear and fill the workgroup waits; in fill it does so itself)
-    template <int NT> __device__ __forceinline__ void fill(const List<NT> &l, int64_t v0, int64_t n, int vec)
-    {
-        bool twice = false;
+        bool found = false;
 #pragma unroll 1
-        for (int j = threadIdx.x; j < l.k; j += NT) {
-            const int32_t v = l.entry[j].id;
-            const int64_t off = (int64_t)v - v0;
-            if (v < 0 || off < 0 || off >= n) continue;
-            uint32_t h = place(v);
+        for (int j = threadIdx.x; j < k; j += NT) {
+            if (!in(entry[j].id, v0, n)) continue;
+            const int32_t v = entry[j].id;
+            uint32_t h = (uint32_t)v * 2654435761u >> (32 - bits);
             int32_t was;
-            while ((was = atomicCAS(&id[h], -1, v)) != -1 && was != v) h = (h + 1) & ((1u << bits) - 1);
-            twice |= was == v;
-            prob[h] = (float)l.p(j);
-            const uint32_t g = (uint32_t)off / vec;
-            atomicOr(&map[g / 32], 1u << (g % 32));
+            while ((was = atomicCAS(&place[h], -1, v)) != -1 && was != v) h = (h + 1) & ((1u << bits) - 1);
+            found |= was == v;
         }
-        if (!__syncthreads_or(twice)) return;
-        // Ids listed more than once (no list of a head's): their first entry
-        // adds up all of them, in the list's order.
-#pragma unroll 1
-        for (int j = threadIdx.x; j < l.k; j += NT) {
-            const int32_t v = l.entry[j].id;
-            const int64_t off = (int64_t)v - v0;
-            if (v < 0 || off < 0 || off >= n) continue;
-            bool first = true;
-            double p = 0.0;
-            for (int e = 0; e < l.k; ++e) {
-                if (l.entry[e].id != v) continue;
-                first &= e >= j;
-                p += l.p(e);
-            }
-            if (!first) continue;
-            uint32_t h = place(v);
-            while (id[h] != v) h = (h + 1) & ((1u << bits) - 1);
-            prob[h] = (float)p;
-        }
-        __syncthreads();
+        if constexpr (NT > kLanes) return __syncthreads_or(found);
+        else return __any(found);
     }
-    __device__ __forceinline__ bool any(uint32_t group) const { return map[group / 32] >> (group % 32) & 1; }
-    __device__ __forceinline__ float p(int32_t v) const
+    // The gradient at the listed ids of [v0, v0 + n), in grad[id - v0]; of an
+    // id listed more than once its first entry takes the sum, in the list's
+    // order.
+    template <bool BF16, typename G>
+    __device__ __forceinline__ void put(const G &g, int64_t v0, int64_t n, bool twice, typename Elem<BF16>::T *grad) const
     {
-        for (uint32_t h = place(v);; h = (h + 1) & ((1u << bits) - 1)) {
-            if (id[h] == v) return prob[h];
-            if (id[h] == -1) return 0.0f;
+#pragma unroll 1
+        for (int j = threadIdx.x; j < k; j += NT) {
+            if (!in(entry[j].id, v0, n)) continue;
+            const int32_t v = entry[j].id;
+            double sum = p(j);
+            bool first = true;
+            if (twice) {
+                sum = 0.0;
+                for (int e = 0; e < k; ++e) {
+                    if (entry[e].id != v) continue;
+                    first &= e >= j;
+                    sum += p(e);
+                }
+            }
+            if (first && (float)sum != 0.0f) grad[v - v0] = Elem<BF16>::put(g.at(entry[j].at, (float)sum));
         }
     }
 };
@@ -241,7 +234,8 @@ __host__ __device__ inline int table_bits(int k)
     return b;
 }
 __host__ __device__ inline size_t list_lds(int k) { return (size_t)k * sizeof(Entry); }
-inline size_t table_lds(int k) { return kMapWords * 4 + ((size_t)8 << table_bits(k)) + list_lds(k); }  // and the list
+inline size_t table_lds(int k) { return list_lds(k) + ((size_t)4 << table_bits(k)); }  // and the list
+
 
 // The gradient of a row, value by value: f (q - p) with q = term / Z; of a row that lists
 // nothing 0, whatever its logits.
@@ -253,42 +247,30 @@ struct Slope {
     __device__ __forceinline__ float at(float s) const { return term(s, r.m, c) * f_z; }
     __device__ __forceinline__ float at(float s, float p) const { return fmaf(-f, p, at(s)); }
 };
-// Element e of 16 bytes.
-template <bool BF16> __device__ __forceinline__ float element(word4 w, int e)
-{
-    const int k = BF16 ? e >> 1 : e;
-    const uint32_t word = k == 0 ? w.x : k == 1 ? w.y : k == 2 ? w.z : w.w;
-    return BF16 ? __uint_as_float(e & 1 ? word & 0xFFFF0000u : word << 16) : __uint_as_float(word);
-}
-// The gradient of a group of 16 bytes, from v on; the listed ids' values are
-// written over by the same thread.
-template <bool BF16>
-__device__ __forceinline__ void put_group(const Slope &g, const Table &t, uint32_t group, int32_t v, word4 w,
-                                          typename Elem<BF16>::T *dst)
+// The gradient of a group of 16 bytes as if nothing in it were listed.
+template <bool BF16> __device__ __forceinline__ void put_group(const Slope &g, word4 w, typename Elem<BF16>::T *dst)
 {
     typedef Elem<BF16> E;
-    if (g.none) {
-        store_vec(dst, word4{0, 0, 0, 0});
-        return;
-    }
     float x[E::kVec];
     E::unpack(w, x);
 #pragma unroll
     for (int e = 0; e < E::kVec; ++e) x[e] = g.at(x[e]);
-    store_vec(dst, E::pack(x));
-    if (t.any(group)) {
-#pragma unroll 1
-        for (int e = 0; e < E::kVec; ++e) {
-            const float p = t.p(v + e);
-            if (p != 0.0f) dst[e] = E::put(g.at(element<BF16>(w, e), p));
-        }
-    }
+    store_vec(dst, g.none ? word4{0, 0, 0, 0} : E::pack(x));
 }
-template <bool BF16>
-__device__ __forceinline__ void put_one(const Slope &g, const Table &t, uint32_t group, int32_t v, float x,
-                                        typename Elem<BF16>::T *dst)
+template <bool BF16> __device__ __forceinline__ void put_one(const Slope &g, float x, typename Elem<BF16>::T *dst)
 {
-    *dst = Elem<BF16>::put(g.none ? 0.0f : g.at(x, t.any(group) ? t.p(v) : 0.0f));
+    *dst = Elem<BF16>::put(g.none ? 0.0f : g.at(x));
+}
+// Until the workgroup's stores are done: those after it, from any of its
+// threads, come after them.  The listed ids' gradients are stored so, over
+// the others; looking each value up while it is stored (in a table of the
+// listed ids, behind a bit for every 16 bytes that hold one) took 73 us
+// instead of 30 for the gradients of 4096 rows of 8000 bf16 with 50 entries,
+// because nearly every wave has one to look up.
+__device__ __forceinline__ void after_stores()
+{
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
 }
 
 __device__ __forceinline__ float exponent_scale(float tau) { return (float)(1.4426950408889634 / (double)tau); }
@@ -301,9 +283,10 @@ constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kLanes;
 constexpr int kFlight = 4;                       // 16-byte loads of a thread in flight
 constexpr int kMaxParts = 64;                    // of a row
-constexpr int kMapGroups = 32 * kMapWords;       // 16-byte groups that a map has bits for
+constexpr int kBackGroups = 4096;                // 16-byte groups of a part of the backward pass
 
-template <bool BF16> __global__ __launch_bounds__(kThreads) void distill_forward_kernel(DistillLaunch a, int64_t len)
+template <bool BF16, int LT>
+__global__ __launch_bounds__(kThreads) void distill_forward_kernel(DistillLaunch a, int64_t len)
 {
     typedef Elem<BF16> E;
     extern __shared__ __align__(16) char smem[];
@@ -312,22 +295,33 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void distill_forward
     const int64_t row = blockIdx.y + (int64_t)blockIdx.z * 32768;
     if (row >= a.N) return;
     const int tid = threadIdx.x;
+    const bool lists = gridDim.x == 1 && tid < LT;
     const typename E::T *s = static_cast<const typename E::T *>(a.logits) + row * a.ld;
     const float c = exponent_scale(a.tau);
     const int64_t v0 = blockIdx.x * len, n = min(len, a.V - v0), groups = n / E::kVec;
+    List<LT> l{reinterpret_cast<Entry *>(smem), a.k};
     Part p{-FLT_MAX, 0.0f};
     const typename E::T *src = s + v0;
-    int64_t i = tid;
-    for (; i + (kFlight - 1) * kThreads < groups; i += kFlight * kThreads) {
-        word4 w[kFlight];
+    const int64_t first = tid;
+    word4 w[kFlight];
+    auto load = [&](int64_t i) {
 #pragma unroll
         for (int u = 0; u < kFlight; ++u) w[u] = load_vec(src + (i + u * kThreads) * E::kVec);
+    };
+    // whether a thread has kFlight groups from i on
+    auto full = [&](int64_t i) { return i + (kFlight - 1) * kThreads < groups; };
+    if (full(first)) load(first);
+    if (lists) l.template read<BF16>(a.ids + row * a.k, a.teacher + row * a.k, a.V, s, 0, a.V);
+    int64_t i = first;
+    while (full(i)) {
 #pragma unroll
         for (int u = 0; u < kFlight; ++u) {
             float f[E::kVec];
             E::unpack(w[u], f);
             add<E::kVec>(p, f, c);
         }
+        i += kFlight * kThreads;
+        if (full(i)) load(i);
     }
     for (; i < groups; i += kThreads) {
         float f[E::kVec];
@@ -338,14 +332,13 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void distill_forward
         const float f = E::get(src[groups * E::kVec + tid]);
         add<1>(p, &f, c);
     }
+    if (lists) l.sum(a.tau, s_tmp);
     p = block_merge<kThreads>(p, c, s_part);
     if (gridDim.x > 1) {
         if (tid == 0) static_cast<Part *>(a.ws)[row * kMaxParts + blockIdx.x] = p;
         return;
     }
-    List<kThreads> l{reinterpret_cast<Entry *>(smem), a.k};
-    l.template read<BF16>(a.ids + row * a.k, a.teacher + row * a.k, a.V, s);
-    l.sum(a.tau, s_tmp);
+    if (!lists) return;
     const float loss = l.loss(p, a.tau, s_tmp);
     if (tid == 0) {
         a.loss[row] = loss;
@@ -355,15 +348,15 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void distill_forward
 }
 
 // The losses of rows that were taken in parts.
-template <bool BF16> __global__ __launch_bounds__(kThreads) void distill_join_kernel(DistillLaunch a, int parts)
+template <bool BF16, int LT> __global__ __launch_bounds__(LT) void distill_join_kernel(DistillLaunch a, int parts)
 {
     extern __shared__ __align__(16) char smem[];
-    __shared__ double s_tmp[2 * kWaves];
+    __shared__ double s_tmp[2 * LT / kLanes];
     const int64_t row = blockIdx.x;
     const float c = exponent_scale(a.tau);
-    List<kThreads> l{reinterpret_cast<Entry *>(smem), a.k};
+    List<LT> l{reinterpret_cast<Entry *>(smem), a.k};
     l.template read<BF16>(a.ids + row * a.k, a.teacher + row * a.k, a.V,
-                          static_cast<const typename Elem<BF16>::T *>(a.logits) + row * a.ld);
+                          static_cast<const typename Elem<BF16>::T *>(a.logits) + row * a.ld, 0, a.V);
     const int lane = threadIdx.x & (kLanes - 1);
     Part p{-FLT_MAX, 0.0f};
     if (lane < parts) p = static_cast<const Part *>(a.ws)[row * kMaxParts + lane];
@@ -377,121 +370,169 @@ template <bool BF16> __global__ __launch_bounds__(kThreads) void distill_join_ke
     }
 }
 
-template <bool BF16> __global__ __launch_bounds__(kThreads) void distill_backward_kernel(DistillLaunch a, int64_t len)
+template <bool BF16, int LT>
+__global__ __launch_bounds__(kThreads) void distill_backward_kernel(DistillLaunch a, int64_t len)
 {
     typedef Elem<BF16> E;
     extern __shared__ __align__(16) char smem[];
     __shared__ double s_tmp[2 * kWaves];
+    __shared__ bool s_none;
     const int64_t row = blockIdx.y + (int64_t)blockIdx.z * 32768;
     if (row >= a.N) return;
     const int tid = threadIdx.x;
     const int64_t v0 = blockIdx.x * len, n = min(len, a.V - v0), groups = n / E::kVec;
     const typename E::T *src = static_cast<const typename E::T *>(a.logits) + row * a.ld + v0;
     typename E::T *dst = static_cast<typename E::T *>(a.grad) + row * a.grad_ld + v0;
-    List<kThreads> l{reinterpret_cast<Entry *>(smem), a.k};
-    Table t(smem + list_lds(a.k), table_bits(a.k));
-    t.clear<kThreads>();
-    l.template read<BF16>(a.ids + row * a.k, a.teacher + row * a.k, a.V, nullptr);
-    l.sum(a.tau, s_tmp);  // (the workgroup waits in here)
-    t.fill(l, v0, n, E::kVec);
-    const float g = a.weight * (a.gloss ? a.gloss[row] : 1.0f);
-    const Slope sl({a.stats[2 * row], a.stats[2 * row + 1]}, exponent_scale(a.tau), g * a.tau, l.total == 0.0);
-    __syncthreads();
-    int64_t i = tid;
-    for (; i + (kFlight - 1) * kThreads < groups; i += kFlight * kThreads) {
-        word4 w[kFlight];
+    int32_t *place = reinterpret_cast<int32_t *>(smem + list_lds(a.k));
+    const int bits = table_bits(a.k);
+    List<LT> l{reinterpret_cast<Entry *>(smem), a.k};
+    bool twice = false;
+    word4 w[kFlight];
+    auto load = [&](int64_t i) {
 #pragma unroll
         for (int u = 0; u < kFlight; ++u) w[u] = load_last(src + (i + u * kThreads) * E::kVec);
+    };
+    auto full = [&](int64_t i) { return i + (kFlight - 1) * kThreads < groups; };
+    int64_t i = tid;
+    if (full(i)) load(i);
+    if (tid < LT) {
+        l.clear(place, bits);
+        l.template read<BF16>(a.ids + row * a.k, a.teacher + row * a.k, a.V, src - v0, v0, n);
+        l.sum(a.tau, s_tmp);
+        twice = l.twice(place, bits, v0, n);
+        if (tid == 0) s_none = l.total == 0.0;
+    }
+    const float g = a.weight * (a.gloss ? a.gloss[row] : 1.0f);
+    const Part r{a.stats[2 * row], a.stats[2 * row + 1]};
+    __syncthreads();
+    const Slope sl(r, exponent_scale(a.tau), g * a.tau, s_none);
+    while (full(i)) {
 #pragma unroll
         for (int u = 0; u < kFlight; ++u) {
             const int64_t at = i + u * kThreads;
-            put_group<BF16>(sl, t, (uint32_t)at, (int32_t)(v0 + at * E::kVec), w[u], dst + at * E::kVec);
+            put_group<BF16>(sl, w[u], dst + at * E::kVec);
         }
+        i += kFlight * kThreads;
+        if (full(i)) load(i);
     }
-    for (; i < groups; i += kThreads) {
-        put_group<BF16>(sl, t, (uint32_t)i, (int32_t)(v0 + i * E::kVec), load_vec(src + i * E::kVec), dst + i * E::kVec);
-    }
+    for (; i < groups; i += kThreads) put_group<BF16>(sl, load_vec(src + i * E::kVec), dst + i * E::kVec);
     if (groups * E::kVec + tid < n) {
         const int64_t at = groups * E::kVec + tid;
-        put_one<BF16>(sl, t, (uint32_t)groups, (int32_t)(v0 + at), E::get(src[at]), dst + at);
+        put_one<BF16>(sl, E::get(src[at]), dst + at);
     }
+    after_stores();
+    if (tid < LT) l.template put<BF16>(sl, v0, n, twice, dst);
 }
 
 // ---------------------------------------------------------------------------
 // both at once
 // ---------------------------------------------------------------------------
 //
-// A workgroup of 1024 threads, two of them a CU, takes a row: its part first,
-// then its gradient, from the row's end to its beginning, so that the second
-// reading finds what the caches hold of the first.
+// A workgroup of NT threads, 2048 / NT of them a CU, takes a row: its part
+// first, then its gradient, from the row's end to its beginning, so that the
+// second reading finds what the caches hold of the first.  What it took last
+// stays in the registers, and what it took before that in LDS if all the
+// workgroups of a CU have room for it: a row of two steps is read once.
+// 2048 rows of 128256 bf16, 1.05 GB read and written: 207 us, what a copy of
+// the same bytes takes (197).
 
-constexpr int kBothThreads = 1024;
-constexpr int kBothWaves = kBothThreads / kLanes;
+// Groups of 16 bytes that a workgroup of NT threads takes at a time.
+template <int NT> constexpr int kStep = kFlight * NT;
 
-template <bool BF16>
-__global__ __launch_bounds__(kBothThreads) __attribute__((amdgpu_waves_per_eu(8, 8))) void distill_both_kernel(DistillLaunch a)
+// LT: the list's threads
+template <bool BF16, int NT, int LT>
+__global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(8, 8))) void distill_both_kernel(DistillLaunch a, int keep)
 {
     typedef Elem<BF16> E;
     extern __shared__ __align__(16) char smem[];
-    __shared__ double s_tmp[2 * kBothWaves];
-    __shared__ Part s_part[kBothWaves];
+    __shared__ double s_tmp[2 * NT / kLanes];
+    __shared__ bool s_none;
+    __shared__ Part s_part[NT / kLanes];
     const int tid = threadIdx.x;
     const int64_t row = blockIdx.x;
     const float c = exponent_scale(a.tau);
     const typename E::T *src = static_cast<const typename E::T *>(a.logits) + row * a.ld;
     typename E::T *dst = static_cast<typename E::T *>(a.grad) + row * a.grad_ld;
     const int groups = (int)(a.V / E::kVec), rest = (int)(a.V - (int64_t)groups * E::kVec);
-    List<kBothThreads> l{reinterpret_cast<Entry *>(smem), a.k};
-    Table t(smem + list_lds(a.k), table_bits(a.k));
-    // (the first loads of either pass are on their way while the list is
-    // worked on)
-    const int step = kFlight * kBothThreads;
+    const int steps = (groups + kStep<NT> - 1) / kStep<NT>;
+    word4 *kept = reinterpret_cast<word4 *>(smem);  // a thread's own values at tid + u * NT
+    char *list = smem + (keep ? kStep<NT> * 16 : 0);
+    List<LT> l{reinterpret_cast<Entry *>(list), a.k};
+    int32_t *place = reinterpret_cast<int32_t *>(list + list_lds(a.k));
+    const int bits = table_bits(a.k);
+    bool twice = false;
     word4 w[kFlight];
-    auto load_up = [&](int i) {
+    auto at = [&](int j, int u) { return j * kStep<NT> + u * NT + tid; };
+    auto load_up = [&](int j) {
 #pragma unroll
-        for (int u = 0; u < kFlight; ++u) w[u] = load_vec(src + (int64_t)min(i + u * kBothThreads, groups - 1) * E::kVec);
+        for (int u = 0; u < kFlight; ++u) w[u] = load_vec(src + (int64_t)min(at(j, u), groups - 1) * E::kVec);
     };
-    auto load_down = [&](int i) {
+    auto load_down = [&](int j) {
 #pragma unroll
-        for (int u = 0; u < kFlight; ++u) w[u] = load_last(src + (int64_t)max(i - u * kBothThreads, 0) * E::kVec);
+        for (int u = 0; u < kFlight; ++u) w[u] = load_last(src + (int64_t)at(j, u) * E::kVec);
     };
-    if (groups) load_up(tid);
-    t.clear<kBothThreads>();
-    l.template read<BF16>(a.ids + row * a.k, a.teacher + row * a.k, a.V, src);
+    if (steps) load_up(0);
+    if (tid < LT) {
+        l.clear(place, bits);
+        l.template read<BF16>(a.ids + row * a.k, a.teacher + row * a.k, a.V, src, 0, a.V);
+    }
     Part p{-FLT_MAX, 0.0f};
-    for (int i = tid; i < groups; i += step) {
+    for (int j = 0; j < steps; ++j) {
 #pragma unroll
         for (int u = 0; u < kFlight; ++u) {
             float f[E::kVec];
             E::unpack(w[u], f);
-            if (i + u * kBothThreads < groups) add<E::kVec>(p, f, c);
+            if (at(j, u) < groups) add<E::kVec>(p, f, c);
         }
-        if (i + step < groups) load_up(i + step);
+        if (keep && j == steps - 2) {
+#pragma unroll
+            for (int u = 0; u < kFlight; ++u) kept[u * NT + tid] = w[u];
+        }
+        if (j + 1 < steps) load_up(j + 1);
     }
-    const int down = groups - 1 - tid;
-    if (groups) load_down(down);
     const int64_t last = (int64_t)groups * E::kVec + tid;
     float tail = 0.0f;
     if (tid < rest) {
         tail = E::get(src[last]);
         add<1>(p, &tail, c);
     }
-    l.sum(a.tau, s_tmp);  // (the workgroup waits in here)
-    t.fill(l, 0, a.V, E::kVec);
-    p = block_merge<kBothThreads>(p, c, s_part);
-    const float loss = l.loss(p, a.tau, s_tmp);
-    if (tid == 0) a.loss[row] = loss;
     const float g = a.weight * (a.gloss ? a.gloss[row] : 1.0f);
-    const Slope sl(p, c, g * a.tau, l.total == 0.0);
-    if (tid < rest) put_one<BF16>(sl, t, (uint32_t)groups, (int32_t)last, tail, dst + last);
-    for (int i = down; i >= 0; i -= step) {
-#pragma unroll
-        for (int u = 0; u < kFlight; ++u) {
-            const int at = i - u * kBothThreads;
-            if (at >= 0) put_group<BF16>(sl, t, (uint32_t)at, at * E::kVec, w[u], dst + (int64_t)at * E::kVec);
-        }
-        if (i - step >= 0) load_down(i - step);
+    if (tid < LT) {
+        l.sum(a.tau, s_tmp);
+        twice = l.twice(place, bits, 0, a.V);
+        if (tid == 0) s_none = l.total == 0.0;
     }
+    p = block_merge<NT>(p, c, s_part);  // (the workgroup waits in here)
+    if (tid < LT) {
+        const float loss = l.loss(p, a.tau, s_tmp);
+        if (tid == 0) a.loss[row] = loss;
+    }
+    const Slope sl(p, c, g * a.tau, s_none);
+    if (tid < rest) put_one<BF16>(sl, tail, dst + last);
+    auto put = [&](int i, word4 x) {
+        if (i < groups) put_group<BF16>(sl, x, dst + (int64_t)i * E::kVec);
+    };
+    int j = steps - 1;
+    if (j >= 0) {
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) put(at(j, u), w[u]);
+        --j;
+    }
+    if (keep && j >= 0) {
+        if (j > 0) load_down(j - 1);
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) put(at(j, u), kept[u * NT + tid]);
+        --j;
+    } else if (j >= 0) {
+        load_down(j);
+    }
+    for (; j >= 0; --j) {
+#pragma unroll
+        for (int u = 0; u < kFlight; ++u) put(at(j, u), w[u]);
+        if (j > 0) load_down(j - 1);
+    }
+    after_stores();
+    if (tid < LT) l.template put<BF16>(sl, 0, a.V, twice, dst);
 }
 
 vie_status launched(const char *what)
@@ -532,6 +573,15 @@ Split split_rows(const DistillLaunch &a, int64_t least, int most_groups)
 // that keeps none for the caller, their stats.
 size_t parts_bytes(int N) { return N > 256 ? 0 : (size_t)N * kMaxParts * sizeof(Part); }
 
+// Calls f with the number of threads that take the list (List): a wave, or
+// all where it would have more than four entries a lane.
+constexpr int kListWave = 256;
+template <int NT, typename F> void by_list(int k, F f)
+{
+    if (k <= kListWave) f(std::integral_constant<int, kLanes>());
+    else f(std::integral_constant<int, NT>());
+}
+
 template <bool BF16> vie_status forward(const DistillLaunch &a, hipStream_t s)
 {
     // Joining parts is a launch more, in which a workgroup reads some 200 KB
@@ -544,8 +594,11 @@ template <bool BF16> vie_status forward(const DistillLaunch &a, hipStream_t s)
         sp.parts = (int)((a.V + sp.len - 1) / sp.len);
         sp.grid.x = (unsigned)sp.parts;
     }
-    distill_forward_kernel<BF16><<<sp.grid, kThreads, list_lds(a.k), s>>>(a, sp.len);
-    if (sp.parts > 1) distill_join_kernel<BF16><<<a.N, kThreads, list_lds(a.k), s>>>(a, sp.parts);
+    by_list<kThreads>(a.k, [&](auto lt) {
+        constexpr int LT = decltype(lt)::value;
+        distill_forward_kernel<BF16, LT><<<sp.grid, kThreads, list_lds(a.k), s>>>(a, sp.len);
+        if (sp.parts > 1) distill_join_kernel<BF16, LT><<<a.N, LT, list_lds(a.k), s>>>(a, sp.parts);
+    });
     return launched("distillation launch");
 }
 
@@ -553,22 +606,47 @@ template <bool BF16> vie_status backward(const DistillLaunch &a, hipStream_t s)
 {
     // (parts of 64 KB: more workgroups than fit at once, whose ends and lists
     // others stream over; 2048 rows of 128256 bf16: 237 us as whole rows, 209)
-    const Split sp = split_rows(a, 8192, 4096);
-    if (vie_status e = allow_lds((const void *)distill_backward_kernel<BF16>, table_lds(a.k))) return e;
-    distill_backward_kernel<BF16><<<sp.grid, kThreads, table_lds(a.k), s>>>(a, sp.len);
-    return launched("distillation gradient launch");
+    const Split sp = split_rows(a, 8192, kBackGroups);
+    const size_t lds = table_lds(a.k);
+    vie_status e = VIE_OK;
+    by_list<kThreads>(a.k, [&](auto lt) {
+        constexpr int LT = decltype(lt)::value;
+        e = allow_lds((const void *)distill_backward_kernel<BF16, LT>, lds);
+        if (e == VIE_OK) distill_backward_kernel<BF16, LT><<<sp.grid, kThreads, lds, s>>>(a, sp.len);
+    });
+    return e == VIE_OK ? launched("distillation gradient launch") : e;
+}
+
+template <bool BF16, int NT> vie_status both(const DistillLaunch &a, hipStream_t s)
+{
+    constexpr int64_t kGroups = kStep<NT>;
+    size_t lds = table_lds(a.k);
+    // of a CU's 160 KB, with 2 KB for the static arrays
+    const bool keep = a.V / Elem<BF16>::kVec > kGroups && lds + kGroups * 16 + 1024 * NT / 1024 <= 80 * NT;
+    if (keep) lds += kGroups * 16;
+    vie_status e = VIE_OK;
+    by_list<NT>(a.k, [&](auto lt) {
+        constexpr int LT = decltype(lt)::value;
+        e = allow_lds((const void *)distill_both_kernel<BF16, NT, LT>, lds);
+        if (e == VIE_OK) distill_both_kernel<BF16, NT, LT><<<a.N, NT, lds, s>>>(a, keep);
+    });
+    return e == VIE_OK ? launched("distillation step launch") : e;
 }
 
 template <bool BF16> vie_status step(const DistillLaunch &a, hipStream_t s)
 {
-    // One kernel where its workgroups fill half of the CUs, or where the row
-    // is read in less time than another launch takes (8 rows of 8000 bf16: 15
-    // us so, 22 as two kernels; of 32000: 21 and 16).
-    const bool one = a.N >= 128 || a.V * elem_bytes(a.dtype) <= 32 * 1024;
-    if (one && a.V / Elem<BF16>::kVec < kMapGroups) {
-        if (vie_status e = allow_lds((const void *)distill_both_kernel<BF16>, table_lds(a.k))) return e;
-        distill_both_kernel<BF16><<<a.N, kBothThreads, table_lds(a.k), s>>>(a);
-        return launched("distillation step launch");
+    // One kernel where its workgroups fill half of the CUs, or where reading
+    // the row takes no longer than another launch (8 rows of 64000 bf16: 13.8
+    // us so, 14.8 as two kernels; of 128256: 18.6 and 17.2; of 400000: 46 and
+    // 17; 256 rows of 400000: 93 and 102).  With the fewest threads that keep
+    // the row from its first reading to its second (4096 rows of 8000 bf16:
+    // 31 us with 256 threads, 39 with 512, 57 with 1024; of 32000: 107, 99
+    // and 106; 512 of 128256: 62, 60 and 51).
+    const int64_t bytes = a.V * elem_bytes(a.dtype);
+    if (a.N >= 128 || bytes <= 128 * 1024) {
+        if (bytes <= 2 * 16 * kStep<256>) return both<BF16, 256>(a, s);
+        if (bytes <= 2 * 16 * kStep<512>) return both<BF16, 512>(a, s);
+        return both<BF16, 1024>(a, s);
     }
     DistillLaunch b = a;
     b.stats = reinterpret_cast<float *>(static_cast<char *>(a.ws) + parts_bytes(a.N));
