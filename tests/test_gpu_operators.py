@@ -427,7 +427,11 @@ DISTILL_CASES = [(1, 1, 1, F32, 1.0, "plain"), (2, 2, 3, BF16, 2.0, "plain"), (3
                  (13, 1000, 50, BF16, 1.0, "odd"), (13, 1000, 50, F32, 3.0, "odd"), (12, 4099, 2048, F32, 1.0, "odd"),
                  (5, 50257, 64, BF16, 2.0, "plain"), (1, 262144, 50, F32, 1.0, "plain"), (2, 151936, 1000, BF16, 4.0, "odd"),
                  (700, 300, 20, BF16, 1.0, "odd"), (1200, 129, 5, F32, 1.0, "odd"), (40, 9001, 600, F32, 0.05, "odd"),
-                 (300, 20000, 64, BF16, 2.0, "odd")]
+                 (300, 20000, 64, BF16, 2.0, "odd"),
+                 # the step's widths, with and without room to keep a row, one step of it and several
+                 (12, 12001, 33, BF16, 1.0, "odd"), (11, 8000, 300, F32, 2.0, "odd"), (11, 30000, 60, BF16, 1.0, "odd"),
+                 (11, 30001, 800, BF16, 2.0, "odd"), (11, 31001, 20, F32, 1.0, "odd"), (130, 70001, 40, BF16, 2.0, "odd"),
+                 (128, 40003, 1500, F32, 1.0, "odd"), (129, 100003, 300, BF16, 1.0, "odd")]
 
 
 @pytest.mark.parametrize("N,V,k,dtype,tau,kind", DISTILL_CASES)
