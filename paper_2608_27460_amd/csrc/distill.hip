@@ -278,6 +278,11 @@ __device__ __forceinline__ float exponent_scale(float tau) { return (float)(1.44
 // ---------------------------------------------------------------------------
 // forward and backward apart: rows in parts, streamed
 // ---------------------------------------------------------------------------
+//
+// Both are bound by memory where there are rows enough: 2048 rows of 128256
+// bf16 forward in 92 us (5.7 TB/s read), backward in 177 (5.9 TB/s read and
+// written).  Few rows are bound by one workgroup's way through a row: 48 rows
+// of 32768 fp32 forward in 7 us, of which a launch is 3.5.
 
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kLanes;
@@ -573,9 +578,13 @@ Split split_rows(const DistillLaunch &a, int64_t least, int most_groups)
 // that keeps none for the caller, their stats.
 size_t parts_bytes(int N) { return N > 256 ? 0 : (size_t)N * kMaxParts * sizeof(Part); }
 
-// Calls f with the number of threads that take the list (List): a wave, or
-// all where it would have more than four entries a lane.
-constexpr int kListWave = 256;
+// Calls f with the number of threads that take the list (List): a wave while
+// it is no longer at it than the others at the row.  Forward, gradient and
+// both in us with a wave and with all, for 1024 rows of 32000 bf16: lists of
+// 128 17/30/28 and 19/29/28, of 256 17/36/34 and 20/31/31, of 512 22/48/45
+// and 23/37/38; for 48 rows: of 128 6.1/6.0/9.9 and 6.9/5.9/10.5, of 256
+// 7.5/8.2/13.6 and 7.1/6.0/11.2.
+constexpr int kListWave = 128;
 template <int NT, typename F> void by_list(int k, F f)
 {
     if (k <= kListWave) f(std::integral_constant<int, kLanes>());
@@ -584,10 +593,10 @@ template <int NT, typename F> void by_list(int k, F f)
 
 template <bool BF16> vie_status forward(const DistillLaunch &a, hipStream_t s)
 {
-    // Joining parts is a launch more, in which a workgroup reads some 200 KB
-    // of a row (one row of 65536 bf16: 12 us whole, 14 in parts; of 262144:
-    // 18 and 15).
-    const bool whole = a.V * elem_bytes(a.dtype) <= 192 * 1024;
+    // Joining parts is a launch more, in which a workgroup reads 150 KB of a
+    // row (one row of 65536 bf16: 6.7 us whole, 7.6 in parts; of 98304: 8.4
+    // and 7.6; 48 rows of 65536: 7.1 and 8.1, of 98304: 8.8 and 8.1).
+    const bool whole = a.V * elem_bytes(a.dtype) <= 150 * 1024;
     Split sp = split_rows(a, whole ? a.V : 32768, INT32_MAX);
     if (sp.parts > kMaxParts) {
         sp.len = ((a.V + kMaxParts - 1) / kMaxParts + 63) / 64 * 64;
@@ -605,7 +614,8 @@ template <bool BF16> vie_status forward(const DistillLaunch &a, hipStream_t s)
 template <bool BF16> vie_status backward(const DistillLaunch &a, hipStream_t s)
 {
     // (parts of 64 KB: more workgroups than fit at once, whose ends and lists
-    // others stream over; 2048 rows of 128256 bf16: 237 us as whole rows, 209)
+    // others stream over; 2048 rows of 128256 bf16: 200 us as whole rows, 187
+    // in parts of 128 KB, 177 so and in parts of 32)
     const Split sp = split_rows(a, 8192, kBackGroups);
     const size_t lds = table_lds(a.k);
     vie_status e = VIE_OK;

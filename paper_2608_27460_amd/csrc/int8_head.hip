@@ -169,7 +169,19 @@ __global__ __launch_bounds__(256) void int8_simple_kernel(const int8_t *__restri
 // (DMA false) go to LDS by way of registers, two stages ahead.
 //
 // The logits leave through LDS of each wave's own, 16 tokens at a time, so
-// that a store covers runs of up to 256 bytes of a token's row; the stages of the next tile go on arriving meanwhile.
+// that a store covers runs of up to 256 bytes of a token's row; the stages of
+// the next tile go on arriving meanwhile.
+//
+// The waits count loads and stores (vmcnt) that this source issues: a kernel
+// of these that spilled registers would add its own, and must not.
+//
+// What bounds it: up to 128 tokens the reading of the rows (151936 x 1024, 1
+// token: 28 us or 5.5 TB/s, past the last-level cache; 128256 x 2048, 64
+// tokens: 60 us with the tokens' own kernel, 4.7 TB/s of rows and logits
+// together).  With more, a compute unit's loads and its products, which take
+// 301 and 318 us of 2048 tokens' 506 if each is alone, at the clock (1.9 GHz)
+// that the matrix cores leave: 2.1e15 operations a second, where the library's
+// product of 8192^3 reaches 2.0e15.
 
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kLanes;
@@ -199,8 +211,16 @@ constexpr int kHeldPad = 16;         // bytes between them: 16 rows' reads hit e
 constexpr int tile_stage(int BT, int KC) { return (kTileRows + BT) * KC; }
 constexpr int tile_out(int MT) { return 512 * MT; }  // of a wave, for its logits on their way out
 constexpr int tile_lds(int stage, int NBUF, int MT, bool held) { return stage * NBUF + kWaves * tile_out(MT) + (held ? kHeldLds : 0); }
-inline bool tokens_fit(int64_t V, int B, int d)  // (and there are 16 bytes of rows, a load)
+// Whether the tokens are held.  Rows that are not aligned: wherever they fit
+// (there is nothing as fast for these rows), if there are 16 bytes of rows, a
+// load.  Aligned ones: as long as every workgroup's quantization takes less
+// than tokens_kernel's launch, held and apart in us: 32000 x 256, 4 tokens
+// 6.5 and 8.1, 16 tokens 8.6 and 8.5; 151936 x 1024, 4 tokens 33.6 and 35.6,
+// 12 tokens 35.6 and 36.2, 16 tokens 37.4 and 36.8; 128256 x 2048, 4 tokens
+// 51.1 and 52.4, 12 tokens 55.0 and 53.8; 32000 x 8192, 1 token 71 and 64.
+inline bool hold_tokens(int64_t V, int B, int d, bool aligned)
 {
+    if (aligned) return B <= 12 && d <= 2048 && B * padded(d) <= 12 * 1024;
     return B <= 16 && B * (padded(d) + kHeldPad) + 64 <= kHeldLds && V * d >= 16;
 }
 
@@ -676,6 +696,19 @@ hipError_t tile_launch(const Int8Launch &a, const int8_t *q, int pitch, const in
     return hipGetLastError();
 }
 
+// The tile that takes all tokens at once, up to 128 of them: a larger one has
+// products of nothing, a smaller one reads the rows more than once.  In us at
+// 128256 x 2048 to bf16, with the tiles of 16, 32, 64, 128 and 256 tokens:
+//    16 tokens   53   53   54   60   77
+//    17          62   53   54   61   76
+//    32          64   54   55   62   77
+//    33          77   64   55   61   77
+//    64          98   67   57   64   77
+//    65         111   80   69   64   77
+//   128         171  103   75   68   80
+//   129         226  118   89   95   80
+//   512         628  348  219  194  143
+// Where the rows bound it, the tiles are as even as the rows allow.
 template <bool OUT_BF16>
 hipError_t tiles_launch(const Int8Launch &a, const int8_t *q, int pitch, const int8_t *x, const float *xs, hipStream_t s)
 {
@@ -705,17 +738,21 @@ __global__ __launch_bounds__(256) void repack_kernel(const int8_t *__restrict__ 
         *reinterpret_cast<word4 *>(to + v * pitch + c) = load16(q + v * d + c, q + V * d);
 }
 int row_pitch(int d) { return (d + 15) / 16 * 16; }
-// From so many tokens on, unaligned rows are copied first: read and written
-// once for it, where int8_simple_kernel would read them for every 16 tokens.
-constexpr int kRepackTokens = 33;
+// Whether unaligned rows are copied first: read and written once for it,
+// where int8_simple_kernel reads them for every 16 tokens, and the worse the
+// longer they are.  In us copied and not: 50257 x 1000, 32 tokens 34 and 31,
+// 33 tokens 35 and 40, 64 tokens 35 and 52; 151936 x 1001, 32 tokens 87 and
+// 98; 20000 x 4097, 17 tokens 51 and 110.
+bool copy_rows(int B, int d) { return d % 16 != 0 && (B > 32 || d > 2048); }
 }  // namespace
 
 // The tokens' int8 values and scales, and unaligned rows copied.
 size_t int8_workspace_bytes(int64_t V, int d, int B)
 {
-    if (tokens_fit(V, B, d)) return 0;
+    // (rows at an odd address, of a multiple of 16 bytes, ask for less)
+    if (hold_tokens(V, B, d, d % 16 == 0)) return 0;
     const size_t tokens = (tokens_bytes(d, B) + (size_t)B * 4 + 255) & ~(size_t)255;
-    return tokens + (d % 16 && B >= kRepackTokens ? (size_t)V * row_pitch(d) : 0);
+    return tokens + (copy_rows(B, d) ? (size_t)V * row_pitch(d) : 0);
 }
 
 vie_status launch_int8_logits(const Int8Launch &a, hipStream_t s)
@@ -724,7 +761,8 @@ vie_status launch_int8_logits(const Int8Launch &a, hipStream_t s)
         return e == hipSuccess ? VIE_OK : fail(VIE_EHIP, "int8 head launch: %s", hipGetErrorString(e));
     };
     const bool bf16 = a.out_dtype == VIE_BF16, aligned = a.d % 16 == 0 && (uintptr_t)a.q % 16 == 0;
-    if (tokens_fit(a.V, a.B, a.d)) return done(a.h_dtype == VIE_BF16 ? few_launch<true>(a, aligned, s) : few_launch<false>(a, aligned, s));
+    if (hold_tokens(a.V, a.B, a.d, aligned))
+        return done(a.h_dtype == VIE_BF16 ? few_launch<true>(a, aligned, s) : few_launch<false>(a, aligned, s));
     int8_t *x = static_cast<int8_t *>(a.ws);
     float *xs = reinterpret_cast<float *>(x + tokens_bytes(a.d, a.B));
     if (a.h_dtype == VIE_BF16) tokens_kernel<true><<<a.B, kTokenThreads, 0, s>>>(static_cast<const uint16_t *>(a.h), a.d, x, xs);
@@ -732,7 +770,7 @@ vie_status launch_int8_logits(const Int8Launch &a, hipStream_t s)
     if (vie_status e = launched("token quantization launch")) return e;
     const int8_t *q = a.q;
     int pitch = a.d;
-    if (a.d % 16 && a.B >= kRepackTokens) {
+    if (copy_rows(a.B, a.d)) {
         int8_t *to = x + ((tokens_bytes(a.d, a.B) + (size_t)a.B * 4 + 255) & ~(size_t)255);
         pitch = row_pitch(a.d);
         repack_kernel<<<(unsigned)((a.V + 3) / 4), 256, 0, s>>>(a.q, a.V, a.d, to, pitch);
