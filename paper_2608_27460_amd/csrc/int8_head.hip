@@ -172,16 +172,17 @@ __global__ __launch_bounds__(256) void int8_simple_kernel(const int8_t *__restri
 // that a store covers runs of up to 256 bytes of a token's row; the stages of
 // the next tile go on arriving meanwhile.
 //
-// The waits count loads and stores (vmcnt) that this source issues: a kernel
-// of these that spilled registers would add its own, and must not.
+// The waits count the loads and stores (vmcnt) that this source issues: a
+// kernel of these that spilled registers would wait for its own too.
 //
 // What bounds it: up to 128 tokens the reading of the rows (151936 x 1024, 1
-// token: 28 us or 5.5 TB/s, past the last-level cache; 128256 x 2048, 64
-// tokens: 60 us with the tokens' own kernel, 4.7 TB/s of rows and logits
-// together).  With more, a compute unit's loads and its products, which take
-// 301 and 318 us of 2048 tokens' 506 if each is alone, at the clock (1.9 GHz)
-// that the matrix cores leave: 2.1e15 operations a second, where the library's
-// product of 8192^3 reaches 2.0e15.
+// token: 28 us or 5.6 TB/s; 128256 x 2048, 64 tokens: 60 us with the tokens'
+// own kernel, 4.7 TB/s of rows and logits together).  With more, a compute
+// unit's loads and its products, which take 301 and 318 us of 2048 tokens' 506
+// if each is alone, at the clock (1.9 GHz) that the matrix cores leave: 2.1e15
+// operations a second, where the library's product of 8192^3 reaches 2.0e15.
+// Four waves of 128 x 128, which read a third less from LDS and whose matrix
+// instructions follow each other without a pause, are no faster (560 us).
 
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kLanes;
