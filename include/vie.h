@@ -363,7 +363,9 @@ vie_status vie_scatter(const int32_t *ids_dev, const float *logits_dev, int32_t 
  * Around the head's logits: the int8 head, the token drawn, distillation
  * ------------------------------------------------------------------------
  * Full-vocabulary rows may be strided: row b starts at element b * ld, ld >=
- * V; what lies between rows is neither read nor written.  Workspaces are
+ * V; what lies between rows is neither read nor written.  Outputs overlap
+ * neither inputs nor each other, but for a gradient in place of its logits
+ * (VIE_EINVAL).  Workspaces are
  * 256-byte aligned device buffers of the caller's, need no initialisation,
  * and carry data between the kernels of one call only: calls that share one
  * must not overlap in time. */
@@ -405,10 +407,10 @@ typedef struct {
  * none), ordered by logit descending, then id ascending, whatever their
  * order in the list.  With l_1 the best logit and t the temperature,
  * candidate j weighs w_j = exp((l_j - l_1) / t) (1 where l_j = l_1, else 0
- * where l_1 is +inf) and C_j = w_1 + .. + w_j.  Kept is the shortest of three prefixes, and at least one
- * candidate: the first K = min(top_k, candidates); the first n with C_n >=
- * top_p C_K; those with w_j >= min_p.  The token is the first j with C_j > u
- * C_kept.  Sums are 64-bit integers of weights rounded to 2^-44 of the best
+ * where l_1 is +inf) and C_j = w_1 + .. + w_j.  Kept is the shortest of
+ * three prefixes, and at least one candidate: the first K = min(top_k,
+ * candidates); the first n with C_n >= top_p C_K; those with w_j >= min_p.
+ * The token is the first j with C_j > u C_kept.  Sums are 64-bit integers of weights rounded to 2^-44 of the best
  * one or finer (for up to 2^18 candidates), so results do not depend on the
  * order of additions.
  *   token_dev int32[B] receives the id, prob_dev fp32[B] (or NULL) its
@@ -444,11 +446,11 @@ vie_status vie_distill_workspace(int64_t V, int32_t N, size_t *bytes);
  *   logit not -inf), q = softmax of s / tau over the V ids,
  *   loss = tau^2 sum_j p_j (log p_j - log q[id_j])
  * (entries whose p_j rounds to zero add nothing).  An id listed more than
- * once counts with each of its entries.  A row that lists nothing has loss 0.  A NaN or +inf
- * among the logits of either side gives NaN, as does a row of the student's
- * that is -inf throughout.  loss_dev fp32[N]; stats_dev fp32[N][2] receives what
- * vie_distill_grad needs: the row's largest logit and the sum of
- * exp((s - largest) / tau).
+ * once counts with each of its entries.  A row that lists nothing has loss 0.
+ * A NaN or +inf among the logits of either side gives NaN, as does a row of
+ * the student's that is -inf throughout.  loss_dev fp32[N]; stats_dev
+ * fp32[N][2] receives what vie_distill_grad needs: the row's largest logit
+ * and the sum of exp((s - largest) / tau).
  * Errors: VIE_EINVAL, VIE_EHIP. */
 vie_status vie_distill(const void *logits_dev, vie_dtype dtype, int32_t N, int64_t V, int64_t ld,
                        const int32_t *ids_dev, const float *teacher_dev, int32_t k, float tau, float *loss_dev,

@@ -69,6 +69,29 @@ size_t matrix_bytes(int32_t rows, int64_t V, int64_t ld, int32_t dtype)
     return ((size_t)(rows - 1) * ld + V) * elem_bytes(dtype);
 }
 
+struct Range {
+    const void *p;
+    size_t bytes;
+};
+// Outputs (the first n_out ranges) apart from each other and from the inputs;
+// a NULL range is none.
+template <int N> vie_status check_ranges(const Range (&r)[N], int n_out)
+{
+    for (int i = 0; i < n_out; ++i)
+        for (int j = i + 1; j < N; ++j)
+            if (r[i].p && r[j].p && overlap(r[i].p, r[i].bytes, r[j].p, r[j].bytes))
+                return fail(VIE_EINVAL, "an output overlaps another argument");
+    return VIE_OK;
+}
+vie_status check_sample(const SampleLaunch &a)
+{
+    const size_t n = (size_t)a.B * 4;
+    const Range r[] = {{a.token, n}, {a.prob, n}, {a.kept, n}, {a.u, n}, {a.logits, matrix_bytes(a.B, a.n, a.ld, a.dtype)},
+                       {a.ids, n * (size_t)a.n}, {a.prm.temperature_dev, n}, {a.prm.top_k_dev, n},
+                       {a.prm.top_p_dev, n}, {a.prm.min_p_dev, n}};
+    return check_ranges(r, 3);
+}
+
 // The gradient's rows are the logits' own or apart from them.
 vie_status check_apart(const DistillLaunch &a)
 {
@@ -80,6 +103,19 @@ vie_status check_apart(const DistillLaunch &a)
     if (overlap(a.logits, matrix_bytes(a.N, a.V, a.ld, a.dtype), a.grad, matrix_bytes(a.N, a.V, a.grad_ld, a.dtype)))
         return fail(VIE_EINVAL, "the gradient overlaps the logits without being in their place");
     return VIE_OK;
+}
+// What is written of a distillation apart from the rest (but for a gradient
+// in place of the logits).
+vie_status check_distilled(const DistillLaunch &a, bool stats_out)
+{
+    const size_t n = (size_t)a.N * 4, list = n * (size_t)a.k;
+    const Range g{a.grad, a.grad ? matrix_bytes(a.N, a.V, a.grad_ld, a.dtype) : 0};
+    const Range logits{a.grad == a.logits ? nullptr : a.logits, matrix_bytes(a.N, a.V, a.ld, a.dtype)};
+    const Range stats{a.stats, 2 * n};
+    const Range none{nullptr, 0};
+    const Range r[] = {g, {a.loss, n}, stats_out ? stats : none, logits, stats_out ? none : stats, {a.ids, list},
+                       {a.teacher, list}, {a.gloss, n}};
+    return check_ranges(r, 3);
 }
 
 }  // namespace
@@ -125,6 +161,7 @@ vie_status vie_sample(const int32_t *ids_dev, const float *logits_dev, int32_t B
     if (vie_status s = check_rows(B, 1)) return s;
     if (vie_status s = check_list(k)) return s;
     const SampleLaunch a{ids_dev, logits_dev, VIE_F32, k, k, B, *params, u_dev, token_dev, prob_dev, kept_dev, nullptr};
+    if (vie_status s = check_sample(a)) return s;
     return launch_sample_lists(a, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -148,6 +185,7 @@ vie_status vie_sample_rows(const void *logits_dev, vie_dtype dtype, int64_t V, i
     if (vie_status s = check_workspace(workspace_dev, workspace_bytes, sample_rows_workspace_bytes(V, B))) return s;
     const SampleLaunch a{nullptr, logits_dev, dtype, V, ld, B, *params, u_dev, token_dev, prob_dev, kept_dev,
                          workspace_dev};
+    if (vie_status s = check_sample(a)) return s;
     return launch_sample_rows(a, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -170,6 +208,7 @@ vie_status vie_distill(const void *logits_dev, vie_dtype dtype, int32_t N, int64
     if (vie_status s = check_workspace(workspace_dev, workspace_bytes, distill_workspace_bytes(V, N))) return s;
     const DistillLaunch a{logits_dev, dtype, N, V, ld, ids_dev, teacher_dev, k, tau, loss_dev, stats_dev,
                           nullptr, 1.0f, nullptr, 0, workspace_dev};
+    if (vie_status s = check_distilled(a, true)) return s;
     return launch_distill(a, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -185,6 +224,7 @@ vie_status vie_distill_grad(const void *logits_dev, vie_dtype dtype, int32_t N, 
     const DistillLaunch a{logits_dev, dtype, N, V, ld, ids_dev, teacher_dev, k, tau, nullptr,
                           const_cast<float *>(stats_dev), gloss_dev, weight, grad_dev, grad_ld, nullptr};
     if (vie_status s = check_apart(a)) return s;
+    if (vie_status s = check_distilled(a, false)) return s;
     return launch_distill_grad(a, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -201,6 +241,7 @@ vie_status vie_distill_step(const void *logits_dev, vie_dtype dtype, int32_t N, 
     const DistillLaunch a{logits_dev, dtype, N, V, ld, ids_dev, teacher_dev, k, tau, loss_dev, nullptr,
                           gloss_dev, weight, grad_dev, grad_ld, workspace_dev};
     if (vie_status s = check_apart(a)) return s;
+    if (vie_status s = check_distilled(a, false)) return s;
     return launch_distill_step(a, static_cast<hipStream_t>(hip_stream));
 }
 

@@ -479,7 +479,7 @@ def _sampling(B: int, device, temperature, top_k, top_p, min_p) -> SamplingParam
         if isinstance(v, torch.Tensor):
             setattr(p, name + "_dev", _values(v, name, torch.int32 if name == "top_k" else torch.float32, (B,), device))
         else:
-            setattr(p, name, v)
+            setattr(p, name, max(-1, min(v, 0x7FFFFFFF)) if name == "top_k" else v)
     return p
 
 

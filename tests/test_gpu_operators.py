@@ -89,6 +89,8 @@ INT8_CASES = [
     (4099, 65, 40, F32, BF16), (3001, 1001, 200, BF16, F32), (1500, 8191, 20, F32, F32), (5000, 1000, 16, BF16, BF16),
     (777, 2040, 16, F32, F32), (9000, 4100, 3, BF16, BF16), (70000, 33, 2, F32, BF16), (3000, 4096, 8, F32, F32),
     (131073, 16, 1, BF16, F32), (500, 8192, 16, BF16, F32),
+    (700, 2049, 20, BF16, F32), (600, 4097, 16, F32, BF16), (600, 4097, 9, BF16, F32), (900, 2048, 6, F32, F32),
+    (900, 2048, 7, F32, F32), (800, 2064, 1, BF16, F32), (1000, 256, 13, BF16, F32),
 ]
 
 
@@ -124,6 +126,17 @@ def test_int8_logits_extremes_and_unaligned_rows(vie):
     out = vie.Int8Head(view, scale.cuda())(h.cuda())
     same_bits(out, int8_reference(q, scale, h, F32))
     assert bool(torch.isnan(out[1:3]).all()) and not bool(torch.isnan(out[[0, 3, 4, 5]]).any())
+
+
+@pytest.mark.parametrize("V,d,B", [(600, 64, 3), (301, 272, 14), (500, 2048, 20), (130, 8192, 1), (257, 4096, 6), (900, 1024, 70)])
+def test_int8_rows_at_an_odd_address(vie, V, d, B):
+    """Rows of a multiple of 16 bytes that begin at an odd address."""
+    say("int8 odd address", V, d, B)
+    q, scale, h = int8_inputs(V, d, B, BF16, V + d)
+    buf = torch.zeros(V * d + 3, dtype=torch.int8).cuda()
+    view = buf[3:].view(V, d)
+    view.copy_(q)
+    same_bits(vie.Int8Head(view, scale.cuda())(h.cuda()), int8_reference(q, scale, h, F32))
 
 
 def test_int8_head_of_quantized_rows(vie):
@@ -567,6 +580,15 @@ def test_graph_replays_and_side_streams(vie, B, V):
     side.synchronize()
     for x, y in zip(got, want):
         assert torch.equal(x, y)
+
+
+def test_top_k_beyond_32_bits_is_no_limit(vie):
+    say("large top_k")
+    z, u = row_logits(3, 5000, F32, 8, False)
+    for big, plain in (((1 << 40) + 1, 0), (-(1 << 40) + 1, 0), ((1 << 31) - 1, 0)):
+        for x, y in zip(vie.sample_rows(z.cuda(), u.cuda(), top_k=big, top_p=0.9),
+                        vie.sample_rows(z.cuda(), u.cuda(), top_k=plain, top_p=0.9)):
+            assert torch.equal(x, y)
 
 
 def test_results_do_not_change_between_runs(vie):

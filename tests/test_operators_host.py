@@ -84,6 +84,45 @@ def test_distill_refuses_results_and_overlaps():
     assert _grad(stats=None) == vie.EINVAL
 
 
+def test_outputs_that_overlap_are_refused():
+    """Every output against every other argument, by its last byte and by its first."""
+    at = {name: (i + 1) << 20 for i, name in enumerate(("a", "b", "c", "d", "e", "f", "g", "h", "i", "j"))}
+    B, V, k = 3, 50, 5
+
+    def sample_prm(x):
+        return vie.SamplingParams(1.0, 1.0, 0.0, 0, x["g"], x["h"], x["i"], x["j"])
+
+    def lists(x):
+        return L.vie_sample(x["a"], x["b"], B, k, C.byref(sample_prm(x)), x["c"], x["d"], x["e"], x["f"], None)
+
+    def rows(x):
+        return L.vie_sample_rows(x["a"], vie.F32, V, V, B, C.byref(sample_prm(x)), x["c"], x["d"], x["e"], x["f"], P, BIG, None)
+
+    def loss(x):
+        return L.vie_distill(x["a"], vie.F32, B, V, V, x["b"], x["c"], k, 1.0, x["d"], x["e"], P, BIG, None)
+
+    def grad(x):
+        return L.vie_distill_grad(x["a"], vie.F32, B, V, V, x["b"], x["c"], k, 1.0, x["e"], x["f"], 1.0, x["d"], V, None)
+
+    def step(x):
+        return L.vie_distill_step(x["a"], vie.F32, B, V, V, x["b"], x["c"], k, 1.0, x["f"], 1.0, x["e"], x["d"], V, P, BIG, None)
+
+    four, lst, row = 4 * B, 4 * B * k, 4 * B * V
+    settings = {n: four for n in "ghij"}
+    for call, outs, sizes in ((lists, "def", {"a": lst, "b": lst, "c": four, "d": four, "e": four, "f": four, **settings}),
+                              (rows, "def", {"a": row, "c": four, "d": four, "e": four, "f": four, **settings}),
+                              (loss, "de", {"a": row, "b": lst, "c": lst, "d": four, "e": 2 * four}),
+                              (grad, "d", {"a": row, "b": lst, "c": lst, "d": row, "e": 2 * four, "f": four}),
+                              (step, "de", {"a": row, "b": lst, "c": lst, "d": row, "e": four, "f": four})):
+        for o in outs:
+            for other, n in sizes.items():
+                if other == o:
+                    continue
+                for where in (at[other] + n - 4, at[other] - sizes[o] + 4):
+                    assert call({**at, o: where}) == vie.EINVAL, (call.__name__, o, other)
+                    assert b"overlap" in L.vie_last_error()
+
+
 def test_workspace_queries():
     n = C.c_size_t()
     assert L.vie_int8_logits_workspace(1000, 64, 40, C.byref(n)) == vie.OK and n.value >= 40 * 64
