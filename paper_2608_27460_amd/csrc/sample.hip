@@ -106,7 +106,11 @@ struct Weights {
 };
 
 // Borders as integers: C >= p T iff C >= reach(p, T), C > u T iff C > below(u, T).
-__device__ __forceinline__ uint64_t reach(double p, uint64_t total) { return p > 0.0 ? (uint64_t)ceil(p * (double)total) : 0ull; }
+// (p T, rounded to fp64, may pass T for p within 2^-52 of 1: T is reached.)
+__device__ __forceinline__ uint64_t reach(double p, uint64_t total)
+{
+    return p > 0.0 ? min((uint64_t)ceil(p * (double)total), total) : 0ull;
+}
 __device__ __forceinline__ uint64_t below(float u, uint64_t total)
 {
     return u > 0.0f ? (uint64_t)fmin((double)u * (double)total, 9.2e18) : 0ull;

@@ -582,6 +582,23 @@ def test_graph_replays_and_side_streams(vie, B, V):
         assert torch.equal(x, y)
 
 
+def test_top_p_next_to_one(vie):
+    """The sums' integers have more bits than fp64: a product with top_p < 1 may round past the sum itself."""
+    say("top_p next to one")
+    p = float(np.nextafter(1.0, 0.0))
+    for B, V, dtype in ((64, 9000, F32), (64, 9000, BF16), (3, 300000, F32)):
+        z, u = row_logits(B, V, dtype, V, False)
+        zd, ud = z.cuda(), u.cuda()
+        near, one = vie.sample_rows(zd, ud, top_p=p), vie.sample_rows(zd, ud, top_p=1.0)
+        assert torch.equal(near[0], one[0]) and torch.equal(near[1], one[1])
+        assert bool((near[2] >= V // 2).all()) and bool((near[2] <= one[2]).all())
+    lg = torch.randn(500, 100, generator=torch.Generator().manual_seed(4)).sort(dim=1, descending=True)[0].contiguous()
+    ids = torch.arange(100, dtype=torch.int32).repeat(500, 1).contiguous()
+    u = torch.rand(500, generator=torch.Generator().manual_seed(5))
+    near, one = (vie.sample(ids.cuda(), lg.cuda(), u.cuda(), top_p=x) for x in (p, 1.0))
+    assert torch.equal(near[0], one[0]) and torch.equal(near[2], one[2])
+
+
 def test_top_k_beyond_32_bits_is_no_limit(vie):
     say("large top_k")
     z, u = row_logits(3, 5000, F32, 8, False)
