@@ -652,11 +652,12 @@ struct DrawLds {
     uint32_t base, last;
 };
 
-// P keys (a power of two, at most E kRowThreads) in descending order: thread
-// t holds keys t, t + kRowThreads, ..; pairs less than a wave apart meet by
+// P keys (a power of two, at most 2 kRowThreads) in descending order: thread
+// t holds keys t and t + kRowThreads; pairs less than a wave apart meet by
 // lane exchanges, the others in LDS.
-template <int E> __device__ void sort_row(uint64_t *key, int P)
+__device__ void sort_row(uint64_t *key, int P)
 {
+    constexpr int E = 2;
     const int tid = threadIdx.x;
     uint64_t v[E];
 #pragma unroll
@@ -669,11 +670,9 @@ template <int E> __device__ void sort_row(uint64_t *key, int P)
     for (int k = 2; k <= P; k <<= 1) {
         for (int j = k >> 1; j >= kLanes; j >>= 1) {
             if (j >= kRowThreads) {
-                if constexpr (E == 2) {
-                    const uint64_t a = v[0], b = v[1];
-                    keep(0, b, k, j);
-                    keep(1, a, k, j);
-                }
+                const uint64_t a = v[0], b = v[1];
+                keep(0, b, k, j);
+                keep(1, a, k, j);
                 continue;
             }
             __syncthreads();
@@ -700,6 +699,45 @@ template <int E> __device__ void sort_row(uint64_t *key, int P)
 #pragma unroll
     for (int e = 0; e < E; ++e)
         if (e * kRowThreads + tid < P) key[e * kRowThreads + tid] = v[e];
+    __syncthreads();
+}
+
+// The same for P keys of at most kRowThreads, different but for zeros, by P
+// threads: each wave puts its 64 in order, and a key's place is the number of
+// larger ones in all the waves' runs, by binary searches whose latencies
+// overlap, four runs at a time.  Zeros, which come last, are not put back.
+__device__ __forceinline__ void sort_distinct(uint64_t *key, int P)
+{
+    const int tid = threadIdx.x, lane = tid & (kLanes - 1);
+    uint64_t v = key[tid];
+#pragma unroll
+    for (int k = 2; k <= kLanes; k <<= 1)
+#pragma unroll
+        for (int j = k >> 1; j > 0; j >>= 1) {
+            const uint64_t o = lane_xor(v, j);
+            const bool larger = ((lane & k) == 0) == ((lane & j) == 0);
+            v = (v > o) == larger ? v : o;
+        }
+    if (P > kLanes) {
+        key[tid] = v;
+        __syncthreads();
+        int place = 0;
+        for (int run = 0; run < P; run += 4 * kLanes) {
+            int n[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int step = kLanes / 2; step >= 1; step >>= 1)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (key[(run + i * kLanes) % P + n[i] + step - 1] > v) n[i] += step;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)  // (and the 64th; runs past P count nothing)
+                place += run + i * kLanes < P ? n[i] + (key[(run + i * kLanes) % P + n[i]] > v) : 0;
+        }
+        __syncthreads();
+        if (v != 0) key[place] = v;
+    } else {
+        key[tid] = v;
+    }
     __syncthreads();
 }
 
@@ -1038,8 +1076,8 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     // and the sooner the fewer they are.
     const int waves = min(P / kLanes, kRowWaves);
     if (tid >= waves * kLanes) return;
-    if (P <= kRowThreads) sort_row<1>(s.d.key, P);
-    else sort_row<2>(s.d.key, P);
+    if (P <= kRowThreads) sort_distinct(s.d.key, P);
+    else sort_row(s.d.key, P);
     uint64_t own[kCollect / kRowThreads];
     int64_t rank[kCollect / kRowThreads];
     uint64_t base = 0;
