@@ -268,8 +268,8 @@ template <int NT> __global__ __launch_bounds__(NT) void sample_list_kernel(Sampl
 // of 262144 normal logits meets some 400 candidates of its bin.
 //
 // Latency bounds it: each kernel is a chain of loads, sums and searches that
-// wait for one another, from 1 to 4 us each.  One row of 262144 fp32: 4.6, 7.3
-// and 17.8 us; 64 rows of 151936 bf16: 7.4, 14.1 and 23.7, where reading them
+// wait for one another, from 1 to 3 us each.  One row of 262144 fp32: 3.8, 7.6
+// and 16.2 us; 64 rows of 151936 bf16: 7.2, 14.1 and 23.0, where reading them
 // takes 4.
 //
 // Rows whose border bins hold more than kCollect candidates take one of two
@@ -705,7 +705,8 @@ __device__ void sort_row(uint64_t *key, int P)
 // The same for P keys of at most kRowThreads, different but for zeros, by P
 // threads: each wave puts its 64 in order, and a key's place is the number of
 // larger ones in all the waves' runs, by binary searches whose latencies
-// overlap, four runs at a time.  Zeros, which come last, are not put back.
+// overlap, four runs at a time (439 keys: 2 us less than in sort_row's way).
+// Zeros, which come last, are not put back.
 __device__ __forceinline__ void sort_distinct(uint64_t *key, int P)
 {
     const int tid = threadIdx.x, lane = tid & (kLanes - 1);
@@ -1168,9 +1169,10 @@ vie_status launch_sample_lists(const SampleLaunch &a, hipStream_t s)
 namespace {
 template <bool BF16> vie_status rows_launch(const SampleLaunch &a, hipStream_t s)
 {
-    // Parts of a row: one workgroup a CU, of 4096 candidates at least (one row
-    // of 262144 fp32 in parts of 2048: 34 us, of 4096 and 8192: 30, of 16384:
-    // 34; of 50000: 24, 25, 26 and 29).
+    // Parts of a row: one workgroup a CU (64 rows of 151936 bf16: 46 us so, 69
+    // with two, 57 with half of one), of 4096 candidates at least (one row of
+    // 262144 fp32 in parts of 2048: 30.5 us, of 4096: 27.1, of 8192: 27.7, of
+    // 16384: 31.2; of 50000: 22.6, 23.4, 24.5 and 28.1).
     const int64_t want = std::min<int64_t>((a.n + 4095) / 4096, 256 / a.B);
     const int S = (int)std::max<int64_t>(1, std::min<int64_t>(want, kMaxParts));
     const int64_t len = ((a.n + S - 1) / S + 63) / 64 * 64;
