@@ -556,9 +556,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
             int64_t v0;
             int b0;
             place(pt, v0, b0);
-            if (v0 + tiles.rows >= V) {
+            if ((v0 + tiles.rows) * pitch + 16 > V * pitch) {
                 // Pieces that would end past the matrix were loaded before its
-                // end: their bytes move to where they belong.
+                // end: their bytes move to where they belong.  (Rows of a few
+                // bytes have such pieces before the last tile, too.)
 #pragma unroll
                 for (int i = 0; i < WL; ++i) {
                     const int64_t v = min<int64_t>(v0 + wave * (kTileRows / kWaves) + LR * i + lrow, V - 1);

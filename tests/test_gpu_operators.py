@@ -89,6 +89,9 @@ INT8_CASES = [
     (4099, 65, 40, F32, BF16), (3001, 1001, 200, BF16, F32), (1500, 8191, 20, F32, F32), (5000, 1000, 16, BF16, BF16),
     (777, 2040, 16, F32, F32), (9000, 4100, 3, BF16, BF16), (70000, 33, 2, F32, BF16), (3000, 4096, 8, F32, F32),
     (131073, 16, 1, BF16, F32), (500, 8192, 16, BF16, F32),
+    # rows of a few bytes: the matrix's last 16 bytes are rows of two tiles
+    (2226, 2, 3, BF16, BF16), (2305, 1, 5, F32, F32), (4097, 7, 2, BF16, F32), (70001, 3, 16, F32, BF16), (2066, 15, 4, BF16, F32),
+    (9, 2, 3, F32, F32), (16, 1, 2, F32, F32), (17, 1, 2, F32, F32), (2570, 5, 1, F32, F32),
     (700, 2049, 20, BF16, F32), (600, 4097, 16, F32, BF16), (600, 4097, 9, BF16, F32), (900, 2048, 6, F32, F32),
     (900, 2048, 7, F32, F32), (800, 2064, 1, BF16, F32), (1000, 256, 13, BF16, F32),
 ]
