@@ -272,6 +272,9 @@ template <int NT> __global__ __launch_bounds__(NT) void sample_list_kernel(Sampl
 // and 16.2 us; 64 rows of 151936 bf16: 7.2, 14.1 and 23.0, where reading them
 // takes 4.
 //
+// Short rows, or many, take a workgroup each, which does all of this in one
+// kernel (rows_one_kernel).
+//
 // Rows whose border bins hold more than kCollect candidates take one of two
 // other ways.  Where each of these bins holds one value (logits that were
 // rounded to bf16 somewhere, constant rows), its candidates weigh the same,
@@ -509,6 +512,17 @@ template <bool BF16> __device__ __forceinline__ Row<BF16> row_of(const SampleLau
     return {static_cast<const typename Elem<BF16>::T *>(a.logits) + (int64_t)b * a.ld, a.n};
 }
 
+// The best key among n logits from i0 on, in every thread (0: no candidate).
+template <bool BF16> __device__ __forceinline__ uint64_t best_of(const Row<BF16> &row, int64_t i0, int64_t n, uint64_t *tmp)
+{
+    uint64_t best = 0;
+    row.each(i0, n, [&](float l, int32_t id) {
+        const uint64_t key = make_key(l, id);
+        best = key > best ? key : best;
+    });
+    return block_reduce<kRowThreads>(best, tmp, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
+}
+
 template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_best_kernel(SampleLaunch a, Parts parts)
 {
     __shared__ uint64_t tmp[kRowWaves];
@@ -517,13 +531,8 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_best_ke
     for (int i = c * kRowThreads + threadIdx.x; i < kBins; i += S * kRowThreads) ws.sum[i] = 0, ws.count[i] = 0;
     if (c == 0 && threadIdx.x == 0) ws.pass = ws.collected = ws.done = 0;
     const Row<BF16> row = row_of<BF16>(a, b);
-    uint64_t best = 0;
     const int64_t i0 = c * parts.len;
-    row.each(i0, min(parts.len, a.n - i0), [&](float l, int32_t id) {
-        const uint64_t key = make_key(l, id);
-        best = key > best ? key : best;
-    });
-    best = block_reduce<kRowThreads>(best, tmp, [](uint64_t x, uint64_t y) { return x > y ? x : y; });
+    const uint64_t best = best_of(row, i0, min(parts.len, a.n - i0), tmp);
     if (threadIdx.x == 0) ws.best[c] = best;
 }
 
@@ -534,90 +543,124 @@ __device__ __forceinline__ uint64_t best_key(const RowSpace &ws, int S)
     return wave_max(k);
 }
 
-// Whether a row has more to draw than its best candidate, or none.
+// Whether a row has more to draw than its best candidate, or none, and the
+// result where not.
 __device__ __forceinline__ bool open(uint64_t best, Settings st) { return best != 0 && st.t > 0.0; }
+__device__ __forceinline__ Result closed(uint64_t best)
+{
+    return best == 0 ? Result{-1, 0.0f, 0} : Result{key_id(best), 1.0f, 1};
+}
+
+// A row's bins in LDS: counts, and sums (bf16: of the bins of more than one
+// value, the others' follow from their counts).
+template <bool BF16> struct BinLds {
+    static constexpr int kSums = BF16 ? 2 : kBins;
+    uint64_t sum[kSums];
+    uint32_t count[kBins];
+    double exp[64];
+    uint32_t pass;
+    uint64_t tmp[kRowWaves];
+
+    __device__ __forceinline__ void clear()
+    {
+        const int tid = threadIdx.x;
+        for (int i = tid; i < kSums / 2; i += kRowThreads) reinterpret_cast<ulonglong2 *>(sum)[i] = {0, 0};
+        for (int i = tid; i < kBins / 4; i += kRowThreads) reinterpret_cast<uint4 *>(count)[i] = {0, 0, 0, 0};
+        if (tid < 64) exp[tid] = kExp2.v[tid];
+        if (tid == 0) pass = 0;
+    }
+    // n logits from i0 on; returns how many of this thread's pass min-p
+    // (bf16: of those in bins of more than one value)
+    __device__ __forceinline__ uint32_t add(const Row<BF16> &row, int64_t i0, int64_t n, const Weights &weights,
+                                            const Bins<BF16> &bin_map, double least)
+    {
+        uint32_t passed = 0;
+        row.groups(i0, n, [&](const float *l, int32_t, auto number) {
+            constexpr int N = decltype(number)::value;
+            int bin[N];
+            uint64_t units[N];
+            if constexpr (BF16) {
+#pragma unroll
+                for (int e = 0; e < N; ++e) bin[e] = bin_map.of(l[e]);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    if (!candidate(l[e])) continue;
+                    atomicAdd(&count[bin[e]], 1u);
+                    if (!bin_map.one(bin[e])) {
+                        const double w = weights.real(l[e]);
+                        passed += w >= least;
+                        atomicAdd((unsigned long long *)&sum[bin[e] != bin_map.top], (unsigned long long)Weights::round(w));
+                    }
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < N; ++e) {  // (without branches, so that their latencies overlap)
+                    bin[e] = bin_map.of(l[e]);
+                    const double w = weights.real(l[e]);
+                    passed += candidate(l[e]) & (w >= least);
+                    units[e] = Weights::round(w);
+                }
+#pragma unroll
+                for (int e = 0; e < N; ++e)
+                    if (candidate(l[e])) {
+                        atomicAdd(&count[bin[e]], 1u);
+                        atomicAdd((unsigned long long *)&sum[bin[e]], (unsigned long long)units[e]);
+                    }
+            }
+        });
+        return passed;
+    }
+    // the weight of the n > 0 candidates of bin i, and those of them that
+    // pass min-p and were not counted yet
+    __device__ __forceinline__ uint64_t weight(int i, uint32_t n, const Weights &weights, const Bins<BF16> &bin_map, double least,
+                                               uint32_t &passed) const
+    {
+        if constexpr (BF16) {
+            if (!bin_map.one(i)) return sum[i != bin_map.top];
+            const double w = weights.real(bin_map.value(i));
+            if (w >= least) passed += n;
+            return Weights::round(w) * n;
+        } else {
+            return sum[i];
+        }
+    }
+    // all threads' numbers into `pass` (complete after the next barrier)
+    __device__ __forceinline__ void add_pass(uint32_t passed)
+    {
+        passed = wave_sum(passed);
+        if ((threadIdx.x & (kLanes - 1)) == 0 && passed) atomicAdd(&pass, passed);
+    }
+};
 
 template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_bins_kernel(SampleLaunch a, Parts parts)
 {
     extern __shared__ __align__(16) char smem[];
-    constexpr int kSums = BF16 ? 2 : kBins;  // (bf16: of the bins of more than one value)
-    uint64_t *s_sum = reinterpret_cast<uint64_t *>(smem);
-    uint32_t *s_count = reinterpret_cast<uint32_t *>(s_sum + kSums);
-    __shared__ double s_exp[64];
-    __shared__ uint32_t s_pass;
+    BinLds<BF16> &s = *reinterpret_cast<BinLds<BF16> *>(smem);
     const int b = parts.b0 + blockIdx.y, tid = threadIdx.x;
     RowSpace &ws = parts.ws[blockIdx.y];
     const Settings st = settings(a.prm, b);
     const Row<BF16> row = row_of<BF16>(a, b);
-    for (int i = tid; i < kSums / 2; i += kRowThreads) reinterpret_cast<ulonglong2 *>(s_sum)[i] = {0, 0};
-    for (int i = tid; i < kBins / 4; i += kRowThreads) reinterpret_cast<uint4 *>(s_count)[i] = {0, 0, 0, 0};
-    if (tid < 64) s_exp[tid] = kExp2.v[tid];
-    if (tid == 0) s_pass = 0;
+    s.clear();
     const uint64_t best = best_key(ws, gridDim.x);
     if (!open(best, st)) return;
-    const Weights weights(key_logit(best), st.t, fixed_shift(a.n), s_exp);
+    const Weights weights(key_logit(best), st.t, fixed_shift(a.n), s.exp);
     const double least = weights.least(st.m);
     const Bins<BF16> bin_map(best);
     __syncthreads();
-    uint32_t pass = 0;
     const int64_t i0 = blockIdx.x * parts.len;
-    row.groups(i0, min(parts.len, a.n - i0), [&](const float *l, int32_t, auto count) {
-        constexpr int N = decltype(count)::value;
-        int bin[N];
-        uint64_t units[N];
-        if constexpr (BF16) {
-#pragma unroll
-            for (int e = 0; e < N; ++e) bin[e] = bin_map.of(l[e]);
-#pragma unroll
-            for (int e = 0; e < N; ++e) {
-                if (!candidate(l[e])) continue;
-                atomicAdd(&s_count[bin[e]], 1u);
-                if (!bin_map.one(bin[e])) {
-                    const double w = weights.real(l[e]);
-                    pass += w >= least;
-                    atomicAdd((unsigned long long *)&s_sum[bin[e] != bin_map.top], (unsigned long long)Weights::round(w));
-                }
-            }
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) {  // (without branches, so that their latencies overlap)
-                bin[e] = bin_map.of(l[e]);
-                const double w = weights.real(l[e]);
-                pass += candidate(l[e]) & (w >= least);
-                units[e] = Weights::round(w);
-            }
-#pragma unroll
-            for (int e = 0; e < N; ++e)
-                if (candidate(l[e])) {
-                    atomicAdd(&s_count[bin[e]], 1u);
-                    atomicAdd((unsigned long long *)&s_sum[bin[e]], (unsigned long long)units[e]);
-                }
-        }
-    });
+    uint32_t passed = s.add(row, i0, min(parts.len, a.n - i0), weights, bin_map, least);
     __syncthreads();
 #pragma unroll 1
     for (int i = tid; i < kBins; i += kRowThreads) {
-        const uint32_t n = s_count[i];
+        const uint32_t n = s.count[i];
         if (n == 0) continue;
-        uint64_t sum;
-        if constexpr (BF16) {
-            if (bin_map.one(i)) {
-                const double w = weights.real(bin_map.value(i));
-                if (w >= least) pass += n;
-                sum = Weights::round(w) * n;
-            } else {
-                sum = s_sum[i != bin_map.top];
-            }
-        } else {
-            sum = s_sum[i];
-        }
+        const uint64_t sum = s.weight(i, n, weights, bin_map, least, passed);
         atomicAdd(&ws.count[i], n);
         atomicAdd((unsigned long long *)&ws.sum[i], (unsigned long long)sum);
     }
-    pass = wave_sum(pass);
-    if ((tid & (kLanes - 1)) == 0 && pass) atomicAdd(&s_pass, pass);
+    s.add_pass(passed);
     __syncthreads();
-    if (tid == 0) atomicAdd(&ws.pass, s_pass);
+    if (tid == 0) atomicAdd(&ws.pass, s.pass);
 }
 
 // The bin that a border falls into, with what lies before it and up to its end.
@@ -870,15 +913,21 @@ __device__ __noinline__ int draw_ties(const Row<BF16> &row, const Weights &weigh
     return 1;
 }
 
+// The draw by the row's workgroups, from the bins, kBinsPer a thread, and
+// the number of candidates that pass min-p.
+template <bool BF16>
+__device__ __forceinline__ void draw_row(const SampleLaunch &a, int b, const Row<BF16> &row, const Settings &st, float u,
+                                         const Weights &weights, const Bins<BF16> &bin_map, const uint32_t (&cnt)[kBinsPer],
+                                         const uint64_t (&sum)[kBinsPer], uint32_t pass, int64_t len, RowSpace &ws, DrawLds &s);
+
 template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_kernel(SampleLaunch a, Parts parts)
 {
     extern __shared__ __align__(16) char smem[];
-    DrawLds &s = *reinterpret_cast<DrawLds *>(smem);
-    const int b = parts.b0 + blockIdx.y, tid = threadIdx.x, S = gridDim.x;
+    const int b = parts.b0 + blockIdx.y, tid = threadIdx.x;
     RowSpace &ws = parts.ws[blockIdx.y];
-    // the bins, kBinsPer a thread (read while the row's settings are)
-    uint32_t cnt[kBinsPer], c = 0;
-    uint64_t sum[kBinsPer], x = 0;
+    // the bins (read while the row's settings are)
+    uint32_t cnt[kBinsPer];
+    uint64_t sum[kBinsPer];
     static_assert(kBinsPer % 4 == 0, "read 16 bytes at a time");
 #pragma unroll
     for (int i = 0; i < kBinsPer; i += 4) {
@@ -894,13 +943,58 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     const Settings st = settings(a.prm, b);
     const float u = a.u[b];
     const Row<BF16> row = row_of<BF16>(a, b);
-    const uint64_t best = best_key(ws, S);
+    const uint64_t best = best_key(ws, gridDim.x);
     if (!open(best, st)) {
-        if (blockIdx.x == 0 && tid == 0) put(a, b, best == 0 ? Result{-1, 0.0f, 0} : Result{key_id(best), 1.0f, 1});
+        if (blockIdx.x == 0 && tid == 0) put(a, b, closed(best));
         return;
     }
-    const Weights weights(key_logit(best), st.t, fixed_shift(a.n));
+    draw_row<BF16>(a, b, row, st, u, Weights(key_logit(best), st.t, fixed_shift(a.n)), Bins<BF16>(best), cnt, sum, pass,
+                   parts.len, ws, *reinterpret_cast<DrawLds *>(smem));
+}
+
+// The three kernels in one, for rows of one part: a workgroup's row, whose
+// bins stay in LDS.
+template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_one_kernel(SampleLaunch a, Parts parts)
+{
+    extern __shared__ __align__(16) char smem[];
+    BinLds<BF16> &s = *reinterpret_cast<BinLds<BF16> *>(smem + sizeof(DrawLds));
+    const int b = parts.b0 + blockIdx.y, tid = threadIdx.x;
+    RowSpace &ws = parts.ws[blockIdx.y];
+    const Settings st = settings(a.prm, b);
+    const float u = a.u[b];
+    const Row<BF16> row = row_of<BF16>(a, b);
+    s.clear();
+    if (tid == 0) ws.done = 0;
+    const uint64_t best = best_of(row, 0, a.n, s.tmp);  // (the workgroup waits in here)
+    if (!open(best, st)) {
+        if (tid == 0) put(a, b, closed(best));
+        return;
+    }
+    const Weights weights(key_logit(best), st.t, fixed_shift(a.n), s.exp);
+    const double least = weights.least(st.m);
     const Bins<BF16> bin_map(best);
+    uint32_t passed = s.add(row, 0, a.n, weights, bin_map, least);
+    __syncthreads();
+    uint32_t cnt[kBinsPer];
+    uint64_t sum[kBinsPer];
+#pragma unroll
+    for (int i = 0; i < kBinsPer; ++i) {
+        cnt[i] = s.count[tid * kBinsPer + i];
+        sum[i] = cnt[i] ? s.weight(tid * kBinsPer + i, cnt[i], weights, bin_map, least, passed) : 0ull;
+    }
+    s.add_pass(passed);
+    __syncthreads();
+    draw_row<BF16>(a, b, row, st, u, weights, bin_map, cnt, sum, s.pass, parts.len, ws, *reinterpret_cast<DrawLds *>(smem));
+}
+
+template <bool BF16>
+__device__ __forceinline__ void draw_row(const SampleLaunch &a, int b, const Row<BF16> &row, const Settings &st, float u,
+                                         const Weights &weights, const Bins<BF16> &bin_map, const uint32_t (&cnt)[kBinsPer],
+                                         const uint64_t (&sum)[kBinsPer], uint32_t pass, int64_t len, RowSpace &ws, DrawLds &s)
+{
+    const int tid = threadIdx.x, S = gridDim.x;
+    uint32_t c = 0;
+    uint64_t x = 0;
 #pragma unroll
     for (int i = 0; i < kBinsPer; ++i) {
         c += cnt[i];
@@ -1022,7 +1116,7 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
         int how = 2;
         if (nslot <= kTies)
             how = draw_ties(row, weights, bin_map, st, u, Borders{K, most, exact_k, exact_end, sum_k, sum_end}, (int)nslot,
-                            parts.len, ws, s, r);
+                            len, ws, s, r);
         else if (blockIdx.x != 0)
             return;
         if (how == 0) return;
@@ -1032,8 +1126,8 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
     }
 
     // collect: this part's in LDS, then all parts' in the workspace
-    const int64_t i0 = blockIdx.x * parts.len;
-    row.groups(i0, min(parts.len, a.n - i0), [&](const float *l, int32_t id, auto count) {
+    const int64_t i0 = blockIdx.x * len;
+    row.groups(i0, min(len, a.n - i0), [&](const float *l, int32_t id, auto count) {
         constexpr int N = decltype(count)::value;
         uint32_t hit = 0;
 #pragma unroll
@@ -1176,15 +1270,28 @@ template <bool BF16> vie_status rows_launch(const SampleLaunch &a, hipStream_t s
     const int64_t want = std::min<int64_t>((a.n + 4095) / 4096, 256 / a.B);
     const int S = (int)std::max<int64_t>(1, std::min<int64_t>(want, kMaxParts));
     const int64_t len = ((a.n + S - 1) / S + 63) / 64 * 64;
-    constexpr int kBinsLds = kBins * 4 + (BF16 ? 2 : kBins) * 8;
+    constexpr int kBinsLds = sizeof(BinLds<BF16>), kOneLds = sizeof(DrawLds) + sizeof(BinLds<BF16>);
+    // A workgroup a row in one kernel takes some 13 us and 5 for every 10000
+    // logits of up to 256 rows, three kernels 21 and more with the work of a
+    // CU.  In us, fp32, three kernels and one: 1 row of 4096 21.6 and 15.1, of
+    // 16384 23.4 and 21.2, of 32000 23.4 and 28.9; 64 rows of 32000 37 and 31,
+    // of 50257 40 and 40, of 128256 53 and 81; 128 of 128256 71 and 80; 200 of
+    // 128256 99 and 83; 1000 of 4096 103 and 58.
+    const bool one = S == 1 || a.n <= 16384 + 512 * (int64_t)a.B;
     hipError_t e = hipFuncSetAttribute((const void *)rows_draw_kernel<BF16>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                        (int)sizeof(DrawLds));
     if (e == hipSuccess)
         e = hipFuncSetAttribute((const void *)rows_bins_kernel<BF16>, hipFuncAttributeMaxDynamicSharedMemorySize, kBinsLds);
+    if (e == hipSuccess)
+        e = hipFuncSetAttribute((const void *)rows_one_kernel<BF16>, hipFuncAttributeMaxDynamicSharedMemorySize, kOneLds);
     if (e != hipSuccess) return fail(VIE_EHIP, "row sampling: %s", hipGetErrorString(e));
     for (int b0 = 0; b0 < a.B; b0 += kMaxRows) {
         const Parts parts{len, b0, static_cast<RowSpace *>(a.ws)};
         const dim3 grid((unsigned)((a.n + len - 1) / len), (unsigned)std::min(kMaxRows, a.B - b0));
+        if (one) {
+            rows_one_kernel<BF16><<<dim3(1, grid.y), kRowThreads, kOneLds, s>>>(a, Parts{a.n, b0, static_cast<RowSpace *>(a.ws)});
+            continue;
+        }
         rows_best_kernel<BF16><<<grid, kRowThreads, 0, s>>>(a, parts);
         rows_bins_kernel<BF16><<<grid, kRowThreads, kBinsLds, s>>>(a, parts);
         rows_draw_kernel<BF16><<<grid, kRowThreads, sizeof(DrawLds), s>>>(a, parts);

@@ -265,7 +265,8 @@ def row_logits(B, V, dtype, seed, masked):
 
 ROW_CASES = [(1, 1, F32, False), (2, 2, BF16, True), (3, 7, BF16, False), (4, 1000, F32, True), (9, 4099, BF16, True),
              (1, 50257, F32, False), (5, 50257, BF16, True), (1, 262144, F32, False), (2, 262147, BF16, False),
-             (70, 3001, F32, True), (300, 513, BF16, True), (1100, 129, F32, True), (3, 151936, BF16, True)]
+             (70, 3001, F32, True), (300, 513, BF16, True), (1100, 129, F32, True), (3, 151936, BF16, True),
+             (20, 30011, F32, True), (30, 30011, BF16, False), (140, 20011, F32, False)]
 
 
 @pytest.mark.parametrize("B,V,dtype,masked", ROW_CASES)
