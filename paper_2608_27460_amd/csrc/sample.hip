@@ -1112,15 +1112,20 @@ __device__ __forceinline__ void draw_row(const SampleLaunch &a, int b, const Row
     if (tid == 0) s.base = 0;
     __syncthreads();
     if (M > kCollect || nslot > kMaxSlots) {  // (the same in every workgroup of the row)
+        // (copies, so that only these have addresses, and the others registers)
+        const Row<BF16> row2 = row;
+        const Weights weights2 = weights;
+        const Bins<BF16> map2 = bin_map;
+        const Settings st2 = st;
         Result r;
         int how = 2;
         if (nslot <= kTies)
-            how = draw_ties(row, weights, bin_map, st, u, Borders{K, most, exact_k, exact_end, sum_k, sum_end}, (int)nslot,
+            how = draw_ties(row2, weights2, map2, st2, u, Borders{K, most, exact_k, exact_end, sum_k, sum_end}, (int)nslot,
                             len, ws, s, r);
         else if (blockIdx.x != 0)
             return;
         if (how == 0) return;
-        if (how == 2) r = draw_by_digits(row, weights, st, u, live, total, pass, s.digits);
+        if (how == 2) r = draw_by_digits(row2, weights2, st2, u, live, total, pass, s.digits);
         if (tid == 0) put(a, b, r);
         return;
     }
