@@ -415,7 +415,7 @@ __device__ __forceinline__ void block_scan(uint32_t &c, uint64_t &s, uint32_t &c
 // by a histogram of the candidates that share the digits before.  If there is
 // none (`sum` above the total), the last candidate.
 template <bool BF16>
-__device__ __noinline__ Place find(const Row<BF16> &row, const Weights &weights, bool by_rank, int64_t rank, uint64_t sum, DigitLds &s)
+__device__ __forceinline__ Place find(const Row<BF16> &row, const Weights &weights, bool by_rank, int64_t rank, uint64_t sum, DigitLds &s)
 {
     const int tid = threadIdx.x;
     uint64_t prefix = 0, before_sum = 0;
@@ -488,7 +488,7 @@ __device__ __forceinline__ Result drawn(const Weights &weights, uint64_t key, ui
 // The borders one after the other, over the whole row: `live` candidates,
 // `total` units of weight, `pass` candidates within min-p.
 template <bool BF16>
-__device__ __noinline__ Result draw_by_digits(const Row<BF16> &row, const Weights &weights, Settings st, float u, uint32_t live, uint64_t total, uint32_t pass,
+__device__ __forceinline__ Result draw_by_digits(const Row<BF16> &row, const Weights &weights, Settings st, float u, uint32_t live, uint64_t total, uint32_t pass,
                                  DigitLds &s)
 {
     Place end{0, total, (int64_t)live};  // the last candidate kept
@@ -801,7 +801,7 @@ struct Borders {
 constexpr int kTies = 8;
 static_assert(kMaxParts * kTies * 2 <= kCollect, "the parts' counts take the place of the collected keys");
 template <bool BF16>
-__device__ __noinline__ int draw_ties(const Row<BF16> &row, const Weights &weights, const Bins<BF16> &bin_map,
+__device__ __forceinline__ int draw_ties(const Row<BF16> &row, const Weights &weights, const Bins<BF16> &bin_map,
                                       const Settings &st, float u, const Borders &known, int nslot, int64_t len,
                                       RowSpace &ws, DrawLds &s, Result &out)
 {
@@ -914,7 +914,9 @@ __device__ __noinline__ int draw_ties(const Row<BF16> &row, const Weights &weigh
 }
 
 // The draw by the row's workgroups, from the bins, kBinsPer a thread, and
-// the number of candidates that pass min-p.
+// the number of candidates that pass min-p.  (The rare paths are inlined: as
+// functions they would take a stack, which costs the kernel 1 us when they
+// are not called.)
 template <bool BF16>
 __device__ __forceinline__ void draw_row(const SampleLaunch &a, int b, const Row<BF16> &row, const Settings &st, float u,
                                          const Weights &weights, const Bins<BF16> &bin_map, const uint32_t (&cnt)[kBinsPer],
@@ -1112,20 +1114,15 @@ __device__ __forceinline__ void draw_row(const SampleLaunch &a, int b, const Row
     if (tid == 0) s.base = 0;
     __syncthreads();
     if (M > kCollect || nslot > kMaxSlots) {  // (the same in every workgroup of the row)
-        // (copies, so that only these have addresses, and the others registers)
-        const Row<BF16> row2 = row;
-        const Weights weights2 = weights;
-        const Bins<BF16> map2 = bin_map;
-        const Settings st2 = st;
         Result r;
         int how = 2;
         if (nslot <= kTies)
-            how = draw_ties(row2, weights2, map2, st2, u, Borders{K, most, exact_k, exact_end, sum_k, sum_end}, (int)nslot,
+            how = draw_ties(row, weights, bin_map, st, u, Borders{K, most, exact_k, exact_end, sum_k, sum_end}, (int)nslot,
                             len, ws, s, r);
         else if (blockIdx.x != 0)
             return;
         if (how == 0) return;
-        if (how == 2) r = draw_by_digits(row2, weights2, st2, u, live, total, pass, s.digits);
+        if (how == 2) r = draw_by_digits(row, weights, st, u, live, total, pass, s.digits);
         if (tid == 0) put(a, b, r);
         return;
     }
