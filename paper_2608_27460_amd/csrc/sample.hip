@@ -268,8 +268,8 @@ template <int NT> __global__ __launch_bounds__(NT) void sample_list_kernel(Sampl
 // of 262144 normal logits meets some 400 candidates of its bin.
 //
 // Latency bounds it: each kernel is a chain of loads, sums and searches that
-// wait for one another, from 1 to 3 us each.  One row of 262144 fp32: 3.8, 7.6
-// and 16.2 us; 64 rows of 151936 bf16: 7.2, 14.1 and 23.0, where reading them
+// wait for one another, from 1 to 3 us each.  One row of 262144 fp32: 3.8, 7.5
+// and 15.4 us; 64 rows of 151936 bf16: 7.2, 14.2 and 21.3, where reading them
 // takes 4.
 //
 // Short rows, or many, take a workgroup each, which does all of this in one
