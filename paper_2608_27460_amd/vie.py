@@ -433,8 +433,14 @@ def _workspace(nbytes: int, device):
     return t, t.data_ptr()
 
 
+def _overwritten(out) -> None:
+    """Lets autograd see that a caller's tensor was written to: a backward pass that saved it then refuses to run."""
+    _torch().autograd.graph.increment_version(out)
+
+
 class Int8Head:
-    """Full-vocabulary logits from the int8 rows and scales of quantize_rows."""
+    """Full-vocabulary logits from the int8 rows and scales of quantize_rows.
+    The quantized products have no derivative: autograd does not record them."""
 
     def __init__(self, q, scale):
         torch = _torch()
@@ -455,7 +461,8 @@ class Int8Head:
         if h.device != self.q.device:
             raise ValueError("h is on %s, not on %s" % (h.device, self.q.device))
         B, hd = h.shape[0], _dtype_of_tensor(h)
-        if out is None:
+        given = out is not None
+        if not given:
             out = torch.empty((B, V), dtype=dtype or torch.float32, device=h.device)
         elif dtype is not None and out.dtype != dtype:
             raise TypeError("out is %s, not %s" % (out.dtype, dtype))
@@ -468,6 +475,8 @@ class Int8Head:
             ws, wp = _workspace(n, h.device)
             _check(lib.vie_int8_logits(self.q.data_ptr(), self.scale.data_ptr(), V, d, hp, hd, B, op, od, ld, wp, n,
                                        _raw_stream(h.device)))
+        if given:
+            _overwritten(out)
         return out
 
 
@@ -551,10 +560,41 @@ def _grad_of(logits, gloss, out):
     return out, gp, ld, None if gloss is None else _values(gloss, "gloss", torch.float32, (N,), logits.device)
 
 
-def distill(logits, ids, teacher, tau: float = 1.0):
-    """(loss fp32 [N], stats fp32 [N, 2]) of the student's logits [N, V] (fp32
-    or bf16) against a teacher's lists ids int32 [N, k], teacher fp32 [N, k] of
-    logits at the temperature tau (vie_distill); stats goes to distill_grad."""
+@functools.lru_cache(maxsize=None)
+def _recorded():
+    """Distillation as autograd records it: (the losses of distill, the loss that distill_step returns)."""
+    torch = _torch()
+
+    class Losses(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, logits, ids, teacher, tau):
+            loss, stats = _losses(logits, ids, teacher, tau)
+            ctx.save_for_backward(logits, ids, teacher, stats)
+            ctx.tau = tau
+            ctx.mark_non_differentiable(stats)
+            return loss, stats
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, gloss, _):
+            logits, ids, teacher, stats = ctx.saved_tensors
+            return distill_grad(logits, ids, teacher, stats, ctx.tau, gloss=gloss.contiguous()), None, None, None
+
+    class Given(torch.autograd.Function):
+        # (`anchor`: a leaf of its own, so that a loss kept for the log does not keep the logits' graph)
+        @staticmethod
+        def forward(ctx, anchor, loss):
+            return loss.view_as(loss)
+
+        @staticmethod
+        def backward(ctx, gloss):
+            raise RuntimeError("distill_step gives the gradient of its loss as the second result; "
+                               "detach the loss, or take it from distill")
+
+    return Losses, lambda loss: Given.apply(torch.empty(0, requires_grad=True), loss)
+
+
+def _losses(logits, ids, teacher, tau):
     torch = _torch()
     (lp, dt, N, V, ld), ip, tp, k = _distill_inputs(logits, ids, teacher)
     n = _workspace_bytes("vie_distill_workspace", V, N)
@@ -567,28 +607,53 @@ def distill(logits, ids, teacher, tau: float = 1.0):
     return loss, stats
 
 
+def distill(logits, ids, teacher, tau: float = 1.0):
+    """(loss fp32 [N], stats fp32 [N, 2]) of the student's logits [N, V] (fp32
+    or bf16) against a teacher's lists ids int32 [N, k], teacher fp32 [N, k] of
+    logits at the temperature tau (vie_distill); stats goes to distill_grad.
+    Where the logits require a gradient, autograd's backward pass takes the
+    losses' from distill_grad (once differentiable); the teacher gets none, and
+    is refused if it requires one.  (Captured into a graph, as any backward
+    pass of torch: while no eager graph of the same leaves is alive.)"""
+    torch = _torch()
+    if torch.is_grad_enabled():
+        if teacher.requires_grad:
+            raise ValueError("teacher requires a gradient, which distillation does not compute: detach it")
+        if logits.requires_grad:
+            return _recorded()[0].apply(logits, ids, teacher, tau)
+    return _losses(logits, ids, teacher, tau)
+
+
 def distill_grad(logits, ids, teacher, stats, tau: float = 1.0, gloss=None, weight: float = 1.0, out=None):
     """Gradient of sum_n weight gloss[n] loss[n] (gloss fp32 [N], ones if None)
-    in the logits, in their type; out may be logits itself (vie_distill_grad)."""
-    torch = _torch()
+    in the logits, in their type; out may be logits itself (vie_distill_grad).
+    Autograd does not record it."""
     (lp, dt, N, V, ld), ip, tp, k = _distill_inputs(logits, ids, teacher)
-    sp = _values(stats, "stats", torch.float32, (N, 2), logits.device)
+    sp = _values(stats, "stats", _torch().float32, (N, 2), logits.device)
     with _on(logits.device):
-        out, gp, gld, glp = _grad_of(logits, gloss, out)
+        grad, gp, gld, glp = _grad_of(logits, gloss, out)
         _check(lib.vie_distill_grad(lp, dt, N, V, ld, ip, tp, k, tau, sp, glp, weight, gp, gld,
                                     _raw_stream(logits.device)))
-    return out
+    if out is not None:
+        _overwritten(out)
+    return grad
 
 
 def distill_step(logits, ids, teacher, tau: float = 1.0, gloss=None, weight: float = 1.0, out=None):
-    """(loss, gradient): distill and distill_grad at once (vie_distill_step)."""
+    """(loss, gradient): distill and distill_grad at once (vie_distill_step).
+    The gradient is the caller's to pass on (logits.backward(gradient)); where
+    an input requires one, a backward pass from the loss raises."""
     torch = _torch()
     (lp, dt, N, V, ld), ip, tp, k = _distill_inputs(logits, ids, teacher)
     n = _workspace_bytes("vie_distill_workspace", V, N)
     with _on(logits.device):
         loss = torch.empty(N, dtype=torch.float32, device=logits.device)
-        out, gp, gld, glp = _grad_of(logits, gloss, out)
+        grad, gp, gld, glp = _grad_of(logits, gloss, out)
         ws, wp = _workspace(n, logits.device)
         _check(lib.vie_distill_step(lp, dt, N, V, ld, ip, tp, k, tau, glp, weight, loss.data_ptr(), gp, gld, wp, n,
                                     _raw_stream(logits.device)))
-    return loss, out
+    if out is not None:
+        _overwritten(out)
+    if (logits.requires_grad or teacher.requires_grad) and torch.is_grad_enabled():
+        loss = _recorded()[1](loss)
+    return loss, grad

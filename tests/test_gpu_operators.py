@@ -703,3 +703,116 @@ def test_many_short_rows(vie):
     check_draws(got, z.numpy(), np.arange(40), u.numpy(), 1.0, 7, 0.8, 0.0, "many rows")
     lg, li, un = lists(20000, 9, 2)
     check_draws(vie.sample(*dev(li, lg, un), top_p=0.7), lg, li, un, 1.0, 0, 0.7, 0.0, "many lists")
+
+
+def leaf(t):
+    return t.detach().clone().requires_grad_()
+
+
+@pytest.mark.parametrize("N,V,k,dtype,tau,kind", [(1, 1, 1, F32, 1.0, "plain"), (13, 1000, 50, BF16, 1.0, "odd"),
+                                                  (12, 4099, 2048, F32, 3.0, "odd"), (300, 20000, 64, BF16, 2.0, "odd")])
+def test_distill_is_recorded_by_autograd(vie, N, V, k, dtype, tau, kind):
+    """A backward pass through distill gives distill_grad's values, whatever else is in the loss."""
+    say("autograd", N, V, k, dtype, tau, kind)
+    s, ids, t = distill_inputs(N, V, k, dtype, N + V, kind)
+    idd, td = dev(ids, t)
+    w = torch.randn(N, generator=torch.Generator().manual_seed(1)).cuda()
+    z = leaf(s.cuda())
+    loss, stats = vie.distill(z, idd, td, tau)
+    plain, plain_stats = vie.distill(z.detach(), idd, td, tau)
+    assert loss.requires_grad and not stats.requires_grad and not plain.requires_grad
+    same_bits(loss.detach(), plain)
+    same_bits(stats, plain_stats)
+    for total, gloss in (((loss * w).sum(), w), (loss.sum(), None), (loss.mean(), torch.full_like(w, 1 / N))):
+        (got,) = torch.autograd.grad(total, z, retain_graph=True)
+        same_bits(got, vie.distill_grad(z.detach(), idd, td, stats, tau, gloss=gloss))
+    with torch.no_grad():
+        assert not vie.distill(z, idd, td, tau)[0].requires_grad
+    # beside another term, through a layer before, in strided rows
+    h = torch.randn(N, 8, generator=torch.Generator().manual_seed(2)).cuda()
+    W = leaf(torch.randn(V, 8, generator=torch.Generator().manual_seed(3)).cuda())
+
+    def logits():
+        y = (h @ W.t()).to(dtype)
+        return torch.cat([y, y[:, :1]], 1)[:, :V]
+
+    y = logits()
+    (0.5 * y.float().square().sum() + vie.distill(y, idd, td, tau)[0].sum()).backward()
+    yd = y.detach()
+    dy = vie.distill_grad(yd, idd, td, vie.distill(yd, idd, td, tau)[1], tau)
+    y2 = logits()
+    (want,) = torch.autograd.grad(y2, W, (yd.float() + dy.float()).to(dtype))
+    # (two terms of y's type are added in another order: a rounding of each and of their sum, through 8 products)
+    ok = torch.isfinite(want)
+    size = (yd.float().abs() + dy.float().abs()).nan_to_num(0, 0, 0).t() @ h.abs()
+    tol = 4 * torch.finfo(dtype).eps * size + 1e-5
+    assert bool(((W.grad - want).abs() <= tol)[ok].all()) and bool((ok == torch.isfinite(W.grad)).all())
+
+
+def test_distill_step_gives_its_gradient_once(vie):
+    """The step's gradient is its second result; a backward pass from its loss says so instead of giving nothing."""
+    say("autograd, step")
+    s, ids, t = distill_inputs(5, 300, 20, F32, 3)
+    idd, td = dev(ids, t)
+    z = leaf(s.cuda())
+    loss, grad = vie.distill_step(z, idd, td, 2.0, weight=0.2)
+    assert not grad.requires_grad
+    z.backward(grad)
+    same_bits(z.grad, vie.distill_step(z.detach(), idd, td, 2.0, weight=0.2)[1])
+    with pytest.raises(RuntimeError, match="second result"):
+        (z.square().mean() + loss.mean()).backward()
+    assert not vie.distill_step(z.detach(), idd, td, 2.0)[0].requires_grad
+    with torch.no_grad():
+        assert not vie.distill_step(z, idd, td, 2.0)[0].requires_grad
+    with pytest.raises(ValueError, match="detach"):
+        vie.distill(z, idd, leaf(td), 2.0)
+
+
+def test_autograd_sees_tensors_written_over(vie):
+    """A tensor that a backward pass needs is not overwritten behind its back."""
+    say("autograd, out=")
+    V, d, B, k = 500, 64, 4, 10
+    q, scale, h = int8_inputs(V, d, B, F32, 1)
+    head = vie.Int8Head(q.cuda(), scale.cuda())
+    s, ids, t = distill_inputs(B, V, k, F32, 2)
+    idd, td = dev(ids, t)
+    stats = vie.distill(s.cuda(), idd, td)[1]
+    for write in (lambda y: head(h.cuda(), out=y), lambda y: vie.distill_step(y.detach(), idd, td, out=y),
+                  lambda y: vie.distill_grad(y.detach(), idd, td, stats, out=y)):
+        y = leaf(s.cuda()).exp()  # (whose backward pass needs y itself)
+        write(y)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            y.sum().backward()
+        z = leaf(s.cuda()) * 1.0
+        loss = vie.distill(z, idd, td)[0]
+        write(z)
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            loss.sum().backward()
+
+
+def test_recorded_distillation_in_a_graph(vie):
+    """Forward and backward passes captured, replayed with new inputs, with eager passes between."""
+    say("autograd, captured")
+    N, V, k = 6, 3001, 12
+    s, ids, t = distill_inputs(N, V, k, BF16, 11)
+    idd, td = dev(ids, t)
+    w = torch.rand(N, generator=torch.Generator().manual_seed(4)).cuda()
+
+    def both(z):
+        loss = vie.distill(z, idd, td, 2.0)[0]
+        return loss.detach(), torch.autograd.grad((loss * w).sum(), z)[0]
+
+    both(leaf(s.cuda()))
+    torch.cuda.synchronize()
+    z = leaf(s.cuda())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = both(z)
+    for rep in range(3):
+        with torch.no_grad():
+            z.copy_(torch.randn(N, V, generator=torch.Generator().manual_seed(rep)))
+        want = both(leaf(z))
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y in zip(out, want):
+            same_bits(x, y)

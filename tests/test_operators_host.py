@@ -153,3 +153,9 @@ def test_binding_refuses_host_tensors_types_and_shapes():
                  lambda: vie.distill_grad(f, i, f, torch.zeros(2, 2))):
         with pytest.raises(ValueError, match="device tensor"):
             call()
+
+
+def test_a_teacher_that_requires_a_gradient_is_refused():
+    f, i = torch.zeros(2, 5), torch.zeros(2, 5, dtype=torch.int32)
+    with pytest.raises(ValueError, match="detach"):
+        vie.distill(f, i, f.clone().requires_grad_())
