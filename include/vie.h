@@ -468,7 +468,8 @@ vie_status vie_distill_grad(const void *logits_dev, vie_dtype dtype, int32_t N, 
                             int64_t grad_ld, void *hip_stream);
 
 /* vie_distill and vie_distill_grad in one call, for a training step that
- * knows g_n beforehand (1 / N for a mean): the same losses and gradients.
+ * knows g_n beforehand (1 / N for a mean): the same losses and gradients, up
+ * to the rounding of a row's sum, which is added in another order.
  * Errors: VIE_EINVAL, VIE_EHIP. */
 vie_status vie_distill_step(const void *logits_dev, vie_dtype dtype, int32_t N, int64_t V, int64_t ld,
                             const int32_t *ids_dev, const float *teacher_dev, int32_t k, float tau,

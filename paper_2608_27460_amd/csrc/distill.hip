@@ -34,8 +34,12 @@ struct Part {
     float m, z;
 };
 __device__ __forceinline__ float term(float s, float m, float c) { return __builtin_amdgcn_exp2f((s - m) * c); }
+// (Contracted to one product and a multiply-add, it would round differently
+// in the two lanes that exchange their parts, and the threads of a row would
+// end with different sums.)
 __device__ __forceinline__ Part merge(Part a, Part b, float c)
 {
+#pragma clang fp contract(off)
     const float m = fmaxf(a.m, b.m);
     return {m, a.z * term(a.m, m, c) + b.z * term(b.m, m, c)};
 }

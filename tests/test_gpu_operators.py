@@ -816,3 +816,24 @@ def test_recorded_distillation_in_a_graph(vie):
         torch.cuda.synchronize()
         for x, y in zip(out, want):
             same_bits(x, y)
+
+
+@pytest.mark.parametrize("N,V,dtype", [(12, 4099, F32), (40, 9001, F32), (130, 20001, BF16), (130, 70001, F32), (3, 150001, F32)])
+def test_distill_step_uses_one_sum_a_row(vie, N, V, dtype):
+    """Equal logits of a row have equal gradients, to the bit, whichever thread
+    stores them; and strides and places change no bit of a step."""
+    say("one sum a row", N, V, dtype)
+    s, ids, t = distill_inputs(N, V, 9, dtype, N + V)
+    s[:, ::2] = 1.25
+    idd, td = dev(ids, t)
+    loss, grad = vie.distill_step(s.cuda(), idd, td, 2.0)
+    same = grad[:, ::2].cpu().float()
+    listed = torch.zeros(N, V, dtype=torch.bool).scatter_(1, torch.from_numpy(ids).long(), True)[:, ::2]
+    for n in range(N):
+        values = same[n][~listed[n]].unique()
+        assert values.numel() == 1, (n, values)
+    view, _ = strided(s, V + 3, 1)
+    out, _ = strided(torch.zeros(N, V, dtype=dtype), V + 7, 3)
+    for x in (vie.distill_step(view, idd, td, 2.0, out=out), vie.distill_step(view, idd, td, 2.0, out=view)):
+        same_bits(x[0], loss)
+        same_bits(x[1], grad)
