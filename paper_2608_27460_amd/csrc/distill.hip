@@ -12,8 +12,9 @@
 // and the sum relative to it, and rescales the sum when the maximum grows.
 // The pair (m, Z) is what the backward pass needs of the forward pass; it
 // is kept as two fp32 numbers rather than as log Z + m / tau, whose rounding
-// would be relative to m.  Sums are fp32 per thread (at most a few hundred
-// terms) and merged pairwise; the list's sums are fp64.
+// would be relative to m.  Sums are fp32 over at most 512 terms of a thread,
+// fp64 over those, and merged pairwise among the threads; the list's sums are
+// fp64.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -52,6 +53,19 @@ template <int N> __device__ __forceinline__ void add(Part &p, const float *f, fl
 #pragma unroll
     for (int i = 0; i < N; ++i) z += term(f[i], m, c);
     p = {m, z};
+}
+// A long row's sum, in 64 bits: what a thread (or a wave) has folded into it
+// after every kFold terms.
+constexpr int kFold = 512;
+struct Folded {
+    float m;
+    double z;
+};
+__device__ __forceinline__ void fold(Folded &all, Part &p, float c)
+{
+    const float m = fmaxf(all.m, p.m);
+    all = {m, all.z * (double)term(all.m, m, c) + (double)(p.z * term(p.m, m, c))};
+    p = {m, 0.0f};
 }
 // The part of W lanes, in each of them.
 template <int W> __device__ __forceinline__ Part wave_merge(Part p, float c)
@@ -294,7 +308,9 @@ constexpr int kFlight = 4;                       // 16-byte loads of a thread in
 constexpr int kMaxParts = 64;                    // of a row
 constexpr int kBackGroups = 4096;                // 16-byte groups of a part of the backward pass
 
-template <bool BF16, int LT>
+// LONG: parts of more than kFold terms a thread (folding in every kernel took
+// 0.2 us of 48 rows of 32768 fp32, and 0.8 of 600 rows of 128256 bf16).
+template <bool BF16, int LT, bool LONG>
 __global__ __launch_bounds__(kThreads) void distill_forward_kernel(DistillLaunch a, int64_t len)
 {
     typedef Elem<BF16> E;
@@ -322,7 +338,8 @@ __global__ __launch_bounds__(kThreads) void distill_forward_kernel(DistillLaunch
     if (full(first)) load(first);
     if (lists) l.template read<BF16>(a.ids + row * a.k, a.teacher + row * a.k, a.V, s, 0, a.V);
     int64_t i = first;
-    while (full(i)) {
+    [[maybe_unused]] Folded all{-FLT_MAX, 0.0};
+    for (int turn = 1; full(i); ++turn) {
 #pragma unroll
         for (int u = 0; u < kFlight; ++u) {
             float f[E::kVec];
@@ -331,6 +348,8 @@ __global__ __launch_bounds__(kThreads) void distill_forward_kernel(DistillLaunch
         }
         i += kFlight * kThreads;
         if (full(i)) load(i);
+        if constexpr (LONG)
+            if (turn % (kFold / (kFlight * E::kVec)) == 0) fold(all, p, c);
     }
     for (; i < groups; i += kThreads) {
         float f[E::kVec];
@@ -340,6 +359,10 @@ __global__ __launch_bounds__(kThreads) void distill_forward_kernel(DistillLaunch
     if (groups * E::kVec + tid < n) {
         const float f = E::get(src[groups * E::kVec + tid]);
         add<1>(p, &f, c);
+    }
+    if constexpr (LONG) {
+        fold(all, p, c);
+        p.z = (float)all.z;
     }
     if (lists) l.sum(a.tau, s_tmp);
     p = block_merge<kThreads>(p, c, s_part);
@@ -486,6 +509,22 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(8, 8))) void
         l.template read<BF16>(a.ids + row * a.k, a.teacher + row * a.k, a.V, src, 0, a.V);
     }
     Part p{-FLT_MAX, 0.0f};
+    // (a wave's sum lies in LDS: the registers are taken.  Only the widest
+    // workgroups take rows of more than two steps.)
+    __shared__ Folded s_all[NT / kLanes];
+    constexpr int kTurns = kFold / (kFlight * E::kVec);
+    const bool folds = NT == 1024 && steps > kTurns;
+    Folded &all = s_all[tid / kLanes];
+    auto fold_wave = [&] {
+        p = wave_merge<kLanes>(p, c);
+        if ((tid & (kLanes - 1)) == 0) {
+            Folded x = all;
+            fold(x, p, c);
+            all = x;
+        }
+        p.z = 0.0f;
+    };
+    if (folds && (tid & (kLanes - 1)) == 0) all = {-FLT_MAX, 0.0};
     for (int j = 0; j < steps; ++j) {
 #pragma unroll
         for (int u = 0; u < kFlight; ++u) {
@@ -493,6 +532,7 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(8, 8))) void
             E::unpack(w[u], f);
             if (at(j, u) < groups) add<E::kVec>(p, f, c);
         }
+        if (folds && (j + 1) % kTurns == 0) fold_wave();
         if (keep && j == steps - 2) {
 #pragma unroll
             for (int u = 0; u < kFlight; ++u) kept[u * NT + tid] = w[u];
@@ -504,6 +544,10 @@ __global__ __launch_bounds__(NT) __attribute__((amdgpu_waves_per_eu(8, 8))) void
     if (tid < rest) {
         tail = E::get(src[last]);
         add<1>(p, &tail, c);
+    }
+    if (folds) {
+        fold_wave();
+        if ((tid & (kLanes - 1)) == 0) p = {all.m, (float)all.z};
     }
     const float g = a.weight * (a.gloss ? a.gloss[row] : 1.0f);
     if (tid < LT) {
@@ -609,7 +653,8 @@ template <bool BF16> vie_status forward(const DistillLaunch &a, hipStream_t s)
     }
     by_list<kThreads>(a.k, [&](auto lt) {
         constexpr int LT = decltype(lt)::value;
-        distill_forward_kernel<BF16, LT><<<sp.grid, kThreads, list_lds(a.k), s>>>(a, sp.len);
+        if (sp.len > kFold * kThreads) distill_forward_kernel<BF16, LT, true><<<sp.grid, kThreads, list_lds(a.k), s>>>(a, sp.len);
+        else distill_forward_kernel<BF16, LT, false><<<sp.grid, kThreads, list_lds(a.k), s>>>(a, sp.len);
         if (sp.parts > 1) distill_join_kernel<BF16, LT><<<a.N, LT, list_lds(a.k), s>>>(a, sp.parts);
     });
     return launched("distillation launch");

@@ -837,3 +837,52 @@ def test_distill_step_uses_one_sum_a_row(vie, N, V, dtype):
     for x in (vie.distill_step(view, idd, td, 2.0, out=out), vie.distill_step(view, idd, td, 2.0, out=view)):
         same_bits(x[0], loss)
         same_bits(x[1], grad)
+
+
+def test_distill_sums_of_very_long_rows(vie):
+    """Equal logits below a thread's largest round the same way in every
+    addition, so that a long fp32 sum runs away from the true one (by 4e-4
+    after 32768 of these, 2e-4 after 16384)."""
+    V, x, tops = 1 << 24, 3.5, 2048
+    Z = tops + (V - tops) * np.exp(-x)
+    # fp32 sums of 512 terms and the merges after them, the exponents; the loss is log Z
+    tol = (512 + 32) * 2.0 ** -24 + (np.log(V) + 3) * 2.0 ** -22 + 2.0 ** -23 * np.log(Z)
+    for N, dtype in ((257, BF16), (130, F32)):
+        say("long rows", N, V, dtype)
+        s = torch.full((N, V), -x, dtype=dtype, device="cuda")
+        s[:, :4 * tops:4] = 0.0
+        ids = torch.full((N, 1), 8, dtype=torch.int32, device="cuda")
+        t = torch.zeros(N, 1, device="cuda")
+        loss, stats = vie.distill(s, ids, t)
+        assert float((loss.double() - np.log(Z)).abs().max()) <= tol
+        assert float((stats[:, 1].double() / Z - 1).abs().max()) <= tol
+        s, ids, t = s[:130], ids[:130], t[:130]  # (in one kernel)
+        loss, grad = vie.distill_step(s, ids, t, out=s)
+        assert float((loss.double() - np.log(Z)).abs().max()) <= tol
+        half = torch.finfo(dtype).eps / 2
+        for at, want in ((slice(4 * tops, V), np.exp(-x) / Z), (slice(0, 8, 4), 1 / Z), (slice(8, 9), 1 / Z - 1)):
+            worst = max(float((grad[n, at].double() / want - 1).abs().max()) for n in range(0, 130, 9))
+            assert worst <= tol + 2.0 ** -21 + half, (at, worst)
+        del s, grad
+
+
+@pytest.mark.parametrize("dtype,V", [(BF16, 300007), (F32, 270001), (BF16, 620001)])
+def test_distill_odd_values_in_long_rows(vie, dtype, V):
+    """Rows of more than 512 terms a thread, among them masked ones and ones with NaN and infinities."""
+    say("long odd rows", dtype, V)
+    n, copies, k, tau, w = 12, 22, 30, 2.0, 0.5
+    s, ids, t = distill_inputs(n, V, k, dtype, V, "odd")
+    g = np.full(n, w)
+    sn = s.float().numpy()
+    ref, grad, Q, P = distill_reference(sn, ids, t, tau, g)
+    sd, idd, td = s.cuda().repeat(copies, 1), *(x.repeat(copies, 1) for x in dev(ids, t))
+    loss, stats = vie.distill(sd, idd, td, tau)
+    back = vie.distill_grad(sd, idd, td, stats, tau, weight=w)
+    step_loss, step_grad = vie.distill_step(sd, idd, td, tau, weight=w, out=sd)
+    for l, d, what in ((loss, back, "apart"), (step_loss, step_grad, "step")):
+        check_loss(l[:n].cpu().numpy(), ref, tau, V, what)
+        check_grad(d[:n].float().cpu().numpy(), grad, Q, P, sn, tau, g, dtype, what)
+        for c in range(1, copies):
+            same_bits(l[c * n:c * n + n], l[:n])
+            i = torch.int32 if dtype == F32 else torch.int16
+            assert torch.equal(d[c * n:c * n + n].view(i), d[:n].view(i))
