@@ -126,22 +126,22 @@ __global__ __launch_bounds__(256) void int8_simple_kernel(const int8_t *__restri
                                                           typename Elem<OUT_BF16>::T *__restrict__ out, int64_t ld)
 {
     const int lane = threadIdx.x & (kLanes - 1), r = lane & 15, g = lane >> 4;
-    const int64_t v0 = ((int64_t)blockIdx.x * 4 + threadIdx.x / kLanes) * 16;
-    const int b0 = blockIdx.y * 16;
+    const int b0 = blockIdx.y * 16, b = b0 + r;
     const int8_t *end = q + V * d;
-    const int8_t *row = q + min(v0 + r, V - 1) * d;
     const int8_t *tok = x + (int64_t)min(b0 + r, B - 1) * padded(d);
-    i32x4 acc = {0, 0, 0, 0};
-    for (int c = 16 * g; c < padded(d); c += kStep) {
-        const word4 w = load16(row + c, end), t = *reinterpret_cast<const word4 *>(tok + c);
-        acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, w), __builtin_bit_cast(i32x4, t), acc, 0, 0, 0);
-    }
-    const int b = b0 + r;
-    if (b >= B) return;
+    for (int64_t v0 = ((int64_t)blockIdx.x * 4 + threadIdx.x / kLanes) * 16; v0 < V; v0 += (int64_t)gridDim.x * 64) {
+        const int8_t *row = q + min(v0 + r, V - 1) * d;
+        i32x4 acc = {0, 0, 0, 0};
+        for (int c = 16 * g; c < padded(d); c += kStep) {
+            const word4 w = load16(row + c, end), t = *reinterpret_cast<const word4 *>(tok + c);
+            acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, w), __builtin_bit_cast(i32x4, t), acc, 0, 0, 0);
+        }
+        if (b >= B) continue;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t v = v0 + 4 * g + i;
-        if (v < V) out[(int64_t)b * ld + v] = Elem<OUT_BF16>::put((float)acc[i] * scale[v] * xs[b]);
+        for (int i = 0; i < 4; ++i) {
+            const int64_t v = v0 + 4 * g + i;
+            if (v < V) out[(int64_t)b * ld + v] = Elem<OUT_BF16>::put((float)acc[i] * scale[v] * xs[b]);
+        }
     }
 }
 
@@ -734,11 +734,13 @@ template <bool H_BF16> hipError_t few_launch(const Int8Launch &a, bool aligned, 
 // lies past d meets zeros of the tokens): a wave per row.
 __global__ __launch_bounds__(256) void repack_kernel(const int8_t *__restrict__ q, int64_t V, int d, int8_t *__restrict__ to, int pitch)
 {
-    const int64_t v = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
-    if (v >= V) return;
-    for (int c = 16 * (threadIdx.x & (kLanes - 1)); c < pitch; c += 16 * kLanes)
-        *reinterpret_cast<word4 *>(to + v * pitch + c) = load16(q + v * d + c, q + V * d);
+    for (int64_t v = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes; v < V; v += (int64_t)gridDim.x * (256 / kLanes))
+        for (int c = 16 * (threadIdx.x & (kLanes - 1)); c < pitch; c += 16 * kLanes)
+            *reinterpret_cast<word4 *>(to + v * pitch + c) = load16(q + v * d + c, q + V * d);
 }
+// Workgroups of 256 threads for n pieces of work: a launch holds fewer than
+// 2^32 threads, so that those of the largest matrices take more than one.
+unsigned grid_of(int64_t n) { return (unsigned)std::min<int64_t>(n, 1 << 22); }
 int row_pitch(int d) { return (d + 15) / 16 * 16; }
 // Whether unaligned rows are copied first: read and written once for it,
 // where int8_simple_kernel reads them for every 16 tokens, and the worse the
@@ -775,11 +777,11 @@ vie_status launch_int8_logits(const Int8Launch &a, hipStream_t s)
     if (copy_rows(a.B, a.d)) {
         int8_t *to = x + ((tokens_bytes(a.d, a.B) + (size_t)a.B * 4 + 255) & ~(size_t)255);
         pitch = row_pitch(a.d);
-        repack_kernel<<<(unsigned)((a.V + 3) / 4), 256, 0, s>>>(a.q, a.V, a.d, to, pitch);
+        repack_kernel<<<grid_of((a.V + 3) / 4), 256, 0, s>>>(a.q, a.V, a.d, to, pitch);
         if (vie_status e = launched("int8 row copy launch")) return e;
         q = to;
     } else if (!aligned) {
-        const dim3 grid((unsigned)((a.V + 63) / 64), (unsigned)((a.B + 15) / 16));
+        const dim3 grid(grid_of((a.V + 63) / 64), (unsigned)((a.B + 15) / 16));
         if (bf16)
             int8_simple_kernel<true><<<grid, 256, 0, s>>>(a.q, a.scale, a.V, a.d, x, xs, a.B, static_cast<uint16_t *>(a.out), a.ld);
         else

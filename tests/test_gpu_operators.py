@@ -886,3 +886,17 @@ def test_distill_odd_values_in_long_rows(vie, dtype, V):
             same_bits(l[c * n:c * n + n], l[:n])
             i = torch.int32 if dtype == F32 else torch.int16
             assert torch.equal(d[c * n:c * n + n].view(i), d[:n].view(i))
+
+
+@pytest.mark.parametrize("V,d,B", [((1 << 26) + 77, 17, 33), ((1 << 30) + 70, 1, 17)])
+def test_int8_more_rows_than_a_launch_has_threads(vie, V, d, B):
+    say("int8, many rows", V, d, B)
+    g = torch.Generator(device="cuda").manual_seed(V)
+    q = torch.randint(-127, 128, (V, d), dtype=torch.int8, device="cuda", generator=g)
+    scale = torch.rand(V, device="cuda", generator=g)
+    h = torch.randn(B, d, generator=torch.Generator().manual_seed(B))
+    out = vie.Int8Head(q, scale)(h.cuda(), dtype=BF16)
+    for at in (0, (1 << 24) - 50, (1 << 26) - 50, (1 << 28) - 50, (1 << 30) - 50, V - 100):
+        part = slice(at, at + 100)
+        if at < V:
+            same_bits(out[:, part].contiguous(), int8_reference(q[part].cpu(), scale[part].cpu(), h, BF16))
