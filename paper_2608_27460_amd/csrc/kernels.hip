@@ -1573,15 +1573,15 @@ __global__ __launch_bounds__(kQuantWaves *kWave) void quantize_kernel(const void
                                                                       float *__restrict__ scale)
 {
     const int lane = threadIdx.x & (kWave - 1);
-    const int64_t row = (int64_t)blockIdx.x * kQuantWaves + threadIdx.x / kWave;
-    if (row >= V) return;
-    float mx = 0.0f;
-    for (int j = lane; j < d; j += kWave) mx = fmaxf(mx, fabsf(stored_at<BF16>(W, row * d + j)));
+    for (int64_t row = (int64_t)blockIdx.x * kQuantWaves + threadIdx.x / kWave; row < V; row += (int64_t)gridDim.x * kQuantWaves) {
+        float mx = 0.0f;
+        for (int j = lane; j < d; j += kWave) mx = fmaxf(mx, fabsf(stored_at<BF16>(W, row * d + j)));
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, kWave));
-    const float sc = __fdiv_rn(mx, 127.0f);
-    for (int j = lane; j < d; j += kWave) q[row * d + j] = quantize_one(stored_at<BF16>(W, row * d + j), sc);
-    if (lane == 0) scale[row] = sc;
+        for (int o = 32; o >= 1; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o, kWave));
+        const float sc = __fdiv_rn(mx, 127.0f);
+        for (int j = lane; j < d; j += kWave) q[row * d + j] = quantize_one(stored_at<BF16>(W, row * d + j), sc);
+        if (lane == 0) scale[row] = sc;
+    }
 }
 
 // ---------------------------------------------------------------------------
@@ -3935,7 +3935,8 @@ vie_status launch_forced(const HnswLaunch &a, const int32_t *forced, int n, hipS
 
 vie_status launch_quantize_rows(const void *W, int dtype, int64_t V, int d, int8_t *q, float *scale, hipStream_t s)
 {
-    const unsigned grid = (unsigned)((V + kQuantWaves - 1) / kQuantWaves);
+    // (a launch holds fewer than 2^32 threads)
+    const unsigned grid = (unsigned)std::min<int64_t>((V + kQuantWaves - 1) / kQuantWaves, 1 << 22);
     if (dtype == VIE_BF16) quantize_kernel<true><<<grid, kQuantWaves * kWave, 0, s>>>(W, V, d, q, scale);
     else quantize_kernel<false><<<grid, kQuantWaves * kWave, 0, s>>>(W, V, d, q, scale);
     return launched(hipGetLastError(), "row quantization launch");

@@ -900,3 +900,15 @@ def test_int8_more_rows_than_a_launch_has_threads(vie, V, d, B):
         part = slice(at, at + 100)
         if at < V:
             same_bits(out[:, part].contiguous(), int8_reference(q[part].cpu(), scale[part].cpu(), h, BF16))
+
+
+def test_quantize_more_rows_than_a_launch_has_threads(vie):
+    V, d = (1 << 26) + 77, 3
+    say("quantize_rows, many rows", V, d)
+    W = torch.randn(V, d, device="cuda", generator=torch.Generator(device="cuda").manual_seed(1))
+    q, scale = vie.quantize_rows(W, synth.F32)
+    for at in (0, 300, 1 << 24, (1 << 26) - 50, V - 100):
+        w = W[at:at + 100].cpu().numpy()
+        sc = (np.abs(w).max(1) / np.float32(127)).astype(np.float32)
+        assert np.array_equal(scale[at:at + 100].cpu().numpy(), sc)
+        assert np.array_equal(q[at:at + 100].cpu().numpy(), np.clip(np.rint((w / sc[:, None]).astype(np.float32)), -127, 127))
