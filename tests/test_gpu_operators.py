@@ -912,3 +912,74 @@ def test_quantize_more_rows_than_a_launch_has_threads(vie):
         sc = (np.abs(w).max(1) / np.float32(127)).astype(np.float32)
         assert np.array_equal(scale[at:at + 100].cpu().numpy(), sc)
         assert np.array_equal(q[at:at + 100].cpu().numpy(), np.clip(np.rint((w / sc[:, None]).astype(np.float32)), -127, 127))
+
+
+def test_the_largest_vocabulary(vie):
+    """2^31 - 1 ids, the most that the calls accept."""
+    V = (1 << 31) - 1
+    say("largest vocabulary")
+    s = torch.full((1, V), -20.0, dtype=BF16, device="cuda")
+    tops = [5, 1 << 30, V - 1]
+    s[0, tops] = torch.tensor([1.0, 3.0, 2.0], dtype=BF16, device="cuda")
+    w = np.exp(np.array([3.0, 2.0, 1.0]) - 3)
+    order = [1 << 30, V - 1, 5]
+    for u, at in ((0.0, 0), (0.66, 0), (0.67, 1), (0.9, 1), (0.92, 2), (0.999, 2)):
+        tok, prob, kept = vie.sample_rows(s, torch.full((1,), u, device="cuda"), top_k=3)
+        assert (int(tok), int(kept)) == (order[at], 3) and abs(float(prob) - w[at] / w.sum()) <= 2.0 ** -23
+    tok, prob, kept = vie.sample_rows(s, torch.zeros(1, device="cuda"), temperature=0.0)
+    assert (int(tok), float(prob), int(kept)) == (1 << 30, 1.0, 1)
+    s.fill_(1.0)  # all alike: the token follows from its number
+    tok, prob, kept = vie.sample_rows(s, torch.full((1,), 0.75, device="cuda"))
+    assert (int(tok), int(kept)) == (int(0.75 * V), V) and abs(float(prob) * V - 1) <= 2.0 ** -23
+    s.fill_(-20.0)
+    s[0, tops] = torch.tensor([1.0, 3.0, 2.0], dtype=BF16, device="cuda")
+    ids = torch.tensor([tops + [-1, 77]], dtype=torch.int32, device="cuda")
+    t = torch.tensor([[0.0, 1.0, 2.0, 9.0, -1.0]], device="cuda")
+    Z = w.sum() + (V - 3) * np.exp(-23.0)
+    logq = np.array([-2.0, 0.0, -1.0, -23.0]) - np.log(Z)
+    y = np.array([0.0, 1.0, 2.0, -1.0])
+    p = np.exp(y) / np.exp(y).sum()
+    want = float((p * (np.log(p) - logq)).sum())
+    loss, grad = vie.distill_step(s, ids, t, out=s)
+    assert abs(float(loss) - want) <= (512 + 32) * 2.0 ** -24 + (np.log(V) + 3) * 2.0 ** -22 + 2.0 ** -23 * want
+    for at, pj, lq in zip(tops + [77, 100, V - 2], list(p) + [0, 0], list(logq) + [logq[3]] * 2):
+        q = np.exp(lq)
+        assert abs(float(grad[0, at]) - (q - pj)) <= 2.0 ** -8 * abs(q - pj) + 1e-4 * q + 2.0 ** -22 * pj
+    del s, grad
+    q = torch.randint(-127, 128, (V, 1), dtype=torch.int8, device="cuda", generator=torch.Generator(device="cuda").manual_seed(2))
+    scale = torch.ones(V, device="cuda")
+    scale[-200:] = 0.25
+    h = torch.tensor([[3.5]])
+    out = vie.Int8Head(q, scale)(h.cuda(), dtype=BF16)
+    for at in (0, (1 << 30) - 50, V - 250):
+        part = slice(at, at + 250)
+        same_bits(out[:, part].contiguous(), int8_reference(q[part].cpu(), scale[part].cpu(), h, BF16))
+
+
+@pytest.mark.parametrize("V,d,B", [(50257, 1000, 32), (3001, 65, 17), (2049, 1001, 31), (70001, 3, 20), (333, 2047, 18),
+                                   (17, 1, 17), (65, 63, 32), (1000, 2033, 29), (64, 2041, 24), (1, 2000, 25)])
+@pytest.mark.parametrize("ht,ot,odd", [(F32, BF16, 0), (BF16, F32, 0), (BF16, BF16, 1), (F32, F32, 7)])
+def test_int8_unaligned_rows_read_for_every_16_tokens(vie, V, d, B, ht, ot, odd):
+    """17 to 32 tokens over rows of up to 2048 bytes that are no multiple of
+    16: pieces that reach into the next row, and past the matrix's end."""
+    say("int8 17-32 tokens, unaligned", V, d, B, ht, ot, odd)
+    q, scale, h = int8_inputs(V, d, B, ht, V + d)
+    buf = torch.full((odd + V * d,), 127, dtype=torch.int8).cuda()
+    view = buf[odd:].view(V, d)
+    view.copy_(q)
+    head, ref = vie.Int8Head(view, scale.cuda()), int8_reference(q, scale, h, ot)
+    same_bits(head(h.cuda(), dtype=ot), ref)
+    out, obuf = strided(torch.zeros(B, V, dtype=ot), V + 3, 1)
+    head(h.cuda(), out=out)
+    same_bits(out, ref)
+    assert bool((between(obuf, B, V, V + 3, 1) == 77.0).all())
+
+
+@pytest.mark.parametrize("V,d,B", [(300, 48, 17), (1001, 2064, 40), (77, 8192, 33), (2000, 112, 300)])
+def test_int8_rows_at_an_odd_address_and_many_tokens(vie, V, d, B):
+    say("int8 odd address, many tokens", V, d, B)
+    q, scale, h = int8_inputs(V, d, B, F32, V + d)
+    buf = torch.full((9 + V * d,), 127, dtype=torch.int8).cuda()
+    view = buf[9:].view(V, d)
+    view.copy_(q)
+    same_bits(vie.Int8Head(view, scale.cuda())(h.cuda()), int8_reference(q, scale, h, F32))
