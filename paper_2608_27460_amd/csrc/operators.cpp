@@ -3,6 +3,8 @@
 // anything is enqueued.
 #include <hip/hip_runtime.h>
 
+#include <initializer_list>
+
 #include "operators.hpp"
 
 using namespace vie;
@@ -29,6 +31,14 @@ vie_status check_matrix(const void *p, int32_t dtype, int64_t V, int64_t ld, con
     if (ld < V || ld >= (int64_t(1) << 40))
         return fail(VIE_EINVAL, "row stride %lld of %s outside [V, 2^40)", (long long)ld, what);
     if ((uintptr_t)p % elem_bytes(dtype)) return fail(VIE_EINVAL, "%s is not aligned to its type", what);
+    return VIE_OK;
+}
+
+// Arrays of 4-byte values.
+vie_status check_words(std::initializer_list<const void *> arrays)
+{
+    for (const void *p : arrays)
+        if ((uintptr_t)p % 4) return fail(VIE_EINVAL, "an array of 4-byte values is not aligned to its type");
     return VIE_OK;
 }
 
@@ -85,6 +95,9 @@ template <int N> vie_status check_ranges(const Range (&r)[N], int n_out)
 }
 vie_status check_sample(const SampleLaunch &a)
 {
+    if (vie_status s = check_words({a.token, a.prob, a.kept, a.u, a.ids, a.prm.temperature_dev, a.prm.top_k_dev,
+                                    a.prm.top_p_dev, a.prm.min_p_dev}))
+        return s;
     const size_t n = (size_t)a.B * 4;
     const Range r[] = {{a.token, n}, {a.prob, n}, {a.kept, n}, {a.u, n}, {a.logits, matrix_bytes(a.B, a.n, a.ld, a.dtype)},
                        {a.ids, n * (size_t)a.n}, {a.prm.temperature_dev, n}, {a.prm.top_k_dev, n},
@@ -104,10 +117,11 @@ vie_status check_apart(const DistillLaunch &a)
         return fail(VIE_EINVAL, "the gradient overlaps the logits without being in their place");
     return VIE_OK;
 }
-// What is written of a distillation apart from the rest (but for a gradient
+// Every array aligned, and what is written of a distillation apart from the rest (but for a gradient
 // in place of the logits).
 vie_status check_distilled(const DistillLaunch &a, bool stats_out)
 {
+    if (vie_status s = check_words({a.ids, a.teacher, a.loss, a.stats, a.gloss})) return s;
     const size_t n = (size_t)a.N * 4, list = n * (size_t)a.k;
     const Range g{a.grad, a.grad ? matrix_bytes(a.N, a.V, a.grad_ld, a.dtype) : 0};
     const Range logits{a.grad == a.logits ? nullptr : a.logits, matrix_bytes(a.N, a.V, a.ld, a.dtype)};
@@ -142,7 +156,7 @@ vie_status vie_int8_logits(const int8_t *q_dev, const float *scale_dev, int64_t 
     if (d < 1 || d > kMaxD) return fail(VIE_EINVAL, "d = %d out of range [1, %d]", d, kMaxD);
     if (vie_status s = check_matrix(h_dev, h_dtype, d, d, "h")) return s;
     if (vie_status s = check_matrix(out_dev, out_dtype, V, out_ld, "the logits")) return s;
-    if ((uintptr_t)scale_dev % 4) return fail(VIE_EINVAL, "scale is not aligned to its type");
+    if (vie_status s = check_words({scale_dev})) return s;
     const size_t n = matrix_bytes(B, V, out_ld, out_dtype);
     if (overlap(out_dev, n, q_dev, (size_t)V * d) || overlap(out_dev, n, scale_dev, (size_t)V * 4) ||
         overlap(out_dev, n, h_dev, (size_t)B * d * elem_bytes(h_dtype)))
@@ -160,6 +174,7 @@ vie_status vie_sample(const int32_t *ids_dev, const float *logits_dev, int32_t B
     if (!ids_dev || !logits_dev || !params || !u_dev || !token_dev) return fail(VIE_EINVAL, "NULL argument");
     if (vie_status s = check_rows(B, 1)) return s;
     if (vie_status s = check_list(k)) return s;
+    if (vie_status s = check_words({logits_dev})) return s;
     const SampleLaunch a{ids_dev, logits_dev, VIE_F32, k, k, B, *params, u_dev, token_dev, prob_dev, kept_dev, nullptr};
     if (vie_status s = check_sample(a)) return s;
     return launch_sample_lists(a, static_cast<hipStream_t>(hip_stream));

@@ -159,3 +159,27 @@ def test_a_teacher_that_requires_a_gradient_is_refused():
     f, i = torch.zeros(2, 5), torch.zeros(2, 5, dtype=torch.int32)
     with pytest.raises(ValueError, match="detach"):
         vie.distill(f, i, f.clone().requires_grad_())
+
+
+def test_arrays_that_are_not_aligned_are_refused():
+    """Every array of 4-byte values, one and two bytes past its place."""
+    at = {name: (i + 1) << 20 for i, name in enumerate("abcdefghij")}
+    B, V, k = 3, 50, 5
+
+    def prm(x):
+        return C.byref(vie.SamplingParams(1.0, 1.0, 0.0, 0, x["g"], x["h"], x["i"], x["j"]))
+
+    calls = {
+        "abcdefghij": lambda x: L.vie_sample(x["a"], x["b"], B, k, prm(x), x["c"], x["d"], x["e"], x["f"], None),
+        "acdefghij": lambda x: L.vie_sample_rows(x["a"], vie.F32, V, V, B, prm(x), x["c"], x["d"], x["e"], x["f"], P, BIG, None),
+        "abcde": lambda x: L.vie_distill(x["a"], vie.F32, B, V, V, x["b"], x["c"], k, 1.0, x["d"], x["e"], P, BIG, None),
+        "abcdef": lambda x: L.vie_distill_grad(x["a"], vie.F32, B, V, V, x["b"], x["c"], k, 1.0, x["e"], x["f"], 1.0, x["d"], V, None),
+        "fabcde": lambda x: L.vie_distill_step(x["a"], vie.F32, B, V, V, x["b"], x["c"], k, 1.0, x["f"], 1.0, x["e"], x["d"], V, P,
+                                               BIG, None),
+        "abc": lambda x: L.vie_int8_logits(P, x["a"], V, 8, x["b"], vie.F32, B, x["c"], vie.F32, V, P, BIG, None),
+    }
+    for names, call in calls.items():
+        for name in names:
+            for off in (1, 2):
+                assert call({**at, name: at[name] + off}) == vie.EINVAL, (names, name, off)
+                assert b"aligned" in L.vie_last_error(), (names, name, off)
