@@ -291,7 +291,7 @@ constexpr int kBinsPer = kBins / kRowThreads;
 constexpr int kCollect = 2048;             // candidates put in order one by one
 constexpr int kMaxParts = 128;
 constexpr int kMaxSlots = 256;             // bins that borders can fall into
-constexpr int kMaxRows = 1024;             // rows of one round of launches (114 KB of workspace each)
+constexpr int kTies = 8;                   // border bins that may be too full to be collected
 
 // Bins of a row of this best key: `of` is monotone in the logit and 0 at the
 // best one.
@@ -338,6 +338,17 @@ struct RowSpace {
     uint64_t key[kCollect];
     uint32_t count[kBins];
     uint32_t pass, collected, done, unused;
+};
+static_assert(kMaxParts * kTies * 2 <= kCollect, "the parts' counts take the place of the collected keys");
+// The same where one workgroup takes the row, whose bins and keys stay in LDS.
+struct OneSpace {
+    uint64_t key[kTies * 2];
+    uint32_t collected, done;
+};
+// What the draw uses of either.
+struct Exchange {
+    uint64_t *key;
+    uint32_t *collected, *done;
 };
 
 // A candidate's place in the order: how many and how much weight come up to
@@ -501,10 +512,9 @@ __device__ __forceinline__ Result draw_by_digits(const Row<BF16> &row, const Wei
     return drawn(weights, at.key, end.sum, end.rank);
 }
 
-// Workgroup (c, i) takes part c of row b0 + i in each of the three kernels.
+// Workgroup (c, b) takes part c of row b in each of the three kernels.
 struct Parts {
     int64_t len;  // candidates of a part
-    int b0;
     RowSpace *ws;
 };
 template <bool BF16> __device__ __forceinline__ Row<BF16> row_of(const SampleLaunch &a, int b)
@@ -526,8 +536,8 @@ template <bool BF16> __device__ __forceinline__ uint64_t best_of(const Row<BF16>
 template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_best_kernel(SampleLaunch a, Parts parts)
 {
     __shared__ uint64_t tmp[kRowWaves];
-    const int b = parts.b0 + blockIdx.y, c = blockIdx.x, S = gridDim.x;
-    RowSpace &ws = parts.ws[blockIdx.y];
+    const int b = blockIdx.y, c = blockIdx.x, S = gridDim.x;
+    RowSpace &ws = parts.ws[b];
     for (int i = c * kRowThreads + threadIdx.x; i < kBins; i += S * kRowThreads) ws.sum[i] = 0, ws.count[i] = 0;
     if (c == 0 && threadIdx.x == 0) ws.pass = ws.collected = ws.done = 0;
     const Row<BF16> row = row_of<BF16>(a, b);
@@ -636,8 +646,8 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_bins_ke
 {
     extern __shared__ __align__(16) char smem[];
     BinLds<BF16> &s = *reinterpret_cast<BinLds<BF16> *>(smem);
-    const int b = parts.b0 + blockIdx.y, tid = threadIdx.x;
-    RowSpace &ws = parts.ws[blockIdx.y];
+    const int b = blockIdx.y, tid = threadIdx.x;
+    RowSpace &ws = parts.ws[b];
     const Settings st = settings(a.prm, b);
     const Row<BF16> row = row_of<BF16>(a, b);
     s.clear();
@@ -798,12 +808,10 @@ struct Borders {
 // bin are counted, and the lowest and the highest of them kept; the last part
 // to finish has those of all.  Returns 0 in the others, 1 with the result,
 // and 2, in the last part, if a bin holds more than one value.
-constexpr int kTies = 8;
-static_assert(kMaxParts * kTies * 2 <= kCollect, "the parts' counts take the place of the collected keys");
 template <bool BF16>
 __device__ __forceinline__ int draw_ties(const Row<BF16> &row, const Weights &weights, const Bins<BF16> &bin_map,
                                       const Settings &st, float u, const Borders &known, int nslot, int64_t len,
-                                      RowSpace &ws, DrawLds &s, Result &out)
+                                      const Exchange &ws, DrawLds &s, Result &out)
 {
     typedef Elem<BF16> E;
     const int tid = threadIdx.x, S = gridDim.x, part = blockIdx.x;
@@ -829,7 +837,7 @@ __device__ __forceinline__ int draw_ties(const Row<BF16> &row, const Weights &we
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    if (tid == 0) s.last = __hip_atomic_fetch_add(&ws.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (tid == 0) s.last = __hip_atomic_fetch_add(ws.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     if (s.last != (uint32_t)S - 1) return 0;
     // all parts' counts, and a bin's value and number
@@ -920,13 +928,13 @@ __device__ __forceinline__ int draw_ties(const Row<BF16> &row, const Weights &we
 template <bool BF16>
 __device__ __forceinline__ void draw_row(const SampleLaunch &a, int b, const Row<BF16> &row, const Settings &st, float u,
                                          const Weights &weights, const Bins<BF16> &bin_map, const uint32_t (&cnt)[kBinsPer],
-                                         const uint64_t (&sum)[kBinsPer], uint32_t pass, int64_t len, RowSpace &ws, DrawLds &s);
+                                         const uint64_t (&sum)[kBinsPer], uint32_t pass, int64_t len, const Exchange &ws, DrawLds &s);
 
 template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_kernel(SampleLaunch a, Parts parts)
 {
     extern __shared__ __align__(16) char smem[];
-    const int b = parts.b0 + blockIdx.y, tid = threadIdx.x;
-    RowSpace &ws = parts.ws[blockIdx.y];
+    const int b = blockIdx.y, tid = threadIdx.x;
+    RowSpace &ws = parts.ws[b];
     // the bins (read while the row's settings are)
     uint32_t cnt[kBinsPer];
     uint64_t sum[kBinsPer];
@@ -951,17 +959,17 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_draw_ke
         return;
     }
     draw_row<BF16>(a, b, row, st, u, Weights(key_logit(best), st.t, fixed_shift(a.n)), Bins<BF16>(best), cnt, sum, pass,
-                   parts.len, ws, *reinterpret_cast<DrawLds *>(smem));
+                   parts.len, Exchange{ws.key, &ws.collected, &ws.done}, *reinterpret_cast<DrawLds *>(smem));
 }
 
 // The three kernels in one, for rows of one part: a workgroup's row, whose
 // bins stay in LDS.
-template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_one_kernel(SampleLaunch a, Parts parts)
+template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_one_kernel(SampleLaunch a)
 {
     extern __shared__ __align__(16) char smem[];
     BinLds<BF16> &s = *reinterpret_cast<BinLds<BF16> *>(smem + sizeof(DrawLds));
-    const int b = parts.b0 + blockIdx.y, tid = threadIdx.x;
-    RowSpace &ws = parts.ws[blockIdx.y];
+    const int b = blockIdx.y, tid = threadIdx.x;
+    OneSpace &ws = static_cast<OneSpace *>(a.ws)[b];
     const Settings st = settings(a.prm, b);
     const float u = a.u[b];
     const Row<BF16> row = row_of<BF16>(a, b);
@@ -986,13 +994,14 @@ template <bool BF16> __global__ __launch_bounds__(kRowThreads) void rows_one_ker
     }
     s.add_pass(passed);
     __syncthreads();
-    draw_row<BF16>(a, b, row, st, u, weights, bin_map, cnt, sum, s.pass, parts.len, ws, *reinterpret_cast<DrawLds *>(smem));
+    draw_row<BF16>(a, b, row, st, u, weights, bin_map, cnt, sum, s.pass, a.n, Exchange{ws.key, &ws.collected, &ws.done},
+                   *reinterpret_cast<DrawLds *>(smem));
 }
 
 template <bool BF16>
 __device__ __forceinline__ void draw_row(const SampleLaunch &a, int b, const Row<BF16> &row, const Settings &st, float u,
                                          const Weights &weights, const Bins<BF16> &bin_map, const uint32_t (&cnt)[kBinsPer],
-                                         const uint64_t (&sum)[kBinsPer], uint32_t pass, int64_t len, RowSpace &ws, DrawLds &s)
+                                         const uint64_t (&sum)[kBinsPer], uint32_t pass, int64_t len, const Exchange &ws, DrawLds &s)
 {
     const int tid = threadIdx.x, S = gridDim.x;
     uint32_t c = 0;
@@ -1145,7 +1154,7 @@ __device__ __forceinline__ void draw_row(const SampleLaunch &a, int b, const Row
     __syncthreads();
     if (S > 1) {
         const uint32_t mine = s.base;
-        if (tid == 0) s.last = atomicAdd(&ws.collected, mine);
+        if (tid == 0) s.last = atomicAdd(ws.collected, mine);
         __syncthreads();
         // Stores and loads at the device's point of coherence: no cache is
         // written back for them (with fences, which do that, the kernel took
@@ -1155,7 +1164,7 @@ __device__ __forceinline__ void draw_row(const SampleLaunch &a, int b, const Row
             __hip_atomic_store(&ws.key[s.last + i], s.d.key[i], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        if (tid == 0) s.last = __hip_atomic_fetch_add(&ws.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (tid == 0) s.last = __hip_atomic_fetch_add(ws.done, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         __syncthreads();
         if (s.last != (uint32_t)S - 1) return;
         for (uint32_t i = tid; i < M; i += kRowThreads)
@@ -1248,7 +1257,30 @@ vie_status launched(const char *what)
 
 }  // namespace
 
-size_t sample_rows_workspace_bytes(int64_t, int B) { return (size_t)std::min(B, kMaxRows) * sizeof(RowSpace); }
+// Parts of a row: one workgroup a CU (64 rows of 151936 bf16: 46 us so, 69
+// with two, 57 with half of one), of 4096 candidates at least (one row of
+// 262144 fp32 in parts of 2048: 30.5 us, of 4096: 27.1, of 8192: 27.7, of
+// 16384: 31.2; of 50000: 22.6, 23.4, 24.5 and 28.1).
+static int parts_of(int64_t V, int B)
+{
+    return (int)std::max<int64_t>(1, std::min<int64_t>({(V + 4095) / 4096, 256 / B, kMaxParts}));
+}
+// A workgroup a row in one kernel takes some 13 us and 5 for every 10000
+// logits of up to 256 rows, three kernels 21 and more with the work of a
+// CU.  In us, fp32, three kernels and one: 1 row of 4096 21.6 and 15.1, of
+// 16384 23.4 and 21.2, of 32000 23.4 and 28.9; 64 rows of 32000 37 and 31,
+// of 50257 40 and 40, of 128256 53 and 81; 128 of 128256 71 and 80; 200 of
+// 128256 99 and 83; 1000 of 4096 103 and 58.
+constexpr int64_t kOne = 16384, kOneRow = 512;
+static bool one_kernel(int64_t V, int B) { return parts_of(V, B) == 1 || V <= kOne + kOneRow * B; }
+
+// Enough for fewer rows, too: the most of them that take three kernels.
+size_t sample_rows_workspace_bytes(int64_t V, int B)
+{
+    static_assert(kOne > 4096, "up to 128 rows of more have parts");
+    const int64_t three = V > kOne ? std::min<int64_t>({B, 128, (V - 1 - kOne) / kOneRow}) : 0;
+    return std::max((size_t)three * sizeof(RowSpace), B * sizeof(OneSpace));
+}
 
 vie_status launch_sample_lists(const SampleLaunch &a, hipStream_t s)
 {
@@ -1265,21 +1297,7 @@ vie_status launch_sample_lists(const SampleLaunch &a, hipStream_t s)
 namespace {
 template <bool BF16> vie_status rows_launch(const SampleLaunch &a, hipStream_t s)
 {
-    // Parts of a row: one workgroup a CU (64 rows of 151936 bf16: 46 us so, 69
-    // with two, 57 with half of one), of 4096 candidates at least (one row of
-    // 262144 fp32 in parts of 2048: 30.5 us, of 4096: 27.1, of 8192: 27.7, of
-    // 16384: 31.2; of 50000: 22.6, 23.4, 24.5 and 28.1).
-    const int64_t want = std::min<int64_t>((a.n + 4095) / 4096, 256 / a.B);
-    const int S = (int)std::max<int64_t>(1, std::min<int64_t>(want, kMaxParts));
-    const int64_t len = ((a.n + S - 1) / S + 63) / 64 * 64;
     constexpr int kBinsLds = sizeof(BinLds<BF16>), kOneLds = sizeof(DrawLds) + sizeof(BinLds<BF16>);
-    // A workgroup a row in one kernel takes some 13 us and 5 for every 10000
-    // logits of up to 256 rows, three kernels 21 and more with the work of a
-    // CU.  In us, fp32, three kernels and one: 1 row of 4096 21.6 and 15.1, of
-    // 16384 23.4 and 21.2, of 32000 23.4 and 28.9; 64 rows of 32000 37 and 31,
-    // of 50257 40 and 40, of 128256 53 and 81; 128 of 128256 71 and 80; 200 of
-    // 128256 99 and 83; 1000 of 4096 103 and 58.
-    const bool one = S == 1 || a.n <= 16384 + 512 * (int64_t)a.B;
     hipError_t e = hipFuncSetAttribute((const void *)rows_draw_kernel<BF16>, hipFuncAttributeMaxDynamicSharedMemorySize,
                                        (int)sizeof(DrawLds));
     if (e == hipSuccess)
@@ -1287,13 +1305,12 @@ template <bool BF16> vie_status rows_launch(const SampleLaunch &a, hipStream_t s
     if (e == hipSuccess)
         e = hipFuncSetAttribute((const void *)rows_one_kernel<BF16>, hipFuncAttributeMaxDynamicSharedMemorySize, kOneLds);
     if (e != hipSuccess) return fail(VIE_EHIP, "row sampling: %s", hipGetErrorString(e));
-    for (int b0 = 0; b0 < a.B; b0 += kMaxRows) {
-        const Parts parts{len, b0, static_cast<RowSpace *>(a.ws)};
-        const dim3 grid((unsigned)((a.n + len - 1) / len), (unsigned)std::min(kMaxRows, a.B - b0));
-        if (one) {
-            rows_one_kernel<BF16><<<dim3(1, grid.y), kRowThreads, kOneLds, s>>>(a, Parts{a.n, b0, static_cast<RowSpace *>(a.ws)});
-            continue;
-        }
+    if (one_kernel(a.n, a.B)) {
+        rows_one_kernel<BF16><<<dim3(1, a.B), kRowThreads, kOneLds, s>>>(a);
+    } else {
+        const int S = parts_of(a.n, a.B);
+        const Parts parts{((a.n + S - 1) / S + 63) / 64 * 64, static_cast<RowSpace *>(a.ws)};
+        const dim3 grid((unsigned)((a.n + parts.len - 1) / parts.len), (unsigned)a.B);
         rows_best_kernel<BF16><<<grid, kRowThreads, 0, s>>>(a, parts);
         rows_bins_kernel<BF16><<<grid, kRowThreads, kBinsLds, s>>>(a, parts);
         rows_draw_kernel<BF16><<<grid, kRowThreads, sizeof(DrawLds), s>>>(a, parts);

@@ -983,3 +983,28 @@ def test_int8_rows_at_an_odd_address_and_many_tokens(vie, V, d, B):
     view = buf[9:].view(V, d)
     view.copy_(q)
     same_bits(vie.Int8Head(view, scale.cuda())(h.cuda()), int8_reference(q, scale, h, F32))
+
+
+@pytest.mark.parametrize("V,dtype", [(40, F32), (17500, BF16), (30000, F32), (81000, F32), (90000, BF16)])
+def test_sample_rows_stays_in_its_workspace(vie, V, dtype):
+    """A workspace for the most rows serves fewer; nothing is written past the
+    size asked for, with rows that are drawn from bins, ties and digits."""
+    say("sampling workspace", V, dtype)
+    most = 200
+    need = vie._workspace_bytes("vie_sample_rows_workspace", V, most)
+    ws = torch.empty(need + 4096, dtype=torch.uint8, device="cuda")
+    z, u = row_logits(most, V, dtype, V, False)
+    z[::3] = 2.5                                                                         # ties
+    z[1::3] = 10 + 1e-2 * torch.randn(z[1::3].shape, generator=torch.Generator().manual_seed(1)).to(dtype)  # one bin, many values
+    z, u = z.cuda(), u.cuda()
+    prm = vie.SamplingParams(1.0, 0.9, 0.0, 0)
+    for B in (1, 2, 7, 8, 9, 31, 127, 128, 129, most):
+        own = vie._workspace_bytes("vie_sample_rows_workspace", V, B)
+        assert own <= need
+        want = vie.sample_rows(z[:B], u[:B], top_p=0.9)
+        got = vie._drawn(B, z.device)
+        ws.fill_(0x5A)
+        vie._check(vie.lib.vie_sample_rows(z.data_ptr(), vie._dtype_of_tensor(z), V, V, B, vie.C.byref(prm), u.data_ptr(),
+                                           *(x.data_ptr() for x in got), ws.data_ptr(), need, vie._raw_stream(z.device)))
+        assert all(torch.equal(x, y) for x, y in zip(got, want)), B
+        assert bool((ws[own:] == 0x5A).all()), B

@@ -183,3 +183,20 @@ def test_arrays_that_are_not_aligned_are_refused():
             for off in (1, 2):
                 assert call({**at, name: at[name] + off}) == vie.EINVAL, (names, name, off)
                 assert b"aligned" in L.vie_last_error(), (names, name, off)
+
+
+def test_sampling_workspace_is_what_the_rows_need():
+    """Little for short rows, whatever their number, and enough for fewer rows and shorter ones."""
+    def need(V, B):
+        n = C.c_size_t()
+        assert L.vie_sample_rows_workspace(V, B, C.byref(n)) == vie.OK
+        return n.value
+
+    assert need(40, 1024) <= 1024 * 256 and need(4096, 65535) <= 65535 * 256
+    sizes = [1, 40, 4096, 4097, 16384, 16385, 16896, 16897, 20000, 50257, 81920, 81921, 128256, 262144, 1 << 24, (1 << 31) - 1]
+    rows = [*range(1, 140), 255, 256, 257, 1023, 1024, 1025, 65535]
+    for V in sizes:
+        assert all(need(V, a) <= need(V, b) for a, b in zip(rows, rows[1:])), V
+    for B in rows:
+        assert all(need(a, B) <= need(b, B) for a, b in zip(sizes, sizes[1:])), B
+    assert need(262144, 1024) <= 128 * 120000
