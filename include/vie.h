@@ -366,9 +366,9 @@ vie_status vie_scatter(const int32_t *ids_dev, const float *logits_dev, int32_t 
  * V; what lies between rows is neither read nor written.  Every array is
  * aligned to its type, and outputs overlap neither inputs nor each other, but
  * for a gradient in place of its logits (VIE_EINVAL).  Workspaces are 256-byte
- * aligned device buffers of the caller's, need no initialisation, and carry
- * data between the kernels of one call only: calls that share one must not
- * overlap in time. */
+ * aligned device buffers of the caller's, apart from every other argument
+ * (VIE_EINVAL), need no initialisation, and carry data between the kernels of
+ * one call only: calls that share one must not overlap in time. */
 
 /* Bytes of device workspace vie_int8_logits needs for these sizes. */
 vie_status vie_int8_logits_workspace(int64_t V, int32_t d, int32_t B, size_t *bytes);

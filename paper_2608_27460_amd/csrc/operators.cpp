@@ -83,26 +83,26 @@ struct Range {
     const void *p;
     size_t bytes;
 };
-// Outputs (the first n_out ranges) apart from each other and from the inputs;
-// a NULL range is none.
+// What is written (the first n_out ranges) apart from each other and from the
+// inputs; a NULL range is none.
 template <int N> vie_status check_ranges(const Range (&r)[N], int n_out)
 {
     for (int i = 0; i < n_out; ++i)
         for (int j = i + 1; j < N; ++j)
             if (r[i].p && r[j].p && overlap(r[i].p, r[i].bytes, r[j].p, r[j].bytes))
-                return fail(VIE_EINVAL, "an output overlaps another argument");
+                return fail(VIE_EINVAL, "an output or the workspace overlaps another argument");
     return VIE_OK;
 }
-vie_status check_sample(const SampleLaunch &a)
+vie_status check_sample(const SampleLaunch &a, size_t ws_bytes)
 {
     if (vie_status s = check_words({a.token, a.prob, a.kept, a.u, a.ids, a.prm.temperature_dev, a.prm.top_k_dev,
                                     a.prm.top_p_dev, a.prm.min_p_dev}))
         return s;
     const size_t n = (size_t)a.B * 4;
-    const Range r[] = {{a.token, n}, {a.prob, n}, {a.kept, n}, {a.u, n}, {a.logits, matrix_bytes(a.B, a.n, a.ld, a.dtype)},
+    const Range r[] = {{a.token, n}, {a.prob, n}, {a.kept, n}, {a.ws, ws_bytes}, {a.u, n}, {a.logits, matrix_bytes(a.B, a.n, a.ld, a.dtype)},
                        {a.ids, n * (size_t)a.n}, {a.prm.temperature_dev, n}, {a.prm.top_k_dev, n},
                        {a.prm.top_p_dev, n}, {a.prm.min_p_dev, n}};
-    return check_ranges(r, 3);
+    return check_ranges(r, 4);
 }
 
 // The gradient's rows are the logits' own or apart from them.
@@ -127,9 +127,9 @@ vie_status check_distilled(const DistillLaunch &a, bool stats_out)
     const Range logits{a.grad == a.logits ? nullptr : a.logits, matrix_bytes(a.N, a.V, a.ld, a.dtype)};
     const Range stats{a.stats, 2 * n};
     const Range none{nullptr, 0};
-    const Range r[] = {g, {a.loss, n}, stats_out ? stats : none, logits, stats_out ? none : stats, {a.ids, list},
+    const Range r[] = {g, {a.loss, n}, stats_out ? stats : none, {a.ws, distill_workspace_bytes(a.V, a.N)}, logits, stats_out ? none : stats, {a.ids, list},
                        {a.teacher, list}, {a.gloss, n}};
-    return check_ranges(r, 3);
+    return check_ranges(r, 4);
 }
 
 }  // namespace
@@ -157,11 +157,11 @@ vie_status vie_int8_logits(const int8_t *q_dev, const float *scale_dev, int64_t 
     if (vie_status s = check_matrix(h_dev, h_dtype, d, d, "h")) return s;
     if (vie_status s = check_matrix(out_dev, out_dtype, V, out_ld, "the logits")) return s;
     if (vie_status s = check_words({scale_dev})) return s;
-    const size_t n = matrix_bytes(B, V, out_ld, out_dtype);
-    if (overlap(out_dev, n, q_dev, (size_t)V * d) || overlap(out_dev, n, scale_dev, (size_t)V * 4) ||
-        overlap(out_dev, n, h_dev, (size_t)B * d * elem_bytes(h_dtype)))
-        return fail(VIE_EINVAL, "the logits overlap the inputs");
-    if (vie_status s = check_workspace(workspace_dev, workspace_bytes, int8_workspace_bytes(V, d, B))) return s;
+    const size_t need = int8_workspace_bytes(V, d, B);
+    if (vie_status s = check_workspace(workspace_dev, workspace_bytes, need)) return s;
+    const Range r[] = {{out_dev, matrix_bytes(B, V, out_ld, out_dtype)}, {need ? workspace_dev : nullptr, need},
+                       {q_dev, (size_t)V * d}, {scale_dev, (size_t)V * 4}, {h_dev, (size_t)B * d * elem_bytes(h_dtype)}};
+    if (vie_status s = check_ranges(r, 2)) return s;
     const Int8Launch a{q_dev, scale_dev, V, d, h_dev, h_dtype, B, out_dev, out_dtype, out_ld, workspace_dev};
     return launch_int8_logits(a, static_cast<hipStream_t>(hip_stream));
 }
@@ -176,7 +176,7 @@ vie_status vie_sample(const int32_t *ids_dev, const float *logits_dev, int32_t B
     if (vie_status s = check_list(k)) return s;
     if (vie_status s = check_words({logits_dev})) return s;
     const SampleLaunch a{ids_dev, logits_dev, VIE_F32, k, k, B, *params, u_dev, token_dev, prob_dev, kept_dev, nullptr};
-    if (vie_status s = check_sample(a)) return s;
+    if (vie_status s = check_sample(a, 0)) return s;
     return launch_sample_lists(a, static_cast<hipStream_t>(hip_stream));
 }
 
@@ -197,10 +197,11 @@ vie_status vie_sample_rows(const void *logits_dev, vie_dtype dtype, int64_t V, i
     if (!logits_dev || !params || !u_dev || !token_dev) return fail(VIE_EINVAL, "NULL argument");
     if (vie_status s = check_rows(B, V)) return s;
     if (vie_status s = check_matrix(logits_dev, dtype, V, ld, "logits")) return s;
-    if (vie_status s = check_workspace(workspace_dev, workspace_bytes, sample_rows_workspace_bytes(V, B))) return s;
+    const size_t need = sample_rows_workspace_bytes(V, B);
+    if (vie_status s = check_workspace(workspace_dev, workspace_bytes, need)) return s;
     const SampleLaunch a{nullptr, logits_dev, dtype, V, ld, B, *params, u_dev, token_dev, prob_dev, kept_dev,
                          workspace_dev};
-    if (vie_status s = check_sample(a)) return s;
+    if (vie_status s = check_sample(a, need)) return s;
     return launch_sample_rows(a, static_cast<hipStream_t>(hip_stream));
 }
 

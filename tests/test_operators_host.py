@@ -200,3 +200,30 @@ def test_sampling_workspace_is_what_the_rows_need():
     for B in rows:
         assert all(need(a, B) <= need(b, B) for a, b in zip(sizes, sizes[1:])), B
     assert need(262144, 1024) <= 128 * 120000
+
+
+def test_workspaces_that_overlap_are_refused():
+    """A workspace over any other argument, by its first byte and by its last 256."""
+    at = {name: (i + 1) << 24 for i, name in enumerate("abcdefghij")}
+    B, V, k = 40, 70000, 5
+    n = C.c_size_t()
+
+    def prm(x):
+        return C.byref(vie.SamplingParams(1.0, 1.0, 0.0, 0, x["g"], x["h"], x["i"], x["j"]))
+
+    four, lst, row = 4 * B, 4 * B * k, 4 * B * V
+    for query, sizes, names, call in (
+            (lambda: L.vie_sample_rows_workspace(V, B, C.byref(n)), (V, B), "acdefghij",
+             lambda x, ws: L.vie_sample_rows(x["a"], vie.F32, V, V, B, prm(x), x["c"], x["d"], x["e"], x["f"], ws, BIG, None)),
+            (lambda: L.vie_distill_workspace(V, B, C.byref(n)), (V, B), "abcde",
+             lambda x, ws: L.vie_distill(x["a"], vie.F32, B, V, V, x["b"], x["c"], k, 1.0, x["d"], x["e"], ws, BIG, None)),
+            (lambda: L.vie_distill_workspace(V, B, C.byref(n)), (V, B), "abcdef",
+             lambda x, ws: L.vie_distill_step(x["a"], vie.F32, B, V, V, x["b"], x["c"], k, 1.0, x["f"], 1.0, x["e"], x["d"], V, ws,
+                                              BIG, None)),
+            (lambda: L.vie_int8_logits_workspace(V, 33, B, C.byref(n)), (V, B), "abcd",
+             lambda x, ws: L.vie_int8_logits(x["a"], x["b"], V, 33, x["c"], vie.F32, B, x["d"], vie.F32, V, ws, BIG, None))):
+        assert query() == vie.OK and n.value >= 256
+        for name in names:
+            for ws in (at[name], at[name] - (n.value - 4) // 256 * 256):
+                assert call(at, C.c_void_p(ws)) == vie.EINVAL, (names, name)
+                assert b"overlap" in L.vie_last_error(), (names, name, L.vie_last_error())
