@@ -1265,20 +1265,23 @@ static int parts_of(int64_t V, int B)
 {
     return (int)std::max<int64_t>(1, std::min<int64_t>({(V + 4095) / 4096, 256 / B, kMaxParts}));
 }
-// A workgroup a row in one kernel takes some 13 us and 5 for every 10000
-// logits of up to 256 rows, three kernels 21 and more with the work of a
-// CU.  In us, fp32, three kernels and one: 1 row of 4096 21.6 and 15.1, of
-// 16384 23.4 and 21.2, of 32000 23.4 and 28.9; 64 rows of 32000 37 and 31,
-// of 50257 40 and 40, of 128256 53 and 81; 128 of 128256 71 and 80; 200 of
-// 128256 99 and 83; 1000 of 4096 103 and 58.
-constexpr int64_t kOne = 16384, kOneRow = 512;
-static bool one_kernel(int64_t V, int B) { return parts_of(V, B) == 1 || V <= kOne + kOneRow * B; }
+// A workgroup a row in one kernel, or three kernels.  In us, one and three:
+//                  fp32                                bf16
+//     1 row    of  8192 16.0 19.9, of 16384 19.5 19.7    16384 18.3 20.7
+//              of 24000 24.4 20.7, of 50257 37.8 21.3    24000 21.8 20.7
+//     8 rows   of 20000 22.9 21.8, of 32000 28.8 22.5    20000 20.1 22.1, 32000 25.5 23.0
+//    64 rows   of 32000 30.1 35.0, of 50257 40.5 36.2    50257 33.5 37.4, 80000 46.3 40.5
+//   128 rows   of 60000 45.7 46.0, of 80000 57.0 53.3    80000 46.2 47.0, 128256 66.6 59.8
+static bool one_kernel(int64_t V, int B, bool bf16)
+{
+    return parts_of(V, B) == 1 || V <= (bf16 ? 20480 + 512 * (int64_t)B : 16384 + 352 * (int64_t)B);
+}
 
-// Enough for fewer rows, too: the most of them that take three kernels.
+// Enough for either type, and for fewer rows, too: the most of them (of up to
+// 128, which have parts) that take three kernels, of fp32.
 size_t sample_rows_workspace_bytes(int64_t V, int B)
 {
-    static_assert(kOne > 4096, "up to 128 rows of more have parts");
-    const int64_t three = V > kOne ? std::min<int64_t>({B, 128, (V - 1 - kOne) / kOneRow}) : 0;
+    const int64_t three = V > 16384 ? std::min<int64_t>({B, 128, (V - 1 - 16384) / 352}) : 0;
     return std::max((size_t)three * sizeof(RowSpace), B * sizeof(OneSpace));
 }
 
@@ -1305,7 +1308,7 @@ template <bool BF16> vie_status rows_launch(const SampleLaunch &a, hipStream_t s
     if (e == hipSuccess)
         e = hipFuncSetAttribute((const void *)rows_one_kernel<BF16>, hipFuncAttributeMaxDynamicSharedMemorySize, kOneLds);
     if (e != hipSuccess) return fail(VIE_EHIP, "row sampling: %s", hipGetErrorString(e));
-    if (one_kernel(a.n, a.B)) {
+    if (one_kernel(a.n, a.B, BF16)) {
         rows_one_kernel<BF16><<<dim3(1, a.B), kRowThreads, kOneLds, s>>>(a);
     } else {
         const int S = parts_of(a.n, a.B);
