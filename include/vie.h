@@ -370,15 +370,18 @@ vie_status vie_scatter(const int32_t *ids_dev, const float *logits_dev, int32_t 
  * (VIE_EINVAL), need no initialisation, and carry data between the kernels of
  * one call only: calls that share one must not overlap in time. */
 
-/* Bytes of device workspace vie_int8_logits needs for these sizes. */
+/* Bytes of device workspace vie_int8_logits needs for these sizes: none for a
+ * few tokens, B d rounded up for more, and where d is no multiple of 16 and B
+ * above 32 (or d above 2048 and B too many to be held: 16 and fewer) a copy
+ * of the matrix besides, V times d rounded up to 16. */
 vie_status vie_int8_logits_workspace(int64_t V, int32_t d, int32_t B, size_t *bytes);
 
 /* The head on int8 rows (quantized data types are the paper's future work,
  * Section 5): the full-vocabulary logits of B tokens from q_dev int8[V][d]
  * and scale_dev fp32[V], as vie_quantize_rows writes them (values in [-127,
- * 127]; any alignment).  Each token h_dev [B][d] of h_dtype is quantized by
- * the same rule (scale xs, values x; a token with a NaN or an infinity gets
- * the scale NaN), and
+ * 127]; any alignment, but rows at multiples of 16 bytes are read fastest).
+ * Each token h_dev [B][d] of h_dtype is quantized by the same rule (scale xs,
+ * values x; a token with a NaN or an infinity gets the scale NaN), and
  *   out[b][v] = fp32(fp32(fp32(sum_j q[v][j] x[b][j]) scale[v]) xs[b])
  * with an exact integer sum, rounded to nearest even if out_dtype is
  * VIE_BF16.  out_dev [B][out_ld] does not overlap the inputs.
@@ -448,7 +451,9 @@ vie_status vie_distill_workspace(int64_t V, int32_t N, size_t *bytes);
  * (entries whose p_j rounds to zero add nothing).  An id listed more than
  * once counts with each of its entries.  A row that lists nothing has loss 0.
  * A NaN or +inf among the logits of either side gives NaN, as does a row of
- * the student's that is -inf throughout.  loss_dev fp32[N]; stats_dev
+ * the student's that is -inf throughout.  The sum behind q is fp32 over 512
+ * terms of a thread, fp64 over those; its rounding enters the loss times
+ * tau^2.  loss_dev fp32[N]; stats_dev
  * fp32[N][2] receives what vie_distill_grad needs: the row's largest logit
  * and the sum of exp((s - largest) / tau).
  * Errors: VIE_EINVAL, VIE_EHIP. */

@@ -298,9 +298,9 @@ __device__ __forceinline__ float exponent_scale(float tau) { return (float)(1.44
 // ---------------------------------------------------------------------------
 //
 // Both are bound by memory where there are rows enough: 2048 rows of 128256
-// bf16 forward in 92 us (5.7 TB/s read), backward in 177 (5.9 TB/s read and
+// bf16 forward in 98 us (5.4 TB/s read), backward in 177 (5.9 TB/s read and
 // written).  Few rows are bound by one workgroup's way through a row: 48 rows
-// of 32768 fp32 forward in 7 us, of which a launch is 3.5.
+// of 32768 fp32 forward in 6 us, of which a launch is 3.5.
 
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kLanes;
@@ -465,8 +465,10 @@ __global__ __launch_bounds__(kThreads) void distill_backward_kernel(DistillLaunc
 // second reading finds what the caches hold of the first.  What it took last
 // stays in the registers, and what it took before that in LDS if all the
 // workgroups of a CU have room for it: a row of two steps is read once.
-// 2048 rows of 128256 bf16, 1.05 GB read and written: 207 us, what a copy of
-// the same bytes takes (197).
+// 2048 rows of 128256 bf16, 1.05 GB read and written: 200 to 208 us, what a
+// copy of the same bytes takes (197 to 212).  Lists that all threads take
+// (LT = NT) cost 2 to 4 vector registers, in scratch memory: 4096 rows of 32000
+// with lists of 300 in 188 us.
 
 // Groups of 16 bytes that a workgroup of NT threads takes at a time.
 template <int NT> constexpr int kStep = kFlight * NT;

@@ -173,16 +173,21 @@ __global__ __launch_bounds__(256) void int8_simple_kernel(const int8_t *__restri
 // the next tile go on arriving meanwhile.
 //
 // The waits count the loads and stores (vmcnt) that this source issues: a
-// kernel of these that spilled registers would wait for its own too.
+// kernel of these that spilled vector registers would wait for its own too.
+// (None does; those of the held tokens spill some 60 scalar registers, to
+// lanes of vector ones, which takes no load.)
 //
 // What bounds it: up to 128 tokens the reading of the rows (151936 x 1024, 1
-// token: 28 us or 5.6 TB/s; 128256 x 2048, 64 tokens: 60 us with the tokens'
-// own kernel, 4.7 TB/s of rows and logits together).  With more, a compute
-// unit's loads and its products, which take 301 and 318 us of 2048 tokens' 506
-// if each is alone, at the clock (1.9 GHz) that the matrix cores leave: 2.1e15
-// operations a second, where the library's product of 8192^3 reaches 2.0e15.
-// Four waves of 128 x 128, which read a third less from LDS and whose matrix
-// instructions follow each other without a pause, are no faster (560 us).
+// token: 33 us or 4.8 TB/s where each call has other rows, 28 where the
+// last-level cache holds some of them; 128256 x 2048, 64 tokens: 55 us and 5
+// of the tokens' own kernel, 5.1 TB/s of rows and logits together).  With
+// more, a compute unit's loads and its products: 301 and 318 us of 2048
+// tokens' 506 if each is alone, at the clock (1.9 GHz) that the matrix cores
+// leave.  It takes 500 to 560 us from call to call, 1.9e15 to 2.1e15
+// operations a second; the library's product of 8192^3 reaches 2.0e15 to
+// 2.1e15.  Four waves of 128 x 128, which read a third less from LDS and whose
+// matrix instructions follow each other without a pause, are no faster (562 us
+// beside 506).
 
 constexpr int kWaves = 8;
 constexpr int kThreads = kWaves * kLanes;
@@ -198,8 +203,8 @@ __device__ __forceinline__ void load_lds16(const int8_t *src, char *dst)
 }
 
 // 16 bytes to any alignment.  PAST: past the caches' keeping, for logits of
-// many tokens, which would push the rows and tokens out of L2 (2048 tokens:
-// 559 us without, 535 with).
+// many tokens, which would push the rows and tokens out of L2 (2048 tokens, in
+// turn: 528 to 535 us without, 509 to 520 with).
 template <bool PAST> __device__ __forceinline__ void store16(char *o, word4 w)
 {
     typedef word4 any_word4 __attribute__((aligned(2)));
@@ -218,7 +223,10 @@ constexpr int tile_lds(int stage, int NBUF, int MT, bool held) { return stage * 
 // than tokens_kernel's launch, held and apart in us: 32000 x 256, 4 tokens
 // 6.5 and 8.1, 16 tokens 8.6 and 8.5; 151936 x 1024, 4 tokens 33.6 and 35.6,
 // 12 tokens 35.6 and 36.2, 16 tokens 37.4 and 36.8; 128256 x 2048, 4 tokens
-// 51.1 and 52.4, 12 tokens 55.0 and 53.8; 32000 x 8192, 1 token 71 and 64.
+// 51.1 and 52.4, 12 tokens 55.0 and 53.8.  Wider rows gain nothing: 128256 x
+// 2304, 1 token 50.0 and 50.4; x 2560, 1 token 59.0 and 59.6, 6 tokens 61.5
+// and 61.3; 32000 x 2560, 1 token 18.8 and 18.6; x 4096 27.4 and 24.6; x 8192
+// 53 and 46.
 inline bool hold_tokens(int64_t V, int B, int d, bool aligned)
 {
     if (aligned) return B <= 12 && d <= 2048 && B * padded(d) <= 12 * 1024;
@@ -633,8 +641,8 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))
         multiply(cur);
         if constexpr (!AHEAD && KS == 2) {
             // The operands of the first products, then one of the second ones
-            // with every two products (2048 tokens of 128256 x 2048: 528 us
-            // as the compiler orders them, 506 so).
+            // with every two products (2048 tokens of 128256 x 2048, in turn:
+            // 538 to 543 us as the compiler orders them, 509 to 520 so).
             constexpr int kReads = MT + NT, kProducts = MT * NT;
             __builtin_amdgcn_sched_group_barrier(0x100, kReads, 0);
 #pragma unroll
