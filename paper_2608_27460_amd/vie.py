@@ -384,6 +384,7 @@ def scatter(ids, logits, V: int):
 
 # ---------------------------------------------------------------------------
 # around the head's logits: the int8 head, the token drawn, distillation
+# (of which autograd records the losses of distill alone)
 # ---------------------------------------------------------------------------
 
 _SAME_DEVICE = contextlib.nullcontext()

@@ -1008,3 +1008,28 @@ def test_sample_rows_stays_in_its_workspace(vie, V, dtype):
                                            *(x.data_ptr() for x in got), ws.data_ptr(), need, vie._raw_stream(z.device)))
         assert all(torch.equal(x, y) for x, y in zip(got, want)), B
         assert bool((ws[own:] == 0x5A).all()), B
+
+
+def test_the_most_rows(vie):
+    """65535 rows, the most that the calls accept."""
+    B = 65535
+    say("most rows")
+    z, u = row_logits(B, 21, BF16, 5, False)
+    got = vie.sample_rows(z.cuda(), u.cuda(), top_k=5, top_p=0.8)
+    some = np.r_[0:300, 32700:33000, B - 300:B]
+    check_draws([x[some] for x in got], z.float().numpy()[some], np.arange(21), u.numpy()[some], 1.0, 5, 0.8, 0.0, "most rows")
+    lg, ids, un = lists(B, 3, 6)
+    got = vie.sample(*dev(ids, lg, un), top_p=0.9)
+    check_draws([x[some] for x in got], lg[some], ids[some], un[some], 1.0, 0, 0.9, 0.0, "most lists")
+    s, ids, t = distill_inputs(B, 9, 3, BF16, 7)
+    idd, td = dev(ids, t)
+    sn = s.float().numpy()[some]
+    ref, grad, Q, P = distill_reference(sn, ids[some], t[some], 2.0, np.ones(some.size))
+    loss, stats = vie.distill(s.cuda(), idd, td, 2.0)
+    back = vie.distill_grad(s.cuda(), idd, td, stats, 2.0)
+    for l, g in ((loss, back), vie.distill_step(s.cuda(), idd, td, 2.0)):
+        check_loss(l.cpu().numpy()[some], ref, 2.0, 9, "most rows")
+        check_grad(g.float().cpu().numpy()[some], grad, Q, P, sn, 2.0, np.ones(some.size), BF16, "most rows")
+    for d in (16, 23):
+        q, scale, h = int8_inputs(40, d, B, BF16, d)
+        same_bits(vie.Int8Head(q.cuda(), scale.cuda())(h.cuda()), int8_reference(q, scale, h, F32))
