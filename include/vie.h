@@ -368,7 +368,8 @@ vie_status vie_scatter(const int32_t *ids_dev, const float *logits_dev, int32_t 
  * for a gradient in place of its logits (VIE_EINVAL).  Workspaces are 256-byte
  * aligned device buffers of the caller's, apart from every other argument
  * (VIE_EINVAL), need no initialisation, and carry data between the kernels of
- * one call only: calls that share one must not overlap in time. */
+ * one call only: calls that share one must not overlap in time.  A workspace
+ * for some number of rows (B, N) serves fewer of them, too. */
 
 /* Bytes of device workspace vie_int8_logits needs for these sizes: none for a
  * few tokens, B d rounded up for more, and where d is no multiple of 16 and B

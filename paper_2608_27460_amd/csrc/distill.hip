@@ -717,7 +717,10 @@ template <bool BF16> vie_status step(const DistillLaunch &a, hipStream_t s)
 
 }  // namespace
 
-size_t distill_workspace_bytes(int64_t, int N) { return parts_bytes(N) + (size_t)N * 8; }
+size_t distill_workspace_bytes(int64_t, int N)  // (enough for fewer rows, which may have parts)
+{
+    return parts_bytes(std::min(N, 256)) + (size_t)N * 8;
+}
 
 vie_status launch_distill(const DistillLaunch &a, hipStream_t s)
 {

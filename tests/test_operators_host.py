@@ -227,3 +227,19 @@ def test_workspaces_that_overlap_are_refused():
             for ws in (at[name], at[name] - (n.value - 4) // 256 * 256):
                 assert call(at, C.c_void_p(ws)) == vie.EINVAL, (names, name)
                 assert b"overlap" in L.vie_last_error(), (names, name, L.vie_last_error())
+
+
+def test_a_workspace_serves_fewer_rows():
+    """What a call asks for never grows as its rows become fewer."""
+    n = C.c_size_t()
+    rows = [*range(1, 70), 127, 128, 129, 255, 256, 257, 258, 300, 1000, 1024, 1025, 40000, 65535]
+    queries = [lambda V, B: L.vie_sample_rows_workspace(V, B, C.byref(n)), lambda V, B: L.vie_distill_workspace(V, B, C.byref(n))]
+    queries += [lambda V, B, d=d: L.vie_int8_logits_workspace(V, d, B, C.byref(n))
+                for d in (1, 15, 16, 256, 1000, 1024, 2047, 2048, 2049, 2064, 4096, 8191, 8192)]
+    for query in queries:
+        for V in (1, 7, 1000, 17000, 50257, 262144):
+            need = []
+            for B in rows:
+                assert query(V, B) == vie.OK
+                need.append(n.value)
+            assert need == sorted(need), V
