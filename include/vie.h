@@ -363,7 +363,8 @@ vie_status vie_scatter(const int32_t *ids_dev, const float *logits_dev, int32_t 
  * Around the head's logits: the int8 head, the token drawn, distillation
  * ------------------------------------------------------------------------
  * Full-vocabulary rows may be strided: row b starts at element b * ld, ld >=
- * V; what lies between rows is neither read nor written.  Every array is
+ * V; what lies between rows is neither read nor written, and may hold another
+ * argument (of two matrices, if their strides are the same).  Every array is
  * aligned to its type, and outputs overlap neither inputs nor each other, but
  * for a gradient in place of its logits (VIE_EINVAL).  Workspaces are 256-byte
  * aligned device buffers of the caller's, apart from every other argument

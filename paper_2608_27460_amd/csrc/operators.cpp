@@ -68,28 +68,37 @@ vie_status check_distill(const void *logits, int32_t dtype, int32_t N, int64_t V
     return VIE_OK;
 }
 
-bool overlap(const void *a, size_t an, const void *b, size_t bn)
-{
-    return (uintptr_t)a < (uintptr_t)b + bn && (uintptr_t)b < (uintptr_t)a + an;
-}
-
-// Bytes from the first to the last of `rows` rows of V values, ld apart.
-size_t matrix_bytes(int32_t rows, int64_t V, int64_t ld, int32_t dtype)
-{
-    return ((size_t)(rows - 1) * ld + V) * elem_bytes(dtype);
-}
-
+// Bytes that an argument takes: `bytes` of them, or rows of `width` that begin
+// `stride` apart and take `bytes` from the first to the last.
 struct Range {
     const void *p;
-    size_t bytes;
+    size_t bytes, width = 0, stride = 0;
 };
+Range matrix(const void *p, int32_t rows, int64_t V, int64_t ld, int32_t dtype)
+{
+    const size_t e = elem_bytes(dtype), span = ((size_t)(rows - 1) * ld + V) * e;
+    if (rows == 1) return {p, span};
+    return {p, span, (size_t)V * e, (size_t)ld * e};
+}
+// What lies between the rows of a matrix is not the matrix: another argument
+// may be there (two matrices of one stride only, as in the halves of wider
+// rows).
+bool overlap(const Range &a, const Range &b)
+{
+    const uintptr_t pa = (uintptr_t)a.p, pb = (uintptr_t)b.p;
+    if (pa >= pb + b.bytes || pb >= pa + a.bytes) return false;
+    if (!a.stride) return b.stride ? overlap(b, a) : true;
+    if (b.stride && b.stride != a.stride) return true;
+    const size_t by = pb >= pa ? (pb - pa) % a.stride : (a.stride - (pa - pb) % a.stride) % a.stride;
+    return by < a.width || by + (b.stride ? b.width : b.bytes) > a.stride;
+}
 // What is written (the first n_out ranges) apart from each other and from the
 // inputs; a NULL range is none.
 template <int N> vie_status check_ranges(const Range (&r)[N], int n_out)
 {
     for (int i = 0; i < n_out; ++i)
         for (int j = i + 1; j < N; ++j)
-            if (r[i].p && r[j].p && overlap(r[i].p, r[i].bytes, r[j].p, r[j].bytes))
+            if (r[i].p && r[j].p && overlap(r[i], r[j]))
                 return fail(VIE_EINVAL, "an output or the workspace overlaps another argument");
     return VIE_OK;
 }
@@ -99,7 +108,7 @@ vie_status check_sample(const SampleLaunch &a, size_t ws_bytes)
                                     a.prm.top_p_dev, a.prm.min_p_dev}))
         return s;
     const size_t n = (size_t)a.B * 4;
-    const Range r[] = {{a.token, n}, {a.prob, n}, {a.kept, n}, {a.ws, ws_bytes}, {a.u, n}, {a.logits, matrix_bytes(a.B, a.n, a.ld, a.dtype)},
+    const Range r[] = {{a.token, n}, {a.prob, n}, {a.kept, n}, {a.ws, ws_bytes}, {a.u, n}, matrix(a.logits, a.B, a.n, a.ld, a.dtype),
                        {a.ids, n * (size_t)a.n}, {a.prm.temperature_dev, n}, {a.prm.top_k_dev, n},
                        {a.prm.top_p_dev, n}, {a.prm.min_p_dev, n}};
     return check_ranges(r, 4);
@@ -113,7 +122,7 @@ vie_status check_apart(const DistillLaunch &a)
             return fail(VIE_EINVAL, "a gradient in place of the logits needs their row stride");
         return VIE_OK;
     }
-    if (overlap(a.logits, matrix_bytes(a.N, a.V, a.ld, a.dtype), a.grad, matrix_bytes(a.N, a.V, a.grad_ld, a.dtype)))
+    if (overlap(matrix(a.logits, a.N, a.V, a.ld, a.dtype), matrix(a.grad, a.N, a.V, a.grad_ld, a.dtype)))
         return fail(VIE_EINVAL, "the gradient overlaps the logits without being in their place");
     return VIE_OK;
 }
@@ -123,10 +132,10 @@ vie_status check_distilled(const DistillLaunch &a, bool stats_out)
 {
     if (vie_status s = check_words({a.ids, a.teacher, a.loss, a.stats, a.gloss})) return s;
     const size_t n = (size_t)a.N * 4, list = n * (size_t)a.k;
-    const Range g{a.grad, a.grad ? matrix_bytes(a.N, a.V, a.grad_ld, a.dtype) : 0};
-    const Range logits{a.grad == a.logits ? nullptr : a.logits, matrix_bytes(a.N, a.V, a.ld, a.dtype)};
-    const Range stats{a.stats, 2 * n};
     const Range none{nullptr, 0};
+    const Range g = a.grad ? matrix(a.grad, a.N, a.V, a.grad_ld, a.dtype) : none;
+    const Range logits = a.grad == a.logits ? none : matrix(a.logits, a.N, a.V, a.ld, a.dtype);
+    const Range stats{a.stats, 2 * n};
     const Range r[] = {g, {a.loss, n}, stats_out ? stats : none, {a.ws, distill_workspace_bytes(a.V, a.N)}, logits, stats_out ? none : stats, {a.ids, list},
                        {a.teacher, list}, {a.gloss, n}};
     return check_ranges(r, 4);
@@ -159,7 +168,7 @@ vie_status vie_int8_logits(const int8_t *q_dev, const float *scale_dev, int64_t 
     if (vie_status s = check_words({scale_dev})) return s;
     const size_t need = int8_workspace_bytes(V, d, B);
     if (vie_status s = check_workspace(workspace_dev, workspace_bytes, need)) return s;
-    const Range r[] = {{out_dev, matrix_bytes(B, V, out_ld, out_dtype)}, {need ? workspace_dev : nullptr, need},
+    const Range r[] = {matrix(out_dev, B, V, out_ld, out_dtype), {need ? workspace_dev : nullptr, need},
                        {q_dev, (size_t)V * d}, {scale_dev, (size_t)V * 4}, {h_dev, (size_t)B * d * elem_bytes(h_dtype)}};
     if (vie_status s = check_ranges(r, 2)) return s;
     const Int8Launch a{q_dev, scale_dev, V, d, h_dev, h_dtype, B, out_dev, out_dtype, out_ld, workspace_dev};

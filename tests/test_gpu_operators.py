@@ -1033,3 +1033,44 @@ def test_the_most_rows(vie):
     for d in (16, 23):
         q, scale, h = int8_inputs(40, d, B, BF16, d)
         same_bits(vie.Int8Head(q.cuda(), scale.cuda())(h.cuda()), int8_reference(q, scale, h, F32))
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_arguments_between_the_rows_of_others(vie, dtype):
+    """Logits and their gradient in the two halves of wider rows, and small arrays behind a row."""
+    say("between rows", dtype)
+    N, V, k = 6, 1001, 8
+    s, ids, t = distill_inputs(N, V, k, dtype, 3)
+    idd, td = dev(ids, t)
+    u = torch.rand(N, generator=torch.Generator().manual_seed(1)).cuda()
+    want = [*vie.distill_step(s.cuda(), idd, td, 2.0), *vie.sample_rows(s.cuda(), u, top_p=0.9)]
+    wide = torch.full((N, 2 * V + 30), 77.0, dtype=dtype, device="cuda")
+    z, g = wide[:, :V], wide[:, V:2 * V]
+    z.copy_(s)
+    stats = vie.distill(z, idd, td, 2.0)[1]
+    vie.distill_grad(z, idd, td, stats, 2.0, out=g)
+    back = g.clone()
+    got = [*vie.distill_step(z, idd, td, 2.0, out=g), *vie.sample_rows(z, u, top_p=0.9)]
+    for x, y in zip(got, want):
+        same_bits(x, y) if x.is_floating_point() else None
+        assert torch.equal(torch.nan_to_num(x.float()), torch.nan_to_num(y.float()))
+    same_bits(back, vie.distill_grad(s.cuda(), idd, td, stats, 2.0))
+    same_bits(z, s)
+    assert bool((wide[:, 2 * V:] == 77.0).all())
+    q, scale, h = int8_inputs(V, 33, N, F32, 4)
+    vie.Int8Head(q.cuda(), scale.cuda())(h.cuda(), out=g)
+    same_bits(g, int8_reference(q, scale, h, dtype))
+    same_bits(z, s)
+    # the token's array in the gap behind row 2
+    ld = 2048
+    buf = torch.zeros(N * ld, dtype=dtype, device="cuda")
+    rows = buf.view(N, ld)[:, :V]
+    rows.copy_(s)
+    gap = buf[2 * ld + 1024:].view(torch.int32)[:N]
+    prm = vie.SamplingParams(1.0, 0.9, 0.0, 0)
+    n = vie._workspace_bytes("vie_sample_rows_workspace", V, N)
+    ws = torch.empty(n, dtype=torch.uint8, device="cuda")
+    vie._check(vie.lib.vie_sample_rows(rows.data_ptr(), vie._dtype_of_tensor(rows), V, ld, N, vie.C.byref(prm), u.data_ptr(),
+                                       gap.data_ptr(), None, None, ws.data_ptr(), n, vie._raw_stream(rows.device)))
+    assert torch.equal(gap, want[2])
+    same_bits(rows, s)

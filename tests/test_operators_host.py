@@ -243,3 +243,20 @@ def test_a_workspace_serves_fewer_rows():
                 assert query(V, B) == vie.OK
                 need.append(n.value)
             assert need == sorted(need), V
+
+
+def test_matrices_that_share_rows_of_one_buffer():
+    """Halves of wider rows do not overlap, but any byte of the other half does, and so do other strides."""
+    B, V, ld, k = 4, 50, 128, 5
+    at = (1 << 20)
+    lists = (C.c_void_p(1 << 24), C.c_void_p(1 << 25))
+
+    def grad(logits, out, gld=ld, stats=C.c_void_p(1 << 26)):
+        return L.vie_distill_grad(C.c_void_p(logits), vie.F32, B, V, ld, *lists, k, 1.0, stats, None, 1.0, C.c_void_p(out), gld, None)
+
+    for off in (4, 4 * 49, 4 * (128 - 49), 4 * 127, 4 * 128, 4 * 129, 4 * 3 * 128, -4, -4 * 49, -4 * 128, -4 * (128 + 79)):
+        assert grad(at, at + off) == vie.EINVAL, off
+        assert b"overlap" in L.vie_last_error()
+    assert grad(at, at + 4 * 64, ld + 1) == vie.EINVAL                       # rows of another stride meet them somewhere
+    for off in (-4, 4 * 49, 4 * 128 - 28, 4 * 128 + 40, 4 * (3 * 128 + 49)):  # 32 bytes of statistics, gaps of 200 to 512
+        assert grad(1 << 27, at, stats=C.c_void_p(at + off)) == vie.EINVAL, off
